@@ -324,9 +324,165 @@ WINO_API int wino_decode(const uint16_t *W, int64_t d, int64_t V, int32_t *token
                          wino_block_stats *block_stats, int32_t *next_step);
 
 /*
+ * Attention of a step's rows over a paged cache (Sec. 4.2.2): what makes the
+ * hidden rows that wino_step scores, for callers who run the transformer.
+ * wino_rope_append rotates the new rows' queries and keys and writes their
+ * keys and values into the cache; wino_attend then lets every new row attend
+ * over the cache under the step's mask.  Both take one description of the
+ * batch.
+ *
+ * Rows.  Sequence s has the rows q_start[s] .. q_start[s] + q_len[s] - 1 of q,
+ * k, v and out; its row i is i rows behind q_start[s].  Sequences may come in
+ * any order and leave rows between them, which are neither read nor written;
+ * they must not share rows.  q_len[s] = 0 leaves a sequence out (a finished
+ * one in a batched decode, whose row space stays).
+ *
+ * Cache.  Slot j of sequence s is slot j % page_size of page
+ * page_table[s][j / page_size]; head h of it is at
+ *     page * page_stride + (j % page_size) * slot_stride + h * head_stride
+ * elements behind k_cache or v_cache, so [pages][slots][heads][dim] and
+ * [pages][heads][slots][dim] are both described by their strides.  A slot is
+ * not a position: which rotary position a row has is said to
+ * wino_rope_append alone.  Sequences may share pages that they only read.
+ *
+ * Where new rows are stored, and which slots row i sees:
+ *   WINO_MASK_FULL    stored at slot new_slot + i; sees slots [0, kv_len)
+ *                     (bidirectional: block rows without a shadow block)
+ *   WINO_MASK_CAUSAL  stored at slot new_slot + i; sees slots [0, new_slot + i]
+ *                     below kv_len (prompts, chunks of prompts, single tokens)
+ *   WINO_MASK_SHADOW  wino_step's row order: q_len = 2 L rows, the L block
+ *                     rows, then the L shadow rows.  Block row l is stored at
+ *                     slot new_slot + l, inside [0, kv_len), and sees
+ *                     [0, kv_len).  Shadow row l is stored at slot kv_len + l,
+ *                     and sees [0, kv_len + L) but for slot new_slot + l (the
+ *                     token that it verifies, Sec. 4.2.2).
+ * A row that sees no slot (kv_len = 0, say) gets zeros.  new_slot may be
+ * negative: causal rows before slot 0 see nothing, and rows with a negative
+ * slot are not stored (padding on the left).
+ *
+ * Values: whatever the cache holds in slots that no row of the sequence sees
+ * (behind kv_len, in pages that are not the sequence's) has no effect, not
+ * even as NaN or infinity.  A slot that some rows see and others do not has
+ * to hold finite values, or those others may become NaN too.
+ *
+ * The lengths, slots and pages are read on the device when the call runs, so a
+ * captured call may be replayed with new ones.  What cannot be checked before
+ * is checked there and ends in WINO_ERR_ARG from wino_read_device_status:
+ * rows outside [0, n_rows), a negative length, a table too narrow for a
+ * length, a page outside [0, n_pages) where one is needed, an odd q_len with
+ * WINO_MASK_SHADOW.  Nothing is then read or written out of range; the outputs
+ * of the sequences concerned are undefined.
+ */
+typedef enum {
+    WINO_BF16 = 0, /* elements of q, k, v, out and the cache; all the same type */
+    WINO_FP16 = 1
+} wino_dtype;
+
+typedef enum {
+    WINO_MASK_FULL = 0,
+    WINO_MASK_CAUSAL = 1,
+    WINO_MASK_SHADOW = 2
+} wino_mask;
+
+/* A [n_rows, heads, head_dim] array: element (r, h, c) at data[r * row_stride + h * head_stride + c].  data is 16-byte
+   aligned, the strides (in elements) are multiples of 8 that are at least head_dim where there is more than one row
+   or head.  A part of a fused projection is described as it is. */
+typedef struct {
+    uint16_t *data;
+    int64_t row_stride, head_stride;
+} wino_heads;
+
+/* The batch (host memory, read during the call only; its arrays are device memory). */
+typedef struct {
+    int32_t n_seq;      /* 1..16384 */
+    int32_t n_rows;     /* rows of q, k, v and out, 1..2^24 */
+    int32_t n_q_heads;  /* a multiple of n_kv_heads, at most 128 times as many */
+    int32_t n_kv_heads; /* 1..1024; query head h reads kv head h / (n_q_heads / n_kv_heads) */
+    int32_t head_dim;   /* 8..128, a multiple of 8 */
+    int32_t dtype;      /* wino_dtype */
+    int32_t mask;       /* wino_mask */
+    int32_t page_size;  /* 16, 32, 64 or a multiple of 128 */
+    int32_t n_pages;    /* pages of the cache */
+    int32_t table_width; /* entries of page_table per sequence; table_width * page_size <= 2^30 */
+    const int32_t *q_start, *q_len, *kv_len, *new_slot; /* [n_seq] each */
+    const int32_t *page_table; /* [n_seq, table_width]; entries that hold no slot of the sequence are not read */
+    uint16_t *k_cache, *v_cache; /* 16-byte aligned; written by wino_rope_append only */
+    int64_t page_stride, slot_stride, head_stride; /* of both, in elements: multiples of 8 */
+} wino_kv_batch;
+
+/* Rotary positions.  Pair j < rot_dim / 2 of a head's first rot_dim dims is (j, j + rot_dim / 2), or with
+   `interleaved` (2j, 2j + 1); it is turned by position * freq[j] radians and multiplied by `factor`.  The other dims
+   are copied.  rot_dim = 0 rotates nothing.  Turns are formed in 64-bit fixed point, so far positions keep their
+   angles to 2^-31 turns. */
+typedef struct {
+    int32_t rot_dim;     /* even, 0..head_dim */
+    int32_t interleaved; /* 0: halves, 1: neighbouring pairs */
+    float factor;        /* finite; 1 unless a scaling asks for another */
+    const double *freq;  /* device [rot_dim / 2], 8-byte aligned, see wino_rope_frequencies */
+    const int32_t *positions; /* device [n_rows], or NULL: new_slot + i, and new_slot + l for both rows of a shadow pair */
+} wino_rope;
+
+/*
+ * Rotary frequencies freq[j] = base^(-2j / rot_dim) (host double
+ * [rot_dim / 2]), scaled for contexts `scale` times the trained length:
+ *   WINO_ROPE_PLAIN   as they are (scale is not used)
+ *   WINO_ROPE_LINEAR  divided by scale (position interpolation)
+ *   WINO_ROPE_PARTS   by parts (YaRN, arXiv 2309.00071): with
+ *                     r = trained_len * freq / (2 pi) turns in the trained
+ *                     context, frequencies with r > 32 are kept, with r < 1
+ *                     divided by scale, in between mixed linearly in r; and
+ *                     *factor = 0.1 ln(scale) + 1
+ * *factor is 1 for the others.  Pure host code.  WINO_ERR_SHAPE for an odd or
+ * negative rot_dim or one above 128, WINO_ERR_ARG for null pointers, base <= 1, scale < 1,
+ * trained_len < 1 (PARTS), or values that are not finite.
+ */
+typedef enum { WINO_ROPE_PLAIN = 0, WINO_ROPE_LINEAR = 1, WINO_ROPE_PARTS = 2 } wino_rope_scaling;
+WINO_API int wino_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double scale, int64_t trained_len,
+                                   double *freq, float *factor);
+
+/*
+ * For every row of every sequence: q_out = rotated q, and K and V of the row
+ * written to its slot of the cache, K rotated.  Rotation in fp32, rounded once
+ * to the element type.
+ *   q, q_out  [n_rows, n_q_heads, head_dim], q_out disjoint from q or the very
+ *             same array (in place); both NULL: only the cache is written
+ *   k, v      [n_rows, n_kv_heads, head_dim]; both NULL: only q is rotated
+ *   ws        workspace of which the first 256 bytes (status words) are used:
+ *             wino_attend's, or 256 bytes of its own, zero-filled before its
+ *             first use.  An error found on the device stays there until a
+ *             wino_attend with the same workspace has reported it.
+ * Two rows of a call that are stored in one slot race.
+ */
+WINO_API int wino_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
+                              const wino_kv_batch *b, const wino_rope *rope, void *ws, void *stream);
+
+/*
+ * Workspace of wino_attend for this batch: status words and room for the parts
+ * of rows whose slots are spread over several CTAs.  Depends on the heads, the
+ * head dim and (below 256 rows times heads) n_rows only, on no length.
+ */
+WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
+
+/*
+ * out[r, h] = sum_j p_j V_j over the slots j that row r sees, p = softmax of
+ * scale * <q[r, h], K_j>.  Products and sums in fp32 (the weights p rounded to
+ * the element type for the product with V), one rounding to the element type
+ * at the end.  Rows of no sequence are left as they are.
+ *   q, out  [n_rows, n_q_heads, head_dim]; out shares no element with q or the
+ *           cache
+ *   scale   finite, > 0 (commonly head_dim^-1/2)
+ *   ws      256-byte aligned, zero-filled before its first use; calls that may
+ *           overlap on the GPU need workspaces of their own
+ * The result does not depend on the order in which CTAs run.
+ */
+WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/*
  * Waits for `stream`, then reads the outcome of the last call that used `ws`
  * (published by its last kernel): WINO_OK, WINO_ERR_DEVICE_TIMEOUT (a bounded
- * wait expired), WINO_ERR_ARG (an active-sequence list entry out of range) or
+ * wait expired), WINO_ERR_ARG (an active-sequence list entry out of range, or
+ * what a batch's device arrays must not hold, see wino_kv_batch) or
  * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).
  */
 WINO_API int wino_read_device_status(const void *ws, void *stream, int *device_status);

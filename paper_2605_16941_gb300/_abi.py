@@ -35,7 +35,16 @@ WINO_OPT_W_PANELS = 8
 EXPORTS = ("wino_workspace_size", "wino_workspace_size_step", "wino_score_rows", "wino_draft_verify", "wino_step",
            "wino_step_static_scratch", "wino_read_device_status", "wino_profile_begin", "wino_profile_end",
            "wino_selftest_wait_timeout", "wino_status_string", "wino_version", "wino_decode", "wino_timeline_begin",
-           "wino_timeline_end", "wino_score_plan", "wino_score_plan_host", "wino_score_launch", "wino_lm_head_panels")
+           "wino_timeline_end", "wino_score_plan", "wino_score_plan_host", "wino_score_launch", "wino_lm_head_panels",
+           "wino_rope_frequencies", "wino_rope_append", "wino_attend_workspace_size", "wino_attend")
+
+# wino_kv_batch.dtype, wino_kv_batch.mask, scalings of wino_rope_frequencies
+WINO_BF16, WINO_FP16 = 0, 1
+WINO_MASK_FULL, WINO_MASK_CAUSAL, WINO_MASK_SHADOW = 0, 1, 2
+ROPE_SCALINGS = {"none": 0, "linear": 1, "parts": 2}
+
+# bytes of status words at the start of a workspace: all that wino_rope_append uses of one
+STATUS_BYTES = 256
 
 # 64-bit words per CTA in a score-kernel timeline (wino_timeline_begin)
 TIMELINE_WORDS = 8
@@ -61,6 +70,26 @@ class WinoParams(C.Structure):
 class WinoBlockStats(C.Structure):
     _fields_ = [("steps", C.c_int32), ("drafted", C.c_int32), ("remasked", C.c_int32), ("fallback", C.c_int32),
                 ("seq_steps", C.c_int32)]
+
+
+class WinoHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class WinoKvBatch(C.Structure):
+    """wino_kv_batch; ``make_kv_batch`` makes one and keeps its tensors alive."""
+    _fields_ = [("n_seq", C.c_int32), ("n_rows", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("mask", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("table_width", C.c_int32), ("q_start", C.c_void_p), ("q_len", C.c_void_p),
+                ("kv_len", C.c_void_p), ("new_slot", C.c_void_p), ("page_table", C.c_void_p),
+                ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("page_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class WinoRope(C.Structure):
+    """wino_rope; ``make_rope`` makes one and keeps its tensors alive."""
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float), ("freq", C.c_void_p),
+                ("positions", C.c_void_p)]
 
 
 # const uint16_t *(*)(void *user, int32_t step, int32_t blk_start)
@@ -89,6 +118,16 @@ def lib() -> C.CDLL:
         L.wino_draft_verify.argtypes = [vp, vp, vp, vp, C.POINTER(WinoParams), vp, vp, vp]
         L.wino_step.restype = C.c_int
         L.wino_step.argtypes = [vp, vp, i64, i64, vp, C.POINTER(WinoParams), vp, vp, vp, sz, vp]
+        heads, batch = C.POINTER(WinoHeads), C.POINTER(WinoKvBatch)
+        L.wino_rope_frequencies.restype = C.c_int
+        L.wino_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, i64, C.POINTER(C.c_double),
+                                            C.POINTER(C.c_float)]
+        L.wino_rope_append.restype = C.c_int
+        L.wino_rope_append.argtypes = [heads, heads, heads, heads, batch, C.POINTER(WinoRope), vp, vp]
+        L.wino_attend_workspace_size.restype = C.c_int
+        L.wino_attend_workspace_size.argtypes = [batch, C.POINTER(sz)]
+        L.wino_attend.restype = C.c_int
+        L.wino_attend.argtypes = [heads, heads, C.c_float, batch, vp, sz, vp]
         L.wino_lm_head_panels.restype = C.c_int
         L.wino_lm_head_panels.argtypes = [vp, i64, i64, vp, vp]
         L.wino_step_static_scratch.restype = C.c_int
@@ -301,6 +340,126 @@ def wino_decode(W, tokens, params: WinoParams, n_blocks: int, hidden, counts, co
     if failure:
         raise failure[0]
     return rc, [(b.steps, b.drafted, b.remasked, b.fallback, b.seq_steps) for b in stats], nxt.value
+
+
+def _device(t):
+    """Index of a tensor's CUDA device; the kernels run on the current one, so every tensor has to be there."""
+    return t.device.index if t.device.type == "cuda" else None
+
+
+def _require(ok: bool, where: str, status: int = WINO_ERR_ARG) -> None:
+    if not ok:
+        raise WinoError(status, where)
+
+
+def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot, *, n_rows: int, n_q_heads: int,
+                  mask: int) -> WinoKvBatch:
+    """wino_kv_batch over a paged cache.  ``k_cache`` and ``v_cache`` are [n_pages, page_size, n_kv_heads, head_dim]
+    views of one layout (a [pages, heads, slots, dim] cache is given as ``cache.transpose(1, 2)``), bfloat16, float16
+    or 16-bit integers that hold bfloat16; ``page_table`` [n_seq, width] and the four length and slot arrays [n_seq]
+    are contiguous int32 on the same device.  The batch keeps the tensors alive."""
+    import torch
+    where = "make_kv_batch"
+    ints = (page_table, q_start, q_len, kv_len, new_slot)
+    _require(k_cache.dim() == 4 and v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and
+             k_cache.element_size() == 2 and page_table.dim() == 2, where, WINO_ERR_SHAPE)
+    n_pages, page_size, n_kv_heads, head_dim = k_cache.shape
+    live = [i for i in range(4) if k_cache.shape[i] > 1]  # strides of single entries say nothing
+    _require(all(k_cache.stride(i) == v_cache.stride(i) for i in live) and k_cache.stride(3) == 1, where,
+             WINO_ERR_SHAPE)
+    _require(all(t.dtype == torch.int32 and t.is_contiguous() and t.device == k_cache.device for t in ints) and
+             v_cache.device == k_cache.device, where)
+    n_seq = page_table.size(0)
+    _require(all(t.numel() == n_seq for t in ints[1:]), where, WINO_ERR_SHAPE)
+    b = WinoKvBatch(n_seq, n_rows, n_q_heads, n_kv_heads, head_dim,
+                    WINO_FP16 if k_cache.dtype == torch.float16 else WINO_BF16, mask, page_size, n_pages,
+                    page_table.size(1), _ptr(q_start), _ptr(q_len), _ptr(kv_len), _ptr(new_slot), _ptr(page_table),
+                    _ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
+    b.tensors = (k_cache, v_cache, *ints)
+    return b
+
+
+def make_rope(freq, *, rot_dim: int, factor: float = 1.0, interleaved: bool = False, positions=None) -> WinoRope:
+    """wino_rope; ``freq`` is a device float64 [rot_dim / 2] tensor (None for rot_dim = 0), ``positions`` device int32
+    [n_rows] or None."""
+    import torch
+    _require(rot_dim == 0 or (freq.dtype == torch.float64 and freq.is_contiguous() and freq.numel() == rot_dim // 2),
+             "make_rope", WINO_ERR_SHAPE)
+    _require(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous()), "make_rope")
+    r = WinoRope(rot_dim, int(interleaved), factor, _ptr(freq) if rot_dim else None, _ptr(positions))
+    r.tensors = (freq, positions)
+    return r
+
+
+def wino_rope_frequencies(rot_dim: int, base: float, *, scaling: str = "none", factor: float = 1.0,
+                          trained_len: int = 1):
+    """(frequencies as a host float64 [rot_dim / 2] tensor, factor on the rotated values) for ``make_rope``."""
+    import torch
+    freq = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64)
+    out = C.c_float(0)
+    _check(lib().wino_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, trained_len,
+                                       C.cast(freq.data_ptr() or C.addressof(out), C.POINTER(C.c_double)),
+                                       C.byref(out)), "wino_rope_frequencies")
+    return freq, out.value
+
+
+def _heads(t, b: WinoKvBatch, heads: int, where: str) -> WinoHeads:
+    """A [n_rows, heads, head_dim] tensor as wino_heads."""
+    rows, h, dim = t.shape
+    _require(rows == b.n_rows and h == heads and dim == b.head_dim, where, WINO_ERR_SHAPE)
+    cache = b.tensors[0]
+    _require(t.dtype == cache.dtype and t.device == cache.device and (dim == 1 or t.stride(2) == 1), where)
+    return WinoHeads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _on_current_device(b: WinoKvBatch, where: str) -> None:
+    import torch
+    _require(_device(b.tensors[0]) == torch.cuda.current_device(), where)
+
+
+def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=None, stream=None) -> None:
+    """Rotate the rows' queries (into ``q_out``, or in place) and write their rotated keys and their values into the
+    batch's cache.  ``q`` None: the cache alone; ``k`` and ``v`` None: the queries alone."""
+    where = "wino_rope_append"
+    qh = qo = kh = vh = None
+    if q is not None:
+        qh = _heads(q, batch, batch.n_q_heads, where)
+        qo = qh if q_out is None else _heads(q_out, batch, batch.n_q_heads, where)
+    if k is not None:
+        kh = _heads(k, batch, batch.n_kv_heads, where)
+    if v is not None:
+        vh = _heads(v, batch, batch.n_kv_heads, where)
+    if rope.positions:
+        _require(rope.tensors[1].numel() == batch.n_rows, where, WINO_ERR_SHAPE)
+    _on_current_device(batch, where)
+    _check(lib().wino_rope_append(qh, qo, kh, vh, batch, rope, _ptr(ws), _stream(stream)), where)
+
+
+def wino_attend_workspace_size(batch: WinoKvBatch) -> int:
+    out = C.c_size_t(0)
+    _check(lib().wino_attend_workspace_size(batch, C.byref(out)), "wino_attend_workspace_size")
+    return out.value
+
+
+def attend_workspace(batch: WinoKvBatch):
+    """A zeroed uint8 device tensor of wino_attend_workspace_size bytes, beside the batch's cache."""
+    import torch
+    return torch.zeros(wino_attend_workspace_size(batch), dtype=torch.uint8, device=batch.tensors[0].device)
+
+
+def append_workspace(device=None):
+    """A zeroed uint8 device tensor of the status words, for wino_rope_append without a wino_attend behind it."""
+    import torch
+    return torch.zeros(STATUS_BYTES, dtype=torch.uint8, device=device or "cuda")
+
+
+def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
+    """Attention of the batch's rows over its cache, into ``out``; ``scale`` defaults to head_dim^-1/2."""
+    where = "wino_attend"
+    qh, oh = _heads(q, batch, batch.n_q_heads, where), _heads(out, batch, batch.n_q_heads, where)
+    _on_current_device(batch, where)
+    _check(lib().wino_attend(qh, oh, batch.head_dim ** -0.5 if scale is None else scale, batch, _ptr(ws), _nbytes(ws),
+                             _stream(stream)), where)
 
 
 def wino_read_device_status(ws, stream=None) -> int:

@@ -23,8 +23,6 @@ constexpr int64_t kMaxV = int64_t(1) << 27;
 constexpr int64_t kMaxPanelRows = int64_t(1) << 30;  // (d/64) * V of a panel copy: its row coordinates stay in int32
 constexpr size_t kAlign = 256;
 
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 // Workspace layout: [status words | tickets[ceil(N/2)] | partial records [N][R] | argmax[N] | pmax[N] |
 // ptarget[N] || entropy partials [N][R]], R = records_per_row(V) bounds the records per row.  `total` ends
 // before the entropy partials, which only wino_score_rows with an entropy output needs (`total_entropy`).
@@ -54,14 +52,9 @@ bool shape_ok(int64_t N, int64_t d, int64_t V)
     return N >= 1 && N <= kMaxN && d >= 8 && d <= kMaxD && d % 8 == 0 && V >= 2 && V <= kMaxV;
 }
 
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+}  // namespace
 
 // ---------------------------------------------------------------- device facts
-
-struct DeviceInfo {
-    int sm_count = 0;
-    bool supported = false;
-};
 
 int device_info(DeviceInfo *out)
 {
@@ -102,6 +95,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
     });
     return fn;
 }
+
+namespace {
 
 // A bf16 row-major [rows, cols] matrix read in boxes of box_rows x 64 with
 // 128-byte swizzling; out-of-range rows/columns read as zero.
@@ -576,7 +571,8 @@ int wino_read_device_status(const void *ws, void *stream, int *device_status)
     StatusWords w{};
     if (cudaMemcpy(&w, ws, sizeof w, cudaMemcpyDeviceToHost) != cudaSuccess)
         return WINO_ERR_CUDA;
-    *device_status = w.last;
+    // `current` outlives a call only where no later kernel of it publishes: wino_rope_append's errors
+    *device_status = w.current ? w.current : w.last;
     return WINO_OK;
 }
 

@@ -1,0 +1,247 @@
+"""wino_attend against the definition in 64 bits (kv_helpers): masks, lengths around tiles and pages, head layouts, types,
+strides, rows that see nothing, poisoned slots, and what a batch's device arrays may hold."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2605_16941_gb300 as wino  # noqa: E402
+from kv_helpers import CAUSAL, FULL, SHADOW, add_rows, attend, check, make_kv  # noqa: E402
+
+BF, FP = torch.bfloat16, torch.float16
+
+
+def run(c, **kw):
+    ws = attend(c, **kw)
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    return check(c)
+
+
+CASES = {
+    # name: (mask, [(rows, kv_len, new_slot)], other arguments of make_kv)
+    "one_slot": (CAUSAL, [(1, 1, 0)], {}),
+    "one_token": (CAUSAL, [(1, 300, 299)], dict(heads=8, kv_heads=2, dim=128)),
+    "no_slots": (FULL, [(3, 0, 0), (2, 5, 0)], {}),
+    "empty_and_absent": (FULL, [(0, 40, 0), (2, 0, 0), (0, 0, 0), (4, 33, 0)], dict(gap=3)),
+    "causal_first_rows": (CAUSAL, [(5, 5, 0), (7, 3, 0)], {}),  # rows past kv_len see kv_len slots
+    "left_padding": (CAUSAL, [(9, 5, -4), (3, 0, -3)], {}),  # rows before slot 0 see nothing
+    "tile_edges": (CAUSAL, [(1, n, n - 1) for n in (127, 128, 129, 255, 256, 257, 385)], dict(gap=1)),
+    "pages_of_16": (FULL, [(3, n, 0) for n in (15, 16, 17, 47, 145)], {}),
+    "pages_of_32": (FULL, [(3, n, 0) for n in (31, 33, 161)], dict(page=32, layout="heads")),
+    "pages_of_64": (FULL, [(3, n, 0) for n in (63, 65, 200)], dict(page=64)),
+    "pages_of_128": (FULL, [(3, n, 0) for n in (128, 129, 300)], dict(page=128, layout="heads")),
+    "pages_of_384": (FULL, [(3, n, 0) for n in (384, 385, 500)], dict(page=384)),
+    "shadow_1": (SHADOW, [(2, 1, 0), (2, 9, 8), (2, 9, 0)], {}),
+    "shadow_32": (SHADOW, [(64, 96, 64), (64, 64, 0), (64, 200, 100)], dict(heads=4, kv_heads=4, dim=128)),
+    "shadow_tile_edge": (SHADOW, [(6, 126, 123), (6, 128, 125), (8, 127, 120)], dict(heads=4, kv_heads=2)),
+    "shadow_right_context": (SHADOW, [(20, 300, 40)], dict(dim=128, layout="heads")),
+    "shadow_large": (SHADOW, [(300, 700, 500)], dict(heads=2, kv_heads=1, dim=64, page=64)),
+    "full_130_rows": (FULL, [(130, 257, 0)], dict(heads=1)),
+    "causal_prompt": (CAUSAL, [(300, 300, 0)], dict(heads=3, kv_heads=3, dim=128)),
+    "causal_ragged": (CAUSAL, [(70, 170, 100), (1, 400, 399), (129, 129, 0), (2, 2, 0)], dict(gap=2, order=[2, 0, 3, 1])),
+    "group_7": (CAUSAL, [(40, 140, 100), (1, 60, 59)], dict(heads=14, kv_heads=2)),
+    "group_5_dim_80": (SHADOW, [(20, 50, 30)], dict(heads=10, kv_heads=2, dim=80)),
+    "group_128": (CAUSAL, [(3, 200, 197)], dict(heads=128, kv_heads=1)),
+    "group_100": (CAUSAL, [(3, 200, 197)], dict(heads=100, kv_heads=1)),
+    "dim_8": (FULL, [(5, 140, 0)], dict(dim=8)),
+    "dim_72": (FULL, [(5, 140, 0)], dict(dim=72, layout="heads")),
+    "dim_96": (CAUSAL, [(50, 140, 90)], dict(dim=96, heads=6, kv_heads=2)),
+    "dim_120": (CAUSAL, [(5, 140, 135)], dict(dim=120)),
+    "many_short": (CAUSAL, [(1 + i % 3, 1 + (7 * i) % 90, (7 * i) % 90 - i % 3) for i in range(500)], {}),
+    "long": (CAUSAL, [(1, 5000, 4999), (2, 9000, 8998)], dict(heads=8, kv_heads=2, dim=128, page=64)),
+    "long_rows": (CAUSAL, [(140, 3000, 2860)], dict(heads=4, kv_heads=2, dim=128, page=32)),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("name", CASES)
+def test_against_definition(name, dtype):
+    mask, seqs, kw = CASES[name]
+    run(add_rows(make_kv(mask, seqs, dtype=dtype, **kw)))
+
+
+@pytest.mark.parametrize("layout", ["slots", "heads"])
+def test_strided_rows(layout):
+    run(add_rows(make_kv(CAUSAL, [(33, 150, 117), (1, 20, 19)], heads=6, kv_heads=2, layout=layout, gap=1),
+                 strided=True))
+
+
+def test_combined_cache():
+    """K and V in one allocation, [pages, 2, slots, heads, dim]: views with one set of strides."""
+    c = make_kv(SHADOW, [(32, 90, 60)], heads=4, kv_heads=2)
+    both = torch.stack([c.k_cache, c.v_cache], dim=1).contiguous()
+    c.k_cache, c.v_cache = both[:, 0], both[:, 1]
+    c.batch = wino.make_kv_batch(c.k_cache, c.v_cache, c.table_dev, *c.ints, n_rows=c.n_rows, n_q_heads=4, mask=SHADOW)
+    run(add_rows(c))
+
+
+@pytest.mark.parametrize("spread", [8.0, 30.0])
+def test_peaked_softmax(spread):
+    """Scores that move the running maximum by far from tile to tile, and rows whose weights all but one vanish."""
+    run(add_rows(make_kv(CAUSAL, [(40, 700, 660)], heads=4, kv_heads=2, dim=128, spread=spread), spread=2.0))
+
+
+def test_rising_maximum():
+    """Keys that grow with the slot: every tile raises the maximum."""
+    c = make_kv(FULL, [(130, 640, 0)], heads=1, dim=64, dtype=FP, poison=False)
+    for j in range(640):
+        c.k_cache[c.table[0, j // 16], j % 16] = 0.02 * j
+    add_rows(c)
+    c.q.fill_(0.5)
+    run(c)
+
+
+def test_constant_values_come_back():
+    """With every V the same, out is that value whatever the weights: off by the weights' rounding at most."""
+    c = make_kv(CAUSAL, [(64, 400, 336)], heads=2, dim=128, poison=False)
+    c.v_cache.fill_(1.5)
+    add_rows(c)
+    run(c)
+
+
+def test_scale():
+    c = add_rows(make_kv(CAUSAL, [(4, 50, 46)]))
+    ws = attend(c, scale=0.37)
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    check(c, scale=0.37)
+
+
+def test_workspace_is_reused_as_it_is():
+    """One workspace through calls of other shapes, and twice the same call: bit for bit the same."""
+    big = add_rows(make_kv(CAUSAL, [(200, 1000, 800), (1, 3000, 2999)], heads=8, kv_heads=2, dim=128))
+    ws = wino.attend_workspace(big.batch)
+    run(big, ws=ws)
+    first = big.out.clone()
+    for mask, seqs in ((SHADOW, [(64, 500, 400)]), (FULL, [(1, 0, 0)])):
+        run(add_rows(make_kv(mask, seqs, heads=4, kv_heads=2)), ws=ws)
+    big.out.fill_(77.0)
+    run(big, ws=ws)
+    assert torch.equal(first, big.out)
+
+
+def test_captured_call_takes_new_lengths():
+    """The lengths, slots and pages are read when the call runs."""
+    seqs = [(4, 900, 896), (1, 300, 299)]
+    c = add_rows(make_kv(CAUSAL, seqs, heads=8, kv_heads=2, dim=128, poison=False))
+    ws = wino.attend_workspace(c.batch)
+    run(c, ws=ws)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        attend(c, ws=ws)
+    for lens in ([(4, 500, 496), (1, 301, 300)], [(3, 17, 14), (1, 0, 0)], seqs):
+        c.seqs = lens
+        c.ints[1:].copy_(torch.tensor([[s[i] for s in lens] for i in range(3)], dtype=torch.int32))
+        c.extra["whole"].fill_(77.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert wino.wino_read_device_status(ws) == wino.WINO_OK
+        check(c)
+
+
+def test_two_streams_with_their_own_workspaces():
+    cs = [add_rows(make_kv(CAUSAL, [(100, 2000, 1900)], heads=8, kv_heads=2, dim=128, seed=i), seed=i) for i in range(2)]
+    wss = [wino.attend_workspace(c.batch) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, ws, s in zip(cs, wss, streams):
+            wino.wino_attend(c.q, c.out, c.batch, ws, stream=s)
+    torch.cuda.synchronize()
+    for c, ws in zip(cs, wss):
+        assert wino.wino_read_device_status(ws) == wino.WINO_OK
+        check(c)
+
+
+def test_shared_prefix_pages():
+    """Two sequences read the same pages."""
+    c = make_kv(CAUSAL, [(2, 100, 98), (2, 100, 98)], poison=False)
+    c.table[1, :5] = c.table[0, :5]
+    c.table_dev.copy_(torch.from_numpy(c.table))
+    run(add_rows(c))
+
+
+@pytest.mark.parametrize("what", ["page", "negative_page", "rows", "start", "length", "kv", "odd_shadow", "shadow_table"])
+def test_bad_device_values_end_in_an_error(what):
+    """Values that only the device can check: an error status, the other sequences as they should be, nothing outside
+    the rows written, and the next call clean."""
+    mask = SHADOW if "shadow" in what else CAUSAL
+    c = add_rows(make_kv(mask, [(4, 60, 50), (4, 70, 60), (2, 40, 30)], gap=1, heads=4, kv_heads=2))
+    ws = wino.attend_workspace(c.batch)
+    keep, table = c.ints.clone(), c.table_dev.clone()
+    if what == "page":
+        c.table_dev[1, 2] = c.k_cache.size(0)
+    elif what == "negative_page":
+        c.table_dev[1, 2] = -1
+    elif what == "rows":
+        c.ints[1, 1] = c.n_rows + 1
+    elif what == "start":
+        c.ints[0, 1] = -3
+    elif what == "length":
+        c.ints[1, 1] = -1
+    elif what == "kv":
+        c.ints[2, 1] = c.table.shape[1] * c.page + 1
+    elif what == "odd_shadow":
+        c.ints[1, 1] = 3
+    else:
+        c.ints[2, 1] = c.table.shape[1] * c.page - 1
+    wino.wino_attend(c.q, c.out, c.batch, ws)
+    assert wino.wino_read_device_status(ws) == wino.WINO_ERR_ARG
+    saved = c.seqs
+    start = c.starts[1]
+    c.extra["whole"][start:start + 4] = 77.0  # undefined rows
+    c.seqs = [saved[0], (0, 0, 0), saved[2]]
+    check(c)
+    c.seqs = saved
+    c.ints.copy_(keep)
+    c.table_dev.copy_(table)
+    run(c, ws=ws)
+
+
+def test_far_offsets():
+    """A cache of more than 2^31 elements: pages at both ends."""
+    kv, dim, page = 8, 128, 64
+    n_pages = (1 << 31) // (kv * dim * page) + 70
+    k = torch.empty((n_pages, page, kv, dim), dtype=BF, device="cuda")
+    v = torch.empty_like(k)
+    pages = [n_pages - 1, 0, n_pages - 2, 1]
+    c = make_kv(CAUSAL, [(3, 250, 247)], heads=16, kv_heads=kv, dim=dim, page=page, poison=False)
+    for i, p in enumerate(pages):
+        k[p].copy_(c.k_cache[c.table[0, i]])
+        v[p].copy_(c.v_cache[c.table[0, i]])
+    small = c.table.copy()
+    far = small.copy()
+    far[0, :4] = pages
+    table = torch.from_numpy(far).cuda()
+    add_rows(c)
+    b = wino.make_kv_batch(k, v, table, *c.ints, n_rows=c.n_rows, n_q_heads=16, mask=CAUSAL)
+    ws = wino.attend_workspace(b)
+    wino.wino_attend(c.q, c.out, b, ws)
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    check(c)
+
+
+def test_large_batch_matches_the_plain_form():
+    """A larger ragged batch against the same sums in fp32 on the device (both roundings counted)."""
+    rng = np.random.default_rng(3)
+    seqs = [(int(n), int(n + c), int(c)) for n, c in zip(rng.integers(1, 700, 6), rng.integers(0, 5000, 6))]
+    c = add_rows(make_kv(CAUSAL, seqs, heads=8, kv_heads=2, dim=128, page=64))
+    ws = attend(c)
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    for s, (n, kv, new) in enumerate(seqs):
+        j = torch.arange(kv, device="cuda")
+        page = c.table_dev[s].long()[j // 64]
+        K, V = (t[page, j % 64].double().repeat_interleave(4, 1) for t in (c.k_cache, c.v_cache))
+        q = c.q[c.starts[s]:c.starts[s] + n].double()
+        x = torch.einsum("rhc,jhc->hrj", q, K) * 128 ** -0.5
+        x.masked_fill_(j[None, None] > new + torch.arange(n, device="cuda")[None, :, None], -torch.inf)
+        p = torch.softmax(x, -1)
+        want, size = torch.einsum("hrj,jhc->rhc", p, V), torch.einsum("hrj,jhc->rhc", p, V.abs())
+        got = c.out[c.starts[s]:c.starts[s] + n].double()
+        # score error (130 u S, S below 64 here: |q||k| scale) twice, 2^-21, n u; weights and result rounded
+        tol = (2 * 130 * 2.0 ** -24 * 64 + 2.0 ** -21 + kv * 2.0 ** -24) * 2 * size + 1.01 * 2.0 ** -8 * (size + want.abs())
+        assert ((got - want).abs() <= tol).all(), s
