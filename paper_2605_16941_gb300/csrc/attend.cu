@@ -1,130 +1,1012 @@
 // attend.cu -- wino_attend: attention of a step's rows over a paged cache.
 //
-// One warp per (row, query head): 32 slots at a time, a slot per lane for the scores, then the dims spread over the
-// lanes for the sum over V, with the running maximum and sum of the softmax in fp32.
+// out = softmax(scale Q K^T) V with the running maximum m, sum l and unnormalised product O of an online softmax: per tile
+// of 128 slots S = Q K^T, m' = max(m, max S), P = exp(S - m'), l' = l exp(m - m') + sum P, O' = O exp(m - m') + P V.
+//
+// Rows.  The G query heads of a kv head share its K and V, so a tile of M = 128 rows is floor(128 / G) row positions times
+// G heads.  A task is one sequence, one kv head and two such tiles: both tiles multiply every K and V tile that is
+// staged.  Where a task has rows in its first tile only (single tokens, short blocks), its two softmax warpgroups take
+// even and odd slot tiles instead, each with its own m, l and O, joined at the end.
+//
+// Work.  A task costs one unit per slot tile.  The units of all tasks in order are cut into equal runs, one per CTA, from
+// lengths that are read on the device; a run that starts or ends inside a task leaves its (m, l, O) in the workspace, and
+// combine_kernel joins the runs of such tasks in the order of the slots.
+//
+// A CTA has 12 warps: two softmax warpgroups (one thread per row), and one warp each for the copies (TMA, one box per
+// page and 64 dims), the MMAs, and the zeros behind the last slot.  S lies in tensor memory, 128 columns per warpgroup;
+// P overwrites it as 16-bit pairs, from where it is the A operand of P V; O lies beside it, DP columns per warpgroup.
+// K and V tiles go through one ring of shared-memory slots in the order in which the MMAs need them.
+//
+// Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
+// 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  m follows
+// the row's maximum only when that has grown by more than 2^8, so that O is rarely rescaled: P is then at most 2^8, and the
+// quotient O / l does not depend on m.
+#include <algorithm>
+#include <cstring>
+#include <mutex>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "kv_batch.cuh"
 #include "ptx.cuh"
+#include "wait.cuh"
 
 namespace wino {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kTileM = 128, kTileN = 128;  // rows and slots of a tile
+constexpr int kSoftmaxThreads = 256;
+constexpr int kAttendThreads = kSoftmaxThreads + 128;
+constexpr int kWarpTma = 8, kWarpMma = 9, kWarpTail = 10;
+constexpr int kMaxCtas = 160;          // an SM each
+constexpr int kRecordBytes = 32;       // SplitRecord
+constexpr int kCombineRows = 32;       // rows per combine CTA
+constexpr int kSplitRows = 2 * kTileM;  // rows of a task
+constexpr float kRescaleLog2 = 8.f;
+constexpr uint32_t kTmemS = 0, kTmemO = 2 * kTileN, kTmemAll = 512;
+constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
+
+// What combine_kernel needs to know of the run that CTA c starts inside a task with (one per CTA).
+struct SplitRecord {
+    int32_t valid;  // the run starts inside a task
+    int32_t seq, kv_head, pair;
+    int32_t first, last;  // CTAs whose runs hold units of that task
+    int32_t pad[2];
+};
+static_assert(sizeof(SplitRecord) == kRecordBytes, "record size");
 
 struct AttendArgs {
     wino_heads q, out;
     wino_kv_batch b;
     float scale_log2;  // scale * log2(e)
     StatusWords *status;
+    SplitRecord *records;  // [kMaxCtas]
+    float2 *part_ml;       // [kMaxCtas][2][split_rows]: m (log2 units), l
+    float4 *part_o;        // [kMaxCtas][2][DP / 4][split_rows]
+    int32_t split_rows;
+    int32_t group, positions;  // query heads per kv head, row positions per tile
+    int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
+    int32_t min_units;         // a CTA's run is at least this long
 };
 
-__device__ __forceinline__ float to_f(uint16_t x, int dtype)
+// Row positions and slots of a task's tiles.
+struct Task {
+    int32_t kv_end;  // slots that some row sees
+    int32_t tiles;   // slot tiles, at least 1
+    bool two;        // rows in both tiles
+};
+
+__device__ __forceinline__ Task task_of(const AttendArgs &a, const SeqRows &q, int32_t pair)
 {
-    return dtype == WINO_BF16 ? __uint_as_float((uint32_t)x << 16) : __half2float(__ushort_as_half(x));
+    const int32_t w = 2 * a.positions;
+    const int32_t last = min(q.n, (pair + 1) * w) - 1;
+    Task t;
+    t.kv_end = row_sees(a.b, q, last).lim;  // no earlier row sees more
+    t.tiles = max(1, (t.kv_end + kTileN - 1) / kTileN);
+    t.two = q.n - pair * w > a.positions;
+    return t;
 }
 
-__device__ __forceinline__ uint16_t from_f(float x, int dtype)
+__device__ __forceinline__ int32_t pairs_of(const AttendArgs &a, const SeqRows &q)
 {
-    return dtype == WINO_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+    return (q.n + 2 * a.positions - 1) / (2 * a.positions);
 }
 
-__global__ void __launch_bounds__(kWarps * 32) attend_kernel(const AttendArgs a)
-{
-    __shared__ int32_t seq;
-    __shared__ float qs[kWarps][128];
-    const wino_kv_batch &b = a.b;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int32_t row = blockIdx.x;
-    ptx::grid_dep_launch_dependents();
-    ptx::grid_dep_wait();
-    if (threadIdx.x == 0)
-        seq = -1;
-    __syncthreads();
-    bool ok = true;
-    for (int32_t s = threadIdx.x; s < b.n_seq; s += kWarps * 32) {
-        const SeqRows q = load_seq(b, s);
-        ok = ok && q.ok;
-        if (q.n > 0 && row >= q.start && row < q.start + q.n)
-            seq = s;
+// Run c of n over t units.
+__device__ __forceinline__ int64_t run_start(int64_t c, int64_t n, int64_t t) { return c * t / n; }
+__device__ __forceinline__ int32_t run_of(int64_t unit, int64_t n, int64_t t) { return (int32_t)(((unit + 1) * n - 1) / t); }
+
+// Where a CTA's run starts, found once per CTA.
+struct RunStart {
+    int64_t units;  // of the run
+    int32_t seq, kv_head, pair, tile;
+};
+
+// A CTA's run as a sequence of tasks or parts of tasks; every role walks it for itself.
+struct Walk {
+    int64_t left;
+    int32_t seq, kv_head, pair, tile;
+    SeqRows q;
+    int32_t n_pairs;
+    // the current part: slot tiles [j0, j1) of task t
+    Task t;
+    int32_t j0, j1;
+
+    __device__ __forceinline__ void start(const AttendArgs &a, const RunStart &r)
+    {
+        left = r.units;
+        seq = r.seq;
+        kv_head = r.kv_head;
+        pair = r.pair;
+        tile = r.tile;
+        if (left > 0) {
+            q = load_seq(a.b, seq);
+            n_pairs = pairs_of(a, q);
+        }
     }
+    __device__ __forceinline__ bool next(const AttendArgs &a)
+    {
+        if (left <= 0)
+            return false;
+        if (pair == n_pairs) {
+            pair = 0;
+            if (++kv_head == a.b.n_kv_heads) {
+                kv_head = 0;
+                do {  // ends: there are units left
+                    if (++seq >= a.b.n_seq)
+                        return false;
+                    q = load_seq(a.b, seq);
+                } while (q.n == 0);
+                n_pairs = pairs_of(a, q);
+            }
+        }
+        t = task_of(a, q, pair);
+        j0 = tile;
+        j1 = (int32_t)min((int64_t)t.tiles, tile + left);
+        left -= j1 - j0;
+        tile = 0;
+        ++pair;
+        return true;
+    }
+    __device__ __forceinline__ int32_t task_pair() const { return pair - 1; }
+    __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == t.tiles; }
+    __device__ __forceinline__ int32_t loads() const { return t.kv_end > 0 ? j1 - j0 : 0; }
+    // The run's last tile ends behind the last slot that a row sees.
+    __device__ __forceinline__ bool tail() const { return j1 == t.tiles && (t.kv_end & (kTileN - 1)) != 0; }
+};
+
+template <int DP>
+struct Config {
+    static constexpr uint32_t kTileBytes = (DP / 64) * kHalfBytes;  // 128 rows or slots
+    static constexpr int kSlots = DP == 128 ? 5 : 12;               // ring slots beside the two Q tiles
+    static constexpr uint32_t kRing = kSlots * kTileBytes;
+    static constexpr uint32_t kSmem = 2 * kTileBytes + kRing + 2560;
+};
+
+struct alignas(8) Shared {
+    uint64_t q_full, q_empty;
+    uint64_t full[12], empty[12];
+    uint64_t s_full[2], p_ready[2], o_done[2];
+    uint64_t tail, zeroed;  // V of a part's last tile has landed; the slots behind the last one hold zeros
+    uint64_t ml_ready, ml_done;
+    uint64_t mma_done;
+    uint32_t tmem;
+    int32_t abort;
+    RunStart run;
+    int64_t units[kAttendThreads / 32];
+    float2 ml[2][kTileM];
+};
+static_assert(sizeof(Shared) <= 2560, "shared block must fit its reserve");
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    if (kBf16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Units of sequence s in the lanes of a group of `width` threads (each returns the sum).
+__device__ __forceinline__ int64_t seq_units(const AttendArgs &a, const SeqRows &q, int lane, int width)
+{
+    int64_t u = 0;
+    const int32_t n_pairs = q.n > 0 ? pairs_of(a, q) : 0;
+    for (int32_t p = lane; p < n_pairs; p += width)
+        u += task_of(a, q, p).tiles;
+    for (int i = width >> 1; i; i >>= 1)
+        u += __shfl_xor_sync(0xffffffffu, u, i);
+    return u * a.b.n_kv_heads;
+}
+
+// Finds this CTA's run (all threads; the result is in sh.run for every thread after the closing barrier).
+__device__ __forceinline__ void find_run(const AttendArgs &a, Shared &sh, bool &ok)
+{
+    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int32_t n_seq = a.b.n_seq;
+    int width = 32;  // threads per sequence
+    while (width > 1 && n_seq * width > kAttendThreads)
+        width >>= 1;
+    const int per = kAttendThreads / width;  // sequences per round
+    const int sub = lane & (width - 1);
+    auto units_of = [&](int32_t s, SeqRows &q) {
+        q.n = 0;
+        q.ok = true;
+        if (s < n_seq)
+            q = load_seq(a.b, s);
+        return seq_units(a, q, sub, width);
+    };
+    SeqRows q;
+    int64_t total = 0, mine = 0;
+    for (int32_t s0 = 0; s0 < n_seq; s0 += per) {
+        mine = units_of(s0 + tid / width, q);
+        ok = ok && q.ok;
+        int64_t w = sub == 0 ? mine : 0;
+        for (int i = 16; i; i >>= 1)
+            w += __shfl_xor_sync(0xffffffffu, w, i);
+        total += w;
+    }
+    if (lane == 0)
+        sh.units[warp] = total;
+    if (tid == 0)
+        sh.run.units = 0;
     __syncthreads();
-    if (seq >= 0) {
-        const SeqRows q = load_seq(b, seq);
-        const RowSees sees = row_sees(b, q, row - q.start);
-        for (int h = blockIdx.y * kWarps + warp; h < min(b.n_q_heads, (int)(blockIdx.y + 1) * kWarps); h += kWarps) {
-            const int hk = h / (b.n_q_heads / b.n_kv_heads);
-            for (int c = lane; c < b.head_dim; c += 32)
-                qs[warp][c] = to_f(a.q.data[row * a.q.row_stride + h * a.q.head_stride + c], b.dtype);
-            __syncwarp();
-            float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int32_t j0 = 0; j0 < sees.lim; j0 += 32) {
-                const int32_t j = j0 + lane;
-                int64_t at = -1;
-                float x = -INFINITY;
-                if (j < sees.lim && j != sees.hole) {
-                    const int32_t page = load_page(b, seq, j / b.page_size, ok);
-                    if (page >= 0) {
-                        at = page * b.page_stride + (j % b.page_size) * b.slot_stride + hk * b.head_stride;
-                        float d = 0.f;
-                        for (int c = 0; c < b.head_dim; ++c)
-                            d = fmaf(qs[warp][c], to_f(b.k_cache[at + c], b.dtype), d);
-                        x = d * a.scale_log2;
+    total = 0;
+    for (int i = 0; i < kAttendThreads / 32; ++i)
+        total += sh.units[i];
+    const int64_t n = min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
+    const int64_t c = blockIdx.x;
+    const int64_t start = run_start(c, n, total), units = c < n ? run_start(c + 1, n, total) - start : 0;
+    // the sequence that holds the run's first unit
+    int64_t before = 0;  // units of earlier rounds
+    for (int32_t s0 = 0; s0 < n_seq && units > 0; s0 += per) {
+        if (n_seq > per)
+            mine = units_of(s0 + tid / width, q);
+        __syncthreads();
+        int64_t pre = sub == 0 ? mine : 0;  // inclusive over the lanes, then over the warps
+        for (int i = 1; i < 32; i <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
+            if (lane >= i)
+                pre += up;
+        }
+        if (lane == 31)
+            sh.units[warp] = pre;
+        __syncthreads();
+        int64_t round = 0, base = before;
+        for (int i = 0; i < kAttendThreads / 32; ++i) {
+            if (i < warp)
+                base += sh.units[i];
+            round += sh.units[i];
+        }
+        const int64_t s_end = base + pre, s_start = s_end - mine;
+        if (sub == 0 && start >= s_start && start < s_end) {
+            const int64_t per_head = mine / a.b.n_kv_heads;
+            RunStart r;
+            r.units = units;
+            r.seq = s0 + tid / width;
+            r.kv_head = (int32_t)((start - s_start) / per_head);
+            int64_t in_head = (start - s_start) % per_head;
+            r.pair = 0;
+            int32_t tiles = task_of(a, q, 0).tiles;
+            while (in_head >= tiles) {
+                in_head -= tiles;
+                tiles = task_of(a, q, ++r.pair).tiles;
+            }
+            r.tile = (int32_t)in_head;
+            sh.run = r;
+            SplitRecord rec{};
+            rec.valid = r.tile > 0;
+            rec.seq = r.seq;
+            rec.kv_head = r.kv_head;
+            rec.pair = r.pair;
+            rec.first = run_of(start - in_head, n, total);
+            rec.last = run_of(start - in_head + tiles - 1, n, total);
+            a.records[c] = rec;
+        }
+        before += round;
+    }
+    if (units == 0 && tid == 0)
+        a.records[c].valid = 0;
+    __syncthreads();
+}
+
+template <int DP, bool kBf16>
+__global__ void __launch_bounds__(kAttendThreads, 1)
+    attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                  const __grid_constant__ CUtensorMap tmV, const AttendArgs a)
+{
+    using C = Config<DP>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];  // swizzle atoms
+    const uint32_t raw = ptx::smem_u32(smem_raw);
+    const uint32_t sq = raw, ring = raw + 2 * C::kTileBytes;
+    Shared &sh = *reinterpret_cast<Shared *>(smem_raw + 2 * C::kTileBytes + C::kRing);
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    auto full = [&](int s) { return ptx::smem_u32(&sh.full[s]); };
+    auto empty = [&](int s) { return ptx::smem_u32(&sh.empty[s]); };
+    auto s_full = [&](int w) { return ptx::smem_u32(&sh.s_full[w]); };
+    auto p_ready = [&](int w) { return ptx::smem_u32(&sh.p_ready[w]); };
+    auto o_done = [&](int w) { return ptx::smem_u32(&sh.o_done[w]); };
+    const uint32_t q_full = ptx::smem_u32(&sh.q_full), q_empty = ptx::smem_u32(&sh.q_empty);
+    const uint32_t tail = ptx::smem_u32(&sh.tail), zeroed = ptx::smem_u32(&sh.zeroed), mma_done = ptx::smem_u32(&sh.mma_done);
+    auto slot_addr = [&](int s) { return ring + (uint32_t)s * C::kTileBytes; };
+
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(q_full, 1);
+        ptx::mbar_init(q_empty, 1);
+        for (int s = 0; s < C::kSlots; ++s) {
+            ptx::mbar_init(full(s), 1);
+            ptx::mbar_init(empty(s), 1);
+        }
+        for (int w = 0; w < 2; ++w) {
+            ptx::mbar_init(s_full(w), 1);
+            ptx::mbar_init(p_ready(w), 4);
+            ptx::mbar_init(o_done(w), 1);
+        }
+        ptx::mbar_init(tail, 1);
+        ptx::mbar_init(zeroed, 1);
+        ptx::mbar_init(ptx::smem_u32(&sh.ml_ready), 8);
+        ptx::mbar_init(ptx::smem_u32(&sh.ml_done), 8);
+        ptx::mbar_init(mma_done, 1);
+        sh.abort = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == kWarpTma && lane == 0) {
+        ptx::prefetch_tensormap(&tmQ);
+        ptx::prefetch_tensormap(&tmK);
+        ptx::prefetch_tensormap(&tmV);
+    }
+    if (warp == kWarpMma) {
+        ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), kTmemAll);
+        ptx::tmem_relinquish();
+    }
+    ptx::grid_dep_launch_dependents();
+    ptx::grid_dep_wait();  // lengths, pages, q and the cache may come from the kernel before
+    bool ok = true;
+    ptx::tc_fence_before();
+    find_run(a, sh, ok);
+    ptx::tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    Walk w;
+    w.start(a, sh.run);
+    if (warp < 8) {
+                // ------------------------------------------------------------ softmax: one thread per row
+        const int g = warp >> 2;                  // warpgroup
+        const int r = (warp & 3) * 32 + lane;     // row of the tile, its TMEM lane
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t t_s = lanes + kTmemS + (uint32_t)g * kTileN;
+        const int pos_in_tile = r / a.group, head_in_group = r % a.group;
+        const float sl2 = a.scale_log2;
+        const float rescale = kRescaleLog2 / sl2;
+        uint32_t done = 0;   // slot tiles of this warpgroup so far
+        uint32_t joins = 0;  // joined parts so far
+        bool aborted = false;
+        auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
+            const bool good = wait_bounded(bar, parity, &sh.abort);
+            return __all_sync(0xffffffffu, good);
+        };
+        while (!aborted && w.next(a)) {
+            const bool two = w.t.two;
+            const int32_t n = w.loads();
+            const int32_t i = (2 * w.task_pair() + (two ? g : 0)) * a.positions + pos_in_tile;  // row of the sequence
+            const bool valid = r < a.positions * a.group && i < w.q.n;
+            RowSees sees{0, -1};
+            if (valid)
+                sees = row_sees(a.b, w.q, i);
+            const bool any = __any_sync(0xffffffffu, valid);
+            float m = -INFINITY, l = 0.f;  // m in units of S
+            bool have = false;             // O holds something
+            for (int32_t j = w.j0 + (two ? 0 : g); j < w.j0 + n; j += two ? 1 : 2) {
+                if (!wait_all(s_full(g), done & 1u)) {
+                    aborted = true;
+                    break;
+                }
+                if (any) {
+                    ptx::tc_fence_after();
+                    const int32_t lim = sees.lim - j * kTileN, hole = sees.hole - j * kTileN;
+                    const bool masked =
+                        __any_sync(0xffffffffu, valid && (lim < kTileN || (hole >= 0 && hole < kTileN)));
+                    // S is read twice, for the maximum and for the weights: holding 128 of it takes more registers than
+                    // a thread has.  Two chunks of 32 columns are in registers at a time, one of them on its way.
+                    float xa[32], xb[32];
+                    auto chunk = [&](float (&x)[32], int c) {  // what this row sees of columns [32 c, 32 c + 32)
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (32 * c + k >= lim || 32 * c + k == hole)
+                                    x[k] = -INFINITY;
+                        }
+                    };
+                    auto max32 = [&](const float (&x)[32]) {
+                        float y[11];
+#pragma unroll
+                        for (int k = 0; k < 10; ++k)
+                            y[k] = ptx::max3(x[3 * k], x[3 * k + 1], x[3 * k + 2]);
+                        y[10] = fmaxf(x[30], x[31]);
+                        const float z0 = ptx::max3(y[0], y[1], y[2]), z1 = ptx::max3(y[3], y[4], y[5]),
+                                    z2 = ptx::max3(y[6], y[7], y[8]), z3 = fmaxf(y[9], y[10]);
+                        return fmaxf(ptx::max3(z0, z1, z2), z3);
+                    };
+                    ptx::tmem_ld_32x32b_x32(t_s, xa);
+                    ptx::tmem_ld_wait(xa);
+                    ptx::tmem_ld_32x32b_x32(t_s + 32, xb);
+                    chunk(xa, 0);
+                    float mx = max32(xa);
+                    ptx::tmem_ld_wait(xb);
+                    ptx::tmem_ld_32x32b_x32(t_s + 64, xa);
+                    chunk(xb, 1);
+                    mx = fmaxf(mx, max32(xb));
+                    ptx::tmem_ld_wait(xa);
+                    ptx::tmem_ld_32x32b_x32(t_s + 96, xb);
+                    chunk(xa, 2);
+                    mx = fmaxf(mx, max32(xa));
+                    ptx::tmem_ld_wait(xb);
+                    ptx::tmem_ld_32x32b_x32(t_s, xa);
+                    chunk(xb, 3);
+                    mx = fmaxf(mx, max32(xb));
+                    const bool grow = mx > m + (m == -INFINITY ? 0.f : rescale);
+                    if (__any_sync(0xffffffffu, grow && m != -INFINITY) && have) {
+                        // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
+                        if (!wait_all(o_done(g), (done - 1u) & 1u)) {
+                            aborted = true;
+                            break;
+                        }
+                        ptx::tc_fence_after();
+                        const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
+                        l *= f;
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x32b_x16(lanes + kTmemO + (uint32_t)(g * DP + c), o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            ptx::tmem_st_32x32b_x16(lanes + kTmemO + (uint32_t)(g * DP + c), o);
+                        }
+                    }
+                    if (grow)
+                        m = mx;
+                    have = true;
+                    const float neg = m == -INFINITY ? 0.f : -m * sl2;
+                    const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(neg, neg);
+                    float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+                    auto weights = [&](const float (&x)[32], int c) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) {
+                            float2 u = ptx::fma2(make_float2(x[k], x[k + 1]), s2, n2);
+                            float2 v = ptx::fma2(make_float2(x[k + 2], x[k + 3]), s2, n2);
+                            u = make_float2(ptx::ex2(u.x), ptx::ex2(u.y));
+                            v = make_float2(ptx::ex2(v.x), ptx::ex2(v.y));
+                            l0 = ptx::add2(l0, u);
+                            l1 = ptx::add2(l1, v);
+                            p[k / 2] = pack2<kBf16>(u.x, u.y);
+                            p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
+                        }
+                        ptx::tmem_st_32x32b_x16(t_s + 16 * c, p);  // columns of S that have been read
+                    };
+                    ptx::tmem_ld_wait(xa);
+                    ptx::tmem_ld_32x32b_x32(t_s + 32, xb);
+                    chunk(xa, 0);
+                    weights(xa, 0);
+                    ptx::tmem_ld_wait(xb);
+                    ptx::tmem_ld_32x32b_x32(t_s + 64, xa);
+                    chunk(xb, 1);
+                    weights(xb, 1);
+                    ptx::tmem_ld_wait(xa);
+                    ptx::tmem_ld_32x32b_x32(t_s + 96, xb);
+                    chunk(xa, 2);
+                    weights(xa, 2);
+                    ptx::tmem_ld_wait(xb);
+                    chunk(xb, 3);
+                    weights(xb, 3);
+                    l += (l0.x + l0.y) + (l1.x + l1.y);
+                    ptx::tmem_st_wait();
+                }
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    ptx::mbar_arrive(p_ready(g));
+                ++done;
+            }
+            if (aborted)
+                break;
+            const bool mine = n > (two ? 0 : g);  // this warpgroup had slot tiles
+            if (mine) {
+                if (!wait_all(o_done(g), (done - 1u) & 1u)) {
+                    aborted = true;
+                    break;
+                }
+                ptx::tc_fence_after();
+            }
+            // Columns [c0, c1) of O, as f0 O_0 + f1 O_1 where two warpgroups join.
+            float f0 = 1.f, f1 = 0.f;
+            float big = m, sum = l;
+            int c0 = 0, c1 = DP;
+            if (!two) {
+                sh.ml[g][r] = make_float2(m, l);
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    ptx::mbar_arrive(ptx::smem_u32(&sh.ml_ready));
+                if (!wait_all(ptx::smem_u32(&sh.ml_ready), joins & 1u)) {
+                    aborted = true;
+                    break;
+                }
+                ptx::tc_fence_after();
+                const float2 m0 = sh.ml[0][r], m1 = sh.ml[1][r];
+                big = fmaxf(m0.x, m1.x);
+                f0 = m0.x == -INFINITY ? 0.f : ptx::ex2((m0.x - big) * sl2);
+                f1 = m1.x == -INFINITY ? 0.f : ptx::ex2((m1.x - big) * sl2);
+                sum = m0.y * f0 + m1.y * f1;
+                c0 = g * (DP / 2);
+                c1 = c0 + DP / 2;
+            }
+            const bool whole = w.whole();
+            const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // no slot seen: zeros; NaN stays NaN
+            const int slot_row = (two ? g * kTileM : 0) + r;
+            const int64_t part = (int64_t)blockIdx.x * 2 + (w.j0 > 0 ? 0 : 1);
+            if (!whole && valid && c0 == 0)
+                a.part_ml[part * a.split_rows + slot_row] = make_float2(big * sl2, sum);
+            if (any) {
+                const int64_t row = w.q.start + i;
+                const int head = w.kv_head * a.group + head_in_group;
+                uint16_t *const dst = a.out.data + row * a.out.row_stride + (int64_t)head * a.out.head_stride;
+                float4 *const po = a.part_o + part * (DP / 4) * a.split_rows + slot_row;
+                const int o_base = two ? g * DP : 0;
+#pragma unroll 1
+                for (int c = c0; c < c1; c += 32) {
+                    float o[32], o1[32];
+                    if (n > 0) {
+                        ptx::tmem_ld_32x32b_x32(lanes + kTmemO + (uint32_t)(o_base + c), o);
+                        if (!two && n > 1)
+                            ptx::tmem_ld_32x32b_x32(lanes + kTmemO + (uint32_t)(DP + c), o1);
+                        ptx::tmem_ld_wait();
+                    }
+                    if (n == 0) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            o[k] = 0.f;
+                    } else if (!two && n > 1) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            o[k] = f0 * o[k] + f1 * o1[k];
+                    }
+                    if (!valid)
+                        continue;
+                    if (whole) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8)
+                            if (c + k < a.b.head_dim) {
+                                uint4 y;
+                                y.x = pack2<kBf16>(o[k] * inv, o[k + 1] * inv);
+                                y.y = pack2<kBf16>(o[k + 2] * inv, o[k + 3] * inv);
+                                y.z = pack2<kBf16>(o[k + 4] * inv, o[k + 5] * inv);
+                                y.w = pack2<kBf16>(o[k + 6] * inv, o[k + 7] * inv);
+                                *reinterpret_cast<uint4 *>(dst + c + k) = y;
+                            }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            po[(int64_t)((c + k) / 4) * a.split_rows] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
                 }
-                float mx = x;
-                for (int i = 16; i; i >>= 1)
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, i));
-                const float mn = fmaxf(m, mx);
-                if (mn == -INFINITY)
+            }
+            if (!two) {  // both have read both accumulators and (m, l)
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    ptx::mbar_arrive(ptx::smem_u32(&sh.ml_done));
+                if (!wait_all(ptx::smem_u32(&sh.ml_done), joins & 1u)) {
+                    aborted = true;
+                    break;
+                }
+                ++joins;
+            }
+        }
+    } else {
+                if (warp == kWarpTma) {
+            // ------------------------------------------------------------ copies
+            constexpr int kHalves = DP / 64;
+            int64_t issued = 0;  // ring slots filled so far
+            uint32_t parts = 0;  // parts of tasks whose Q was loaded
+            bool aborted = false;
+            const int box = lane / kHalves, half = lane % kHalves;  // this lane's copy of a slot tile
+            while (!aborted && w.next(a)) {
+                const int32_t n = w.loads();
+                if (n == 0)
                     continue;
-                const float p = ptx::ex2(x - mn), f = ptx::ex2(m - mn);
-                m = mn;
-                l = l * f + p;
-                for (int i = 0; i < 4; ++i)
-                    o[i] *= f;
-                for (int t = 0; t < 32; ++t) {
-                    const int64_t av = __shfl_sync(0xffffffffu, at, t);
-                    const float pt = __shfl_sync(0xffffffffu, p, t);
-                    if (av >= 0)
-                        for (int i = 0; i < 4; ++i)
-                            if (lane + 32 * i < b.head_dim)
-                                o[i] = fmaf(pt, to_f(b.v_cache[av + lane + 32 * i], b.dtype), o[i]);
+                const bool two = w.t.two;
+                // Q: the part's one or two tiles
+                if (!__all_sync(0xffffffffu, wait_bounded(q_empty, (parts & 1u) ^ 1u, &sh.abort))) {
+                    aborted = true;
+                    break;
+                }
+                if (lane == 0)
+                    ptx::mbar_arrive_expect_tx(q_full, (uint32_t)(two ? 2 : 1) * kHalves * (uint32_t)(a.positions * a.group) * 128u);
+                __syncwarp();
+                if (lane < kHalves * (two ? 2 : 1)) {
+                    const int tile = lane / kHalves, h = lane % kHalves;
+                    ptx::tma_load_3d(sq + (uint32_t)tile * C::kTileBytes + (uint32_t)h * kHalfBytes, &tmQ, q_full, h * 64,
+                                     w.kv_head * a.group, w.q.start + (2 * w.task_pair() + tile) * a.positions);
+                }
+                ++parts;
+                // K and V, in the order in which the MMAs take them: K runs `lead` tiles ahead of V
+                const int lead = two ? 1 : 2;
+                // Page numbers: 32 consecutive table entries in the lanes, and the 32 behind them on their way.
+                const int32_t last_entry = (w.t.kv_end - 1) / a.b.page_size;
+                int32_t window = (w.j0 * kTileN) / a.b.page_size;  // first entry of `near`
+                auto entries = [&](int32_t e0) {
+                    const int32_t e = e0 + lane;
+                    return e <= last_entry ? load_page(a.b, w.seq, e, ok) : -1;
+                };
+                int32_t before = -1, near = entries(window), next = entries(window + 32);
+                auto copy = [&](const CUtensorMap *m, int32_t j) -> bool {
+                    const int s = (int)(issued % C::kSlots);
+                    const uint32_t phase = (uint32_t)(issued / C::kSlots) & 1u;
+                    const int32_t first = j * kTileN;
+                    const int32_t boxes = min(a.boxes, (w.t.kv_end - first + a.box_rows - 1) / a.box_rows);
+                    const int32_t at = first + box * a.box_rows;  // this lane's first slot
+                    const int32_t entry = at / a.b.page_size;
+                    const int32_t e = entry - window;
+                    // entries of this tile lie in `before` (V behind K), `near` or `next`
+                    const int32_t p0 = __shfl_sync(0xffffffffu, before, e & 31), p1 = __shfl_sync(0xffffffffu, near, e & 31),
+                                  p2 = __shfl_sync(0xffffffffu, next, e & 31);
+                    int32_t page = e < 0 ? p0 : (e < 32 ? p1 : p2);
+                    if (!__all_sync(0xffffffffu, wait_bounded(empty(s), phase ^ 1u, &sh.abort)))
+                        return false;
+                    if (lane == 0)
+                        ptx::mbar_arrive_expect_tx(full(s), (uint32_t)(boxes * kHalves * a.box_rows) * 128u);
+                    __syncwarp();
+                    if (box < boxes) {
+                        if (page < 0)
+                            page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
+                        ptx::tma_load_4d(slot_addr(s) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u, m,
+                                         full(s), half * 64, at - entry * a.b.page_size, w.kv_head, page);
+                    }
+                    ++issued;
+                    return true;
+                };
+                for (int32_t i = -lead; i < n && !aborted; ++i) {
+                    if (i >= 0 && !copy(&tmV, w.j0 + i))
+                        aborted = true;
+                    if (!aborted && i + lead < n) {
+                        const int32_t j = w.j0 + i + lead;
+                        const int32_t e_last = (min(w.t.kv_end, (j + 1) * kTileN) - 1) / a.b.page_size;
+                        if (e_last - window >= 48) {  // V, up to 3 tiles (24 entries) behind, stays within `before`
+                            before = near;
+                            near = next;
+                            window += 32;
+                            next = entries(window + 32);
+                        }
+                        if (!copy(&tmK, j))
+                            aborted = true;
+                    }
                 }
             }
-            for (int i = 16; i; i >>= 1)
-                l += __shfl_xor_sync(0xffffffffu, l, i);
-            for (int i = 0; i < 4; ++i)
-                if (lane + 32 * i < b.head_dim)
-                    a.out.data[row * a.out.row_stride + h * a.out.head_stride + lane + 32 * i] =
-                        from_f(l > 0.f ? o[i] / l : 0.f, b.dtype);
+            if (aborted && lane == 0) {  // copies already issued land before the shared memory goes away
+                if (parts > 0)
+                    wait_drain(q_full, (parts - 1) & 1u);
+                for (int s = 0; s < C::kSlots && s < issued; ++s)
+                    wait_drain(full(s), (uint32_t)((issued - 1 - s) / C::kSlots) & 1u);
+            }
+            __syncwarp();
+        } else if (warp == kWarpMma) {
+            // ------------------------------------------------------------ MMAs, issued by one thread
+            if (ptx::elect_one()) {
+                const uint32_t id_s = ptx::idesc_f16_f32(kTileM, kTileN, kBf16, false);
+                const uint32_t id_o = ptx::idesc_f16_f32(kTileM, DP, kBf16, true);
+                int64_t taken = 0;  // ring slots taken so far
+                uint32_t parts = 0, n_zeroed = 0;
+                uint32_t n_p[2] = {0, 0};  // slot tiles of each warpgroup whose P V was issued
+                bool aborted = false;
+                int slot = 0;
+                auto take = [&]() -> bool {  // the next ring slot has landed
+                    slot = (int)(taken % C::kSlots);
+                    const bool good = wait_bounded(full(slot), (uint32_t)(taken / C::kSlots) & 1u, &sh.abort);
+                    ++taken;
+                    return good;
+                };
+                auto scores = [&](int g, int qt, int ks) {  // S_g = Q_qt K^T
+                    const uint64_t da = ptx::sdesc_kmajor_sw128(sq + (uint32_t)qt * C::kTileBytes);
+                    const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks));
+    #pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const uint64_t off = (uint64_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
+                        ptx::mma_bf16(tmem + kTmemS + (uint32_t)g * kTileN, da + off, db + off, id_s, k != 0);
+                    }
+                    ptx::mma_commit(s_full(g));
+                };
+                auto values = [&](int g, int vs, bool add) {  // O_g (+)= P_g V
+                    const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), kHalfBytes);
+    #pragma unroll
+                    for (int k = 0; k < kTileN / 16; ++k)
+                        ptx::mma_f16_ts(tmem + kTmemO + (uint32_t)(g * DP), tmem + kTmemS + (uint32_t)(g * kTileN + k * 8),
+                                        db + (uint64_t)(k * (2048 >> 4)), id_o, (add || k != 0) ? 1u : 0u);
+                    ptx::mma_commit(o_done(g));
+                };
+                auto weights = [&](int g) -> bool {  // P_g is in tensor memory
+                    const bool good = wait_bounded(p_ready(g), n_p[g] & 1u, &sh.abort);
+                    ++n_p[g];
+                    ptx::tc_fence_after();
+                    return good;
+                };
+                while (!aborted && w.next(a)) {
+                    const int32_t n = w.loads();
+                    if (n == 0)
+                        continue;
+                    const bool two = w.t.two;
+                    const int lead = two ? 1 : 2;
+                    if (!wait_bounded(q_full, parts & 1u, &sh.abort)) {
+                        aborted = true;
+                        break;
+                    }
+                    ++parts;
+                    for (int32_t i = -lead; i < n && !aborted; ++i) {
+                        const bool last = i + lead == n - 1;
+                        const int g = two ? 0 : (i & 1);
+                        int vs = 0;
+                        if (i >= 0) {
+                            bool good = take();
+                            vs = slot;
+                            const bool zeros = i == n - 1 && w.tail();
+                            if (good && zeros)
+                                ptx::mbar_arrive(tail);
+                            good = good && weights(g);
+                            if (good && zeros)
+                                good = wait_bounded(zeroed, n_zeroed++ & 1u, &sh.abort);
+                            if (!good) {
+                                aborted = true;
+                                break;
+                            }
+                            values(g, vs, i >= lead);
+                            if (!two)
+                                ptx::mma_commit(empty(vs));
+                        }
+                        int ks = -1;
+                        if (i + lead < n) {
+                            if (!take()) {
+                                aborted = true;
+                                break;
+                            }
+                            ks = slot;
+                            scores(g, 0, ks);
+                        }
+                        if (two && i >= 0) {
+                            if (!weights(1)) {
+                                aborted = true;
+                                break;
+                            }
+                            values(1, vs, i > 0);
+                            ptx::mma_commit(empty(vs));
+                        }
+                        if (ks >= 0) {
+                            if (two)
+                                scores(1, 1, ks);
+                            ptx::mma_commit(empty(ks));
+                            if (last)
+                                ptx::mma_commit(q_empty);
+                        }
+                    }
+                }
+                ptx::mma_commit(mma_done);  // nothing may still write tensor memory when it is released
+                wait_drain(mma_done, 0);
+            }
+            __syncwarp();
+        } else if (warp == kWarpTail) {
+            // ------------------------------------------------------------ zeros behind the last slot
+            // V of slots that no row sees may be anything, and P = 0 times NaN is not 0.
+            int64_t before = 0;  // ring slots of earlier parts
+                uint32_t tails = 0;
+            bool aborted = false;
+            while (!aborted && w.next(a)) {
+                const int32_t n = w.loads();
+                if (n == 0)
+                    continue;
+                before += 2 * n;
+                if (!w.tail())
+                    continue;
+                const int64_t at = before - 1;  // V of the last tile is the part's last slot
+                const int s = (int)(at % C::kSlots);
+                // full(s) alone would not do: it may still be in an earlier phase of the same parity
+            aborted = !wait_bounded(tail, tails++ & 1u, &sh.abort) ||
+                      !wait_bounded(full(s), (uint32_t)(at / C::kSlots) & 1u, &sh.abort);
+                aborted = __any_sync(0xffffffffu, aborted);
+                if (aborted)
+                    break;
+                const int first = w.t.kv_end & (kTileN - 1);
+                uint8_t *const v = smem_raw + (slot_addr(s) - raw);
+                for (int x = first * 8 + lane; x < kTileN * 8; x += 32)
+    #pragma unroll
+                    for (int h = 0; h < DP / 64; ++h)
+                        *reinterpret_cast<uint4 *>(v + h * kHalfBytes + x * 16) = make_uint4(0, 0, 0, 0);
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0)
+                    ptx::mbar_arrive(zeroed);
+            }
         }
     }
     if (!ok)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (warp == kWarpMma)
+        ptx::tmem_dealloc(tmem, kTmemAll);
+    if (threadIdx.x == 0 && sh.abort)
+        atomicExch(&a.status->current, (int32_t)WINO_ERR_DEVICE_TIMEOUT);
 }
 
-__global__ void publish_kernel(StatusWords *status)
+// Joins the parts of the tasks that the runs' borders cut: CTA (c, y) takes rows 32 y .. of the task in which run c + 1
+// starts, if that is the first border inside it.  Lanes are rows, warps take columns in turn.
+template <int DP, bool kBf16>
+__global__ void __launch_bounds__(128) combine_kernel(const AttendArgs a)
 {
+    ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();
-    status->last = status->current;
-    status->current = WINO_OK;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        a.status->last = a.status->current;
+        a.status->current = WINO_OK;
+    }
+    const int32_t c = (int32_t)blockIdx.x + 1;
+    if (c >= kMaxCtas)
+        return;
+    const SplitRecord rec = a.records[c];
+    if (!rec.valid || rec.first != c - 1)
+        return;
+    const int slot_row = (int)blockIdx.y * kCombineRows + ((int)threadIdx.x & 31);
+    const int g = slot_row / kTileM, r = slot_row % kTileM;
+    const SeqRows q = load_seq(a.b, rec.seq);
+    const int32_t i = (2 * rec.pair + g) * a.positions + r / a.group;
+    if (slot_row >= a.split_rows || r >= a.positions * a.group || i >= q.n)
+        return;
+    auto part_of = [&](int32_t k) { return (int64_t)k * 2 + (k == rec.first ? 1 : 0); };
+    float m = -INFINITY;
+    for (int32_t k = rec.first; k <= rec.last; ++k)
+        m = fmaxf(m, a.part_ml[part_of(k) * a.split_rows + slot_row].x);
+    constexpr int kChunks = DP / 16;  // float4 columns per warp
+    float4 o[kChunks];
+#pragma unroll
+    for (int x = 0; x < kChunks; ++x)
+        o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    const int w = (int)threadIdx.x >> 5;
+    for (int32_t k = rec.first; k <= rec.last; ++k) {
+        const float2 ml = a.part_ml[part_of(k) * a.split_rows + slot_row];
+        const float f = ml.x == -INFINITY ? 0.f : ptx::ex2(ml.x - m);
+        l += f * ml.y;
+        const float4 *po = a.part_o + part_of(k) * (DP / 4) * a.split_rows + slot_row;
+        if (f == 0.f)
+            continue;  // nothing seen in this part, or nothing left of it
+#pragma unroll
+        for (int x = 0; x < kChunks; ++x) {
+            const float4 y = po[(int64_t)(x * 4 + w) * a.split_rows];
+            o[x].x = fmaf(f, y.x, o[x].x);
+            o[x].y = fmaf(f, y.y, o[x].y);
+            o[x].z = fmaf(f, y.z, o[x].z);
+            o[x].w = fmaf(f, y.w, o[x].w);
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+    const int head = rec.kv_head * a.group + r % a.group;
+    uint16_t *const dst = a.out.data + (int64_t)(q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
+#pragma unroll
+    for (int x = 0; x < kChunks; ++x) {
+        const int col = (x * 4 + w) * 4;
+        if (col < a.b.head_dim)
+            *reinterpret_cast<uint2 *>(dst + col) =
+                make_uint2(pack2<kBf16>(o[x].x * inv, o[x].y * inv), pack2<kBf16>(o[x].z * inv, o[x].w * inv));
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+int32_t positions_per_tile(const wino_kv_batch &b) { return kTileM / (b.n_q_heads / b.n_kv_heads); }
+
+int32_t split_rows(const wino_kv_batch &b)
+{
+    const int32_t g = b.n_q_heads / b.n_kv_heads;
+    return b.n_rows <= positions_per_tile(b) ? (b.n_rows * g + 31) / 32 * 32 : kSplitRows;
+}
+
+struct Scratch {
+    size_t records, ml, o, total;
+};
+
+Scratch scratch_layout(const wino_kv_batch &b)
+{
+    const size_t dp = b.head_dim <= 64 ? 64 : 128, rows = (size_t)split_rows(b) * 2 * kMaxCtas;
+    Scratch s{};
+    s.records = 0;
+    s.ml = round_up(kMaxCtas * sizeof(SplitRecord), 256);
+    s.o = s.ml + rows * sizeof(float2);
+    s.total = s.o + rows * dp * sizeof(float);
+    return s;
+}
+
+// A tensor map over 16-bit elements in 128-byte swizzled boxes 64 elements wide; strides in elements.
+int encode(CUtensorMap *m, int32_t dtype, const void *ptr, int rank, const int64_t *dims, const int64_t *strides,
+           const int32_t *box)
+{
+    auto fn = encode_fn();
+    if (!fn)
+        return WINO_ERR_CUDA;
+    cuuint64_t d[4], st[3];
+    cuuint32_t bx[4], es[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        d[i] = (cuuint64_t)dims[i];
+        bx[i] = (cuuint32_t)box[i];
+        if (i > 0)  // the stride of a single entry is never used; the encoder wants a legal one
+            st[i - 1] = (cuuint64_t)(dims[i] > 1 ? strides[i] : 64) * 2;
+    }
+    return fn(m, dtype == WINO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+              const_cast<void *>(ptr), d, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? WINO_OK
+               : WINO_ERR_CUDA;
+}
+
+template <int DP, bool kBf16>
+int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, const AttendArgs &a, int ctas,
+           cudaStream_t stream)
+{
+    static std::mutex mu;
+    static bool done[64];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64)
+        return WINO_ERR_CUDA;
+    {
+        std::lock_guard<std::mutex> g(mu);
+        if (!done[dev]) {
+            if (cudaFuncSetAttribute(attend_kernel<DP, kBf16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)Config<DP>::kSmem) != cudaSuccess)
+                return WINO_ERR_CUDA;
+            done[dev] = true;
+        }
+    }
+    static_assert(Config<DP>::kSmem <= kSmemLimit, "shared memory");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kAttendThreads);
+    cfg.dynamicSmemBytes = Config<DP>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attend_kernel<DP, kBf16>, tq, tk, tv, a) != cudaSuccess)
+        return WINO_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)std::max(1, ctas - 1), (unsigned)((a.split_rows + kCombineRows - 1) / kCombineRows));
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16>, a) == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t attend_scratch_bytes(const wino_kv_batch &) { return 0; }
+size_t attend_scratch_bytes(const wino_kv_batch &b) { return scratch_layout(b).total; }
 
-int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *,
-                  StatusWords *status, int, cudaStream_t stream)
+int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
+                  StatusWords *status, int sm_count, cudaStream_t stream)
 {
-    AttendArgs a{q, out, b, scale * 1.4426950408889634f, status};
-    attend_kernel<<<dim3((unsigned)b.n_rows, (unsigned)((b.n_q_heads + kWarps - 1) / kWarps)), kWarps * 32, 0, stream>>>(a);
-    if (cudaGetLastError() != cudaSuccess)
-        return WINO_ERR_CUDA;
-    publish_kernel<<<1, 1, 0, stream>>>(status);
-    return cudaGetLastError() == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
+    const Scratch L = scratch_layout(b);
+    AttendArgs a{};
+    a.q = q;
+    a.out = out;
+    a.b = b;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.status = status;
+    a.records = reinterpret_cast<SplitRecord *>(scratch + L.records);
+    a.part_ml = reinterpret_cast<float2 *>(scratch + L.ml);
+    a.part_o = reinterpret_cast<float4 *>(scratch + L.o);
+    a.split_rows = split_rows(b);
+    a.group = b.n_q_heads / b.n_kv_heads;
+    a.positions = positions_per_tile(b);
+    a.box_rows = std::min(b.page_size, kTileN);
+    a.boxes = kTileN / a.box_rows;
+    a.min_units = 2;
+    CUtensorMap tq, tk, tv;
+    const int64_t q_dims[3] = {b.head_dim, b.n_q_heads, b.n_rows}, q_strides[3] = {1, q.head_stride, q.row_stride};
+    const int32_t q_box[3] = {64, a.group, a.positions};
+    const int64_t kv_dims[4] = {b.head_dim, b.page_size, b.n_kv_heads, b.n_pages};
+    const int64_t kv_strides[4] = {1, b.slot_stride, b.head_stride, b.page_stride};
+    const int32_t kv_box[4] = {64, a.box_rows, 1, 1};
+    int rc;
+    if ((rc = encode(&tq, b.dtype, q.data, 3, q_dims, q_strides, q_box)) != WINO_OK ||
+        (rc = encode(&tk, b.dtype, b.k_cache, 4, kv_dims, kv_strides, kv_box)) != WINO_OK ||
+        (rc = encode(&tv, b.dtype, b.v_cache, 4, kv_dims, kv_strides, kv_box)) != WINO_OK)
+        return rc;
+    const int ctas = std::min(sm_count, kMaxCtas);
+    if (b.head_dim <= 64)
+        return b.dtype == WINO_BF16 ? launch<64, true>(tq, tk, tv, a, ctas, stream)
+                                    : launch<64, false>(tq, tk, tv, a, ctas, stream);
+    return b.dtype == WINO_BF16 ? launch<128, true>(tq, tk, tv, a, ctas, stream)
+                                : launch<128, false>(tq, tk, tv, a, ctas, stream);
 }
 
 }  // namespace wino
