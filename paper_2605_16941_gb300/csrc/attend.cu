@@ -38,20 +38,22 @@ namespace {
 constexpr int kTileM = 128, kTileN = 128;  // rows and slots of a tile
 constexpr int kSoftmaxThreads = 256;
 constexpr int kAttendThreads = kSoftmaxThreads + 128;
-constexpr int kWarpTma = 8, kWarpMma = 9, kWarpTail = 10;
-constexpr int kMaxCtas = 160;          // an SM each
-constexpr int kRecordBytes = 32;       // SplitRecord
-constexpr int kCombineRows = 32;       // rows per combine CTA
+constexpr int kWarpTma = 8, kWarpMma = 9, kWarpTail = 10, kWarpPlan = 11;
+constexpr int kMaxCtas = 160;           // an SM each
+constexpr int kRecordBytes = 32;        // SplitRecord
+constexpr int kCombineRows = 32;        // rows per combine CTA
 constexpr int kSplitRows = 2 * kTileM;  // rows of a task
+constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
+constexpr int kTaskCost = 2;            // what a task costs beside its slot tiles, in slot tiles
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemS = 0, kTmemO = 2 * kTileN, kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 
-// What combine_kernel needs to know of the run that CTA c starts inside a task with (one per CTA).
+// What combine_kernel needs to know of the task that CTA c's run starts inside (one per CTA).
 struct SplitRecord {
-    int32_t valid;  // the run starts inside a task
+    int32_t valid;  // an earlier run holds slot tiles of it too
     int32_t seq, kv_head, pair;
-    int32_t first, last;  // CTAs whose runs hold units of that task
+    int32_t first, last;  // CTAs whose runs hold slot tiles of it
     int32_t pad[2];
 };
 static_assert(sizeof(SplitRecord) == kRecordBytes, "record size");
@@ -66,94 +68,59 @@ struct AttendArgs {
     float4 *part_o;        // [kMaxCtas][2][DP / 4][split_rows]
     int32_t split_rows;
     int32_t group, positions;  // query heads per kv head, row positions per tile
+    uint32_t pair_magic;       // ceil(2^32 / (2 positions))
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
     int32_t min_units;         // a CTA's run is at least this long
 };
 
-// Row positions and slots of a task's tiles.
-struct Task {
-    int32_t kv_end;  // slots that some row sees
-    int32_t tiles;   // slot tiles, at least 1
-    bool two;        // rows in both tiles
-};
-
-__device__ __forceinline__ Task task_of(const AttendArgs &a, const SeqRows &q, int32_t pair)
-{
-    const int32_t w = 2 * a.positions;
-    const int32_t last = min(q.n, (pair + 1) * w) - 1;
-    Task t;
-    t.kv_end = row_sees(a.b, q, last).lim;  // no earlier row sees more
-    t.tiles = max(1, (t.kv_end + kTileN - 1) / kTileN);
-    t.two = q.n - pair * w > a.positions;
-    return t;
-}
-
+// Tasks of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256, so that the product with
+// pair_magic is the quotient (its error is below 2^24 / 2^32 < 1 / 256).
 __device__ __forceinline__ int32_t pairs_of(const AttendArgs &a, const SeqRows &q)
 {
-    return (q.n + 2 * a.positions - 1) / (2 * a.positions);
+    return (int32_t)__umulhi((uint32_t)(q.n + 2 * a.positions - 1), a.pair_magic);
 }
 
-// Run c of n over t units.
-__device__ __forceinline__ int64_t run_start(int64_t c, int64_t n, int64_t t) { return c * t / n; }
-__device__ __forceinline__ int32_t run_of(int64_t unit, int64_t n, int64_t t) { return (int32_t)(((unit + 1) * n - 1) / t); }
+// Slots that some row of task `pair` sees: its last row sees as many as any.
+__device__ __forceinline__ int32_t task_slots(const AttendArgs &a, const SeqRows &q, int32_t pair)
+{
+    return row_sees(a.b, q, min(q.n, (pair + 1) * 2 * a.positions) - 1).lim;
+}
 
-// Where a CTA's run starts, found once per CTA.
-struct RunStart {
-    int64_t units;  // of the run
-    int32_t seq, kv_head, pair, tile;
+__device__ __forceinline__ int32_t tiles_of(int32_t slots) { return max(1, (slots + kTileN - 1) / kTileN); }
+
+// The cut of `total` units into n runs: the first `more` of them are one unit longer.
+struct Cut {
+    int64_t total, per, more;
+    int32_t n;
+    __device__ __forceinline__ Cut(int64_t t, int32_t ctas, int32_t min_units) : total(t)
+    {
+        n = (int32_t)min((int64_t)ctas, max((int64_t)1, quotient(t, min_units)));
+        per = quotient(t, n);
+        more = t - per * n;
+    }
+    __device__ __forceinline__ int64_t start(int64_t c) const { return c * per + min(c, more); }
+    __device__ __forceinline__ int32_t run_of(int64_t unit) const
+    {
+        const int64_t longer = more * (per + 1);
+        return (int32_t)(unit < longer ? quotient(unit, per + 1) : more + quotient(unit - longer, per));
+    }
+    static __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)  // 64-bit division is slow
+    {
+        return ((x | y) >> 31) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+    }
 };
 
-// A CTA's run as a sequence of tasks or parts of tasks; every role walks it for itself.
-struct Walk {
-    int64_t left;
-    int32_t seq, kv_head, pair, tile;
+// One part of a task, as the planning warp hands it to the others: slot tiles [j0, j0 + n) of one sequence, kv head and
+// pair of row tiles.
+enum : int32_t { kTwo = 1, kTail = 2, kWhole = 4, kEnd = 8 };
+struct alignas(16) Part {
+    int32_t flags;   // kTwo: rows in both tiles; kTail: the last tile ends behind kv_end; kWhole: the task's only part
+    int32_t kv_end;  // slots that some row sees
+    int32_t j0, n;   // n = 0: nothing to see, the rows get zeros
+    int32_t seq, kv_head;
+    int32_t i0;      // the sequence's row of the first position
+    int32_t pad;
     SeqRows q;
-    int32_t n_pairs;
-    // the current part: slot tiles [j0, j1) of task t
-    Task t;
-    int32_t j0, j1;
-
-    __device__ __forceinline__ void start(const AttendArgs &a, const RunStart &r)
-    {
-        left = r.units;
-        seq = r.seq;
-        kv_head = r.kv_head;
-        pair = r.pair;
-        tile = r.tile;
-        if (left > 0) {
-            q = load_seq(a.b, seq);
-            n_pairs = pairs_of(a, q);
-        }
-    }
-    __device__ __forceinline__ bool next(const AttendArgs &a)
-    {
-        if (left <= 0)
-            return false;
-        if (pair == n_pairs) {
-            pair = 0;
-            if (++kv_head == a.b.n_kv_heads) {
-                kv_head = 0;
-                do {  // ends: there are units left
-                    if (++seq >= a.b.n_seq)
-                        return false;
-                    q = load_seq(a.b, seq);
-                } while (q.n == 0);
-                n_pairs = pairs_of(a, q);
-            }
-        }
-        t = task_of(a, q, pair);
-        j0 = tile;
-        j1 = (int32_t)min((int64_t)t.tiles, tile + left);
-        left -= j1 - j0;
-        tile = 0;
-        ++pair;
-        return true;
-    }
-    __device__ __forceinline__ int32_t task_pair() const { return pair - 1; }
-    __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == t.tiles; }
-    __device__ __forceinline__ int32_t loads() const { return t.kv_end > 0 ? j1 - j0 : 0; }
-    // The run's last tile ends behind the last slot that a row sees.
-    __device__ __forceinline__ bool tail() const { return j1 == t.tiles && (t.kv_end & (kTileN - 1)) != 0; }
 };
 
 template <int DP>
@@ -161,10 +128,13 @@ struct Config {
     static constexpr uint32_t kTileBytes = (DP / 64) * kHalfBytes;  // 128 rows or slots
     static constexpr int kSlots = DP == 128 ? 5 : 12;               // ring slots beside the two Q tiles
     static constexpr uint32_t kRing = kSlots * kTileBytes;
-    static constexpr uint32_t kSmem = 2 * kTileBytes + kRing + 2560;
+    static constexpr uint32_t kShared = 3072;
+    static constexpr uint32_t kSmem = 2 * kTileBytes + kRing + kShared;
 };
 
-struct alignas(8) Shared {
+struct alignas(16) Shared {
+    Part parts[kParts];
+    uint64_t part_full[kParts], part_empty[kParts];
     uint64_t q_full, q_empty;
     uint64_t full[12], empty[12];
     uint64_t s_full[2], p_ready[2], o_done[2];
@@ -173,11 +143,9 @@ struct alignas(8) Shared {
     uint64_t mma_done;
     uint32_t tmem;
     int32_t abort;
-    RunStart run;
-    int64_t units[kAttendThreads / 32];
     float2 ml[2][kTileM];
 };
-static_assert(sizeof(Shared) <= 2560, "shared block must fit its reserve");
+static_assert(sizeof(Shared) <= 3072, "shared block must fit its reserve");
 
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
@@ -190,107 +158,173 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
     return r;
 }
 
-// Units of sequence s in the lanes of a group of `width` threads (each returns the sum).
-__device__ __forceinline__ int64_t seq_units(const AttendArgs &a, const SeqRows &q, int lane, int width)
+// Bounded wait of a whole warp: the same answer in every lane.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int32_t *abort)
 {
-    int64_t u = 0;
-    const int32_t n_pairs = q.n > 0 ? pairs_of(a, q) : 0;
-    for (int32_t p = lane; p < n_pairs; p += width)
-        u += task_of(a, q, p).tiles;
-    for (int i = width >> 1; i; i >>= 1)
-        u += __shfl_xor_sync(0xffffffffu, u, i);
-    return u * a.b.n_kv_heads;
+    return __all_sync(0xffffffffu, wait_bounded(bar, parity, abort));
 }
 
-// Finds this CTA's run (all threads; the result is in sh.run for every thread after the closing barrier).
-__device__ __forceinline__ void find_run(const AttendArgs &a, Shared &sh, bool &ok)
+// A reader's place in the ring of parts.
+struct PartReader {
+    uint32_t count = 0;
+    __device__ __forceinline__ uint32_t parity() const { return (count / kParts) & 1u; }
+    __device__ __forceinline__ int slot() const { return (int)(count % kParts); }
+};
+
+// The planning warp: cuts the work and hands this CTA's run out part by part.
+__device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, bool &ok)
 {
-    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int32_t n_seq = a.b.n_seq;
-    int width = 32;  // threads per sequence
-    while (width > 1 && n_seq * width > kAttendThreads)
+    const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads;
+    int width = 32;  // lanes per sequence
+    while (width > 1 && n_seq * width > 32)
         width >>= 1;
-    const int per = kAttendThreads / width;  // sequences per round
-    const int sub = lane & (width - 1);
-    auto units_of = [&](int32_t s, SeqRows &q) {
+    const int per_round = 32 / width, sub = lane & (width - 1);
+    SeqRows q;
+    int64_t mine = 0;  // units of this lane's sequence
+    auto load_round = [&](int32_t s0) {
+        const int32_t s = s0 + lane / width;
         q.n = 0;
         q.ok = true;
         if (s < n_seq)
             q = load_seq(a.b, s);
-        return seq_units(a, q, sub, width);
-    };
-    SeqRows q;
-    int64_t total = 0, mine = 0;
-    for (int32_t s0 = 0; s0 < n_seq; s0 += per) {
-        mine = units_of(s0 + tid / width, q);
         ok = ok && q.ok;
-        int64_t w = sub == 0 ? mine : 0;
+        int64_t u = 0;
+        const int32_t n_pairs = q.n > 0 ? pairs_of(a, q) : 0;
+        for (int32_t p = sub; p < n_pairs; p += width)
+            u += tiles_of(task_slots(a, q, p)) + kTaskCost;
+        for (int i = width >> 1; i; i >>= 1)
+            u += __shfl_xor_sync(0xffffffffu, u, i);
+        mine = u * n_kv;
+    };
+    int64_t total = 0;
+    for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
+        load_round(s0);
+        int64_t u = sub == 0 ? mine : 0;
         for (int i = 16; i; i >>= 1)
-            w += __shfl_xor_sync(0xffffffffu, w, i);
-        total += w;
+            u += __shfl_xor_sync(0xffffffffu, u, i);
+        total += u;
+    }
+    const Cut cut(total, (int32_t)gridDim.x, a.min_units);
+    const int32_t c = (int32_t)blockIdx.x;
+    int64_t at = cut.start(c);  // the next unit to hand out
+    const int64_t end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
+    SplitRecord rec{};
+    int32_t seq = 0, kv_head = 0, pair = 0;
+    int64_t task = 0;  // the unit at which the current task starts
+    uint32_t sent = 0;
+    bool go = at < end;
+    if (go) {
+        // the sequence that holds unit `at`
+        int64_t before = 0;
+        for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
+            if (n_seq > per_round)
+                load_round(s0);
+            int64_t pre = sub == 0 ? mine : 0;
+            for (int i = 1; i < 32; i <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
+                if (lane >= i)
+                    pre += up;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, before + pre > at);
+            if (hit) {
+                const int src = __ffs(hit) - 1;  // a sequence's first lane: `pre` grows there only
+                seq = s0 + src / width;
+                task = before + __shfl_sync(0xffffffffu, pre, src) - __shfl_sync(0xffffffffu, mine, src);
+                mine = __shfl_sync(0xffffffffu, mine, src);
+                q.start = __shfl_sync(0xffffffffu, q.start, src);
+                q.n = __shfl_sync(0xffffffffu, q.n, src);
+                q.kv = __shfl_sync(0xffffffffu, q.kv, src);
+                q.base = __shfl_sync(0xffffffffu, q.base, src);
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, pre, 31);
+        }
+        // its kv head, and by the sum over 32 tasks at a time the task
+        const int64_t head = Cut::quotient(mine, n_kv);
+        kv_head = (int32_t)Cut::quotient(at - task, head);
+        task += kv_head * head;
+        const int32_t n_pairs = pairs_of(a, q);
+        for (int32_t p0 = 0; p0 < n_pairs; p0 += 32) {
+            const int32_t p = p0 + lane;
+            const int64_t cost = p < n_pairs ? tiles_of(task_slots(a, q, p)) + kTaskCost : 0;
+            int64_t pre = cost;
+            for (int i = 1; i < 32; i <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
+                if (lane >= i)
+                    pre += up;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, task + pre > at);
+            if (hit) {
+                const int src = __ffs(hit) - 1;
+                pair = p0 + src;
+                task += __shfl_sync(0xffffffffu, pre, src) - __shfl_sync(0xffffffffu, cost, src);
+                break;
+            }
+            task += __shfl_sync(0xffffffffu, pre, 31);
+        }
+        const int32_t tiles = tiles_of(task_slots(a, q, pair));
+        rec.valid = at - task > kTaskCost;
+        rec.seq = seq;
+        rec.kv_head = kv_head;
+        rec.pair = pair;
+        rec.first = cut.run_of(task + kTaskCost);
+        rec.last = cut.run_of(task + kTaskCost + tiles - 1);
     }
     if (lane == 0)
-        sh.units[warp] = total;
-    if (tid == 0)
-        sh.run.units = 0;
-    __syncthreads();
-    total = 0;
-    for (int i = 0; i < kAttendThreads / 32; ++i)
-        total += sh.units[i];
-    const int64_t n = min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
-    const int64_t c = blockIdx.x;
-    const int64_t start = run_start(c, n, total), units = c < n ? run_start(c + 1, n, total) - start : 0;
-    // the sequence that holds the run's first unit
-    int64_t before = 0;  // units of earlier rounds
-    for (int32_t s0 = 0; s0 < n_seq && units > 0; s0 += per) {
-        if (n_seq > per)
-            mine = units_of(s0 + tid / width, q);
-        __syncthreads();
-        int64_t pre = sub == 0 ? mine : 0;  // inclusive over the lanes, then over the warps
-        for (int i = 1; i < 32; i <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
-            if (lane >= i)
-                pre += up;
+        a.records[c] = rec;
+    int32_t n_pairs = go ? pairs_of(a, q) : 0;
+    while (true) {
+        Part part;
+        part.flags = kEnd;
+        part.kv_end = part.j0 = part.n = part.i0 = part.pad = 0;
+        if (go) {
+            const int32_t slots = task_slots(a, q, pair), tiles = tiles_of(slots);
+            // a task's own cost comes before its tiles
+            const int64_t t0 = at - task - kTaskCost, t1 = end - task - kTaskCost;
+            part.j0 = (int32_t)max((int64_t)0, t0);
+            part.n = (int32_t)min((int64_t)tiles, t1) - part.j0;
+            part.kv_end = slots;
+            part.i0 = pair * 2 * a.positions;
+            const bool to_end = part.j0 + part.n == tiles;
+            part.flags = (q.n - part.i0 > a.positions ? kTwo : 0) |
+                         (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
+            task += tiles + kTaskCost;
+            at = task;
+            go = at < end;
         }
-        if (lane == 31)
-            sh.units[warp] = pre;
-        __syncthreads();
-        int64_t round = 0, base = before;
-        for (int i = 0; i < kAttendThreads / 32; ++i) {
-            if (i < warp)
-                base += sh.units[i];
-            round += sh.units[i];
-        }
-        const int64_t s_end = base + pre, s_start = s_end - mine;
-        if (sub == 0 && start >= s_start && start < s_end) {
-            const int64_t per_head = mine / a.b.n_kv_heads;
-            RunStart r;
-            r.units = units;
-            r.seq = s0 + tid / width;
-            r.kv_head = (int32_t)((start - s_start) / per_head);
-            int64_t in_head = (start - s_start) % per_head;
-            r.pair = 0;
-            int32_t tiles = task_of(a, q, 0).tiles;
-            while (in_head >= tiles) {
-                in_head -= tiles;
-                tiles = task_of(a, q, ++r.pair).tiles;
+        part.seq = seq;
+        part.kv_head = kv_head;
+        part.q = q;
+        const bool last = (part.flags & kEnd) != 0;
+        if (last || part.n > 0) {  // a run may end within a task's own cost
+            if (part.kv_end == 0)
+                part.n = 0;
+            const int slot = (int)(sent % kParts);
+            if (!warp_wait(ptx::smem_u32(&sh.part_empty[slot]), ((sent / kParts) & 1u) ^ 1u, &sh.abort))
+                return;
+            if (lane == 0) {
+                sh.parts[slot] = part;
+                ptx::mbar_arrive(ptx::smem_u32(&sh.part_full[slot]));
             }
-            r.tile = (int32_t)in_head;
-            sh.run = r;
-            SplitRecord rec{};
-            rec.valid = r.tile > 0;
-            rec.seq = r.seq;
-            rec.kv_head = r.kv_head;
-            rec.pair = r.pair;
-            rec.first = run_of(start - in_head, n, total);
-            rec.last = run_of(start - in_head + tiles - 1, n, total);
-            a.records[c] = rec;
+            ++sent;
         }
-        before += round;
+        if (last)
+            return;
+        if (go && ++pair == n_pairs) {
+            pair = 0;
+            if (++kv_head == n_kv) {
+                kv_head = 0;
+                do {  // there are units left, so there is a sequence with rows
+                    ++seq;
+                    q.n = 0;
+                    if (seq < n_seq)
+                        q = load_seq(a.b, seq);
+                } while (q.n == 0 && seq < n_seq);
+                go = q.n > 0;
+                n_pairs = go ? pairs_of(a, q) : 0;
+            }
+        }
     }
-    if (units == 0 && tid == 0)
-        a.records[c].valid = 0;
-    __syncthreads();
 }
 
 template <int DP, bool kBf16>
@@ -306,29 +340,37 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     auto full = [&](int s) { return ptx::smem_u32(&sh.full[s]); };
     auto empty = [&](int s) { return ptx::smem_u32(&sh.empty[s]); };
-    auto s_full = [&](int w) { return ptx::smem_u32(&sh.s_full[w]); };
-    auto p_ready = [&](int w) { return ptx::smem_u32(&sh.p_ready[w]); };
-    auto o_done = [&](int w) { return ptx::smem_u32(&sh.o_done[w]); };
+    auto s_full = [&](int g) { return ptx::smem_u32(&sh.s_full[g]); };
+    auto p_ready = [&](int g) { return ptx::smem_u32(&sh.p_ready[g]); };
+    auto o_done = [&](int g) { return ptx::smem_u32(&sh.o_done[g]); };
+    auto part_full = [&](int s) { return ptx::smem_u32(&sh.part_full[s]); };
+    auto part_empty = [&](int s) { return ptx::smem_u32(&sh.part_empty[s]); };
     const uint32_t q_full = ptx::smem_u32(&sh.q_full), q_empty = ptx::smem_u32(&sh.q_empty);
-    const uint32_t tail = ptx::smem_u32(&sh.tail), zeroed = ptx::smem_u32(&sh.zeroed), mma_done = ptx::smem_u32(&sh.mma_done);
+    const uint32_t tail = ptx::smem_u32(&sh.tail), zeroed = ptx::smem_u32(&sh.zeroed);
+    const uint32_t ml_ready = ptx::smem_u32(&sh.ml_ready), ml_done = ptx::smem_u32(&sh.ml_done);
+    const uint32_t mma_done = ptx::smem_u32(&sh.mma_done);
     auto slot_addr = [&](int s) { return ring + (uint32_t)s * C::kTileBytes; };
 
     if (threadIdx.x == 0) {
+        for (int s = 0; s < kParts; ++s) {
+            ptx::mbar_init(part_full(s), 1);
+            ptx::mbar_init(part_empty(s), 11);  // 8 softmax warps, copies, MMAs, zeros
+        }
         ptx::mbar_init(q_full, 1);
         ptx::mbar_init(q_empty, 1);
         for (int s = 0; s < C::kSlots; ++s) {
             ptx::mbar_init(full(s), 1);
             ptx::mbar_init(empty(s), 1);
         }
-        for (int w = 0; w < 2; ++w) {
-            ptx::mbar_init(s_full(w), 1);
-            ptx::mbar_init(p_ready(w), 4);
-            ptx::mbar_init(o_done(w), 1);
+        for (int g = 0; g < 2; ++g) {
+            ptx::mbar_init(s_full(g), 1);
+            ptx::mbar_init(p_ready(g), 4);
+            ptx::mbar_init(o_done(g), 1);
         }
         ptx::mbar_init(tail, 1);
         ptx::mbar_init(zeroed, 1);
-        ptx::mbar_init(ptx::smem_u32(&sh.ml_ready), 8);
-        ptx::mbar_init(ptx::smem_u32(&sh.ml_done), 8);
+        ptx::mbar_init(ml_ready, 8);
+        ptx::mbar_init(ml_done, 8);
         ptx::mbar_init(mma_done, 1);
         sh.abort = 0;
         ptx::fence_barrier_init();
@@ -342,97 +384,94 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), kTmemAll);
         ptx::tmem_relinquish();
     }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = sh.tmem;
     ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();  // lengths, pages, q and the cache may come from the kernel before
     bool ok = true;
-    ptx::tc_fence_before();
-    find_run(a, sh, ok);
-    ptx::tc_fence_after();
-    const uint32_t tmem = sh.tmem;
-    Walk w;
-    w.start(a, sh.run);
+    PartReader reader;
+    // the next part; false after the last one or an abort.  done_with() gives its place back.
+    auto next_part = [&]() -> bool {
+        if (!wait_bounded(part_full(reader.slot()), reader.parity(), &sh.abort))
+            return false;
+        return (sh.parts[reader.slot()].flags & kEnd) == 0;
+    };
+    auto done_with = [&]() {  // by one lane, after the warp's reads
+        ptx::mbar_arrive(part_empty(reader.slot()));
+    };
+
+    // A softmax thread holds its row of S: the launch's 384 x 168 registers are split 208 / 88.
     if (warp < 8) {
-                // ------------------------------------------------------------ softmax: one thread per row
-        const int g = warp >> 2;                  // warpgroup
-        const int r = (warp & 3) * 32 + lane;     // row of the tile, its TMEM lane
+        // ------------------------------------------------------------ softmax: one thread per row
+        ptx::regs_inc<208>();
+        const int g = warp >> 2;               // warpgroup
+        const int r = (warp & 3) * 32 + lane;  // row of the tile, its TMEM lane
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t t_s = lanes + kTmemS + (uint32_t)g * kTileN;
-        const int pos_in_tile = r / a.group, head_in_group = r % a.group;
+        const int pos_in_tile = r / a.group;
         const float sl2 = a.scale_log2;
         const float rescale = kRescaleLog2 / sl2;
         uint32_t done = 0;   // slot tiles of this warpgroup so far
         uint32_t joins = 0;  // joined parts so far
-        bool aborted = false;
-        auto wait_all = [&](uint32_t bar, uint32_t parity) -> bool {
-            const bool good = wait_bounded(bar, parity, &sh.abort);
-            return __all_sync(0xffffffffu, good);
-        };
-        while (!aborted && w.next(a)) {
-            const bool two = w.t.two;
-            const int32_t n = w.loads();
-            const int32_t i = (2 * w.task_pair() + (two ? g : 0)) * a.positions + pos_in_tile;  // row of the sequence
-            const bool valid = r < a.positions * a.group && i < w.q.n;
-            RowSees sees{0, -1};
-            if (valid)
-                sees = row_sees(a.b, w.q, i);
+        while (__all_sync(0xffffffffu, next_part())) {
+            const Part &part = sh.parts[reader.slot()];
+            const bool two = (part.flags & kTwo) != 0;
+            const int32_t n = part.n;
+            const int32_t i = part.i0 + (two ? g : 0) * a.positions + pos_in_tile;  // row of the sequence
+            const bool valid = pos_in_tile < a.positions && i < part.q.n;
+            int32_t lim = 0, hole = -1;  // what the row sees, from the current tile's first slot on
+            if (valid) {
+                const RowSees sees = row_sees(a.b, part.q, i);
+                lim = sees.lim;
+                hole = sees.hole;
+            }
             const bool any = __any_sync(0xffffffffu, valid);
             float m = -INFINITY, l = 0.f;  // m in units of S
-            bool have = false;             // O holds something
-            for (int32_t j = w.j0 + (two ? 0 : g); j < w.j0 + n; j += two ? 1 : 2) {
-                if (!wait_all(s_full(g), done & 1u)) {
-                    aborted = true;
+            const int32_t step = two ? 1 : 2, first = two ? 0 : g;
+            lim -= (part.j0 + first) * kTileN;
+            hole -= (part.j0 + first) * kTileN;
+            int32_t t = first;
+            bool good = true;
+            for (; t < n; t += step, lim -= step * kTileN, hole -= step * kTileN) {
+                if (!(good = warp_wait(s_full(g), done & 1u, &sh.abort)))
                     break;
-                }
                 if (any) {
                     ptx::tc_fence_after();
-                    const int32_t lim = sees.lim - j * kTileN, hole = sees.hole - j * kTileN;
-                    const bool masked =
-                        __any_sync(0xffffffffu, valid && (lim < kTileN || (hole >= 0 && hole < kTileN)));
-                    // S is read twice, for the maximum and for the weights: holding 128 of it takes more registers than
-                    // a thread has.  Two chunks of 32 columns are in registers at a time, one of them on its way.
-                    float xa[32], xb[32];
-                    auto chunk = [&](float (&x)[32], int c) {  // what this row sees of columns [32 c, 32 c + 32)
-                        if (masked) {
+                    float x[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        ptx::tmem_ld_32x32b_x32(t_s + 32 * c, x[c]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        ptx::tmem_ld_wait(x[c]);
+                    if (__any_sync(0xffffffffu, valid && (lim < kTileN || (hole >= 0 && hole < kTileN)))) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
                                 if (32 * c + k >= lim || 32 * c + k == hole)
-                                    x[k] = -INFINITY;
-                        }
-                    };
-                    auto max32 = [&](const float (&x)[32]) {
-                        float y[11];
+                                    x[c][k] = -INFINITY;
+                    }
+                    float y[8];
 #pragma unroll
-                        for (int k = 0; k < 10; ++k)
-                            y[k] = ptx::max3(x[3 * k], x[3 * k + 1], x[3 * k + 2]);
-                        y[10] = fmaxf(x[30], x[31]);
-                        const float z0 = ptx::max3(y[0], y[1], y[2]), z1 = ptx::max3(y[3], y[4], y[5]),
-                                    z2 = ptx::max3(y[6], y[7], y[8]), z3 = fmaxf(y[9], y[10]);
-                        return fmaxf(ptx::max3(z0, z1, z2), z3);
-                    };
-                    ptx::tmem_ld_32x32b_x32(t_s, xa);
-                    ptx::tmem_ld_wait(xa);
-                    ptx::tmem_ld_32x32b_x32(t_s + 32, xb);
-                    chunk(xa, 0);
-                    float mx = max32(xa);
-                    ptx::tmem_ld_wait(xb);
-                    ptx::tmem_ld_32x32b_x32(t_s + 64, xa);
-                    chunk(xb, 1);
-                    mx = fmaxf(mx, max32(xb));
-                    ptx::tmem_ld_wait(xa);
-                    ptx::tmem_ld_32x32b_x32(t_s + 96, xb);
-                    chunk(xa, 2);
-                    mx = fmaxf(mx, max32(xa));
-                    ptx::tmem_ld_wait(xb);
-                    ptx::tmem_ld_32x32b_x32(t_s, xa);
-                    chunk(xb, 3);
-                    mx = fmaxf(mx, max32(xb));
+                    for (int k = 0; k < 8; ++k) {
+                        y[k] = ptx::max3(x[0][k], x[0][k + 8], x[0][k + 16]);
+                        y[k] = ptx::max3(y[k], x[0][k + 24], x[1][k]);
+                        y[k] = ptx::max3(y[k], x[1][k + 8], x[1][k + 16]);
+                        y[k] = ptx::max3(y[k], x[1][k + 24], x[2][k]);
+                        y[k] = ptx::max3(y[k], x[2][k + 8], x[2][k + 16]);
+                        y[k] = ptx::max3(y[k], x[2][k + 24], x[3][k]);
+                        y[k] = ptx::max3(y[k], x[3][k + 8], x[3][k + 16]);
+                        y[k] = fmaxf(y[k], x[3][k + 24]);
+                    }
+                    const float mx = ptx::max3(ptx::max3(y[0], y[1], y[2]), ptx::max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
                     const bool grow = mx > m + (m == -INFINITY ? 0.f : rescale);
-                    if (__any_sync(0xffffffffu, grow && m != -INFINITY) && have) {
+                    if (t != first && __any_sync(0xffffffffu, grow && m != -INFINITY)) {
                         // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
-                        if (!wait_all(o_done(g), (done - 1u) & 1u)) {
-                            aborted = true;
+                        if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
                             break;
-                        }
                         ptx::tc_fence_after();
                         const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
                         l *= f;
@@ -449,16 +488,16 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     if (grow)
                         m = mx;
-                    have = true;
                     const float neg = m == -INFINITY ? 0.f : -m * sl2;
                     const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(neg, neg);
                     float2 l0 = make_float2(0.f, 0.f), l1 = l0;
-                    auto weights = [&](const float (&x)[32], int c) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
                         uint32_t p[16];
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
-                            float2 u = ptx::fma2(make_float2(x[k], x[k + 1]), s2, n2);
-                            float2 v = ptx::fma2(make_float2(x[k + 2], x[k + 3]), s2, n2);
+                            float2 u = ptx::fma2(make_float2(x[c][k], x[c][k + 1]), s2, n2);
+                            float2 v = ptx::fma2(make_float2(x[c][k + 2], x[c][k + 3]), s2, n2);
                             u = make_float2(ptx::ex2(u.x), ptx::ex2(u.y));
                             v = make_float2(ptx::ex2(v.x), ptx::ex2(v.y));
                             l0 = ptx::add2(l0, u);
@@ -466,23 +505,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             p[k / 2] = pack2<kBf16>(u.x, u.y);
                             p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
                         }
-                        ptx::tmem_st_32x32b_x16(t_s + 16 * c, p);  // columns of S that have been read
-                    };
-                    ptx::tmem_ld_wait(xa);
-                    ptx::tmem_ld_32x32b_x32(t_s + 32, xb);
-                    chunk(xa, 0);
-                    weights(xa, 0);
-                    ptx::tmem_ld_wait(xb);
-                    ptx::tmem_ld_32x32b_x32(t_s + 64, xa);
-                    chunk(xb, 1);
-                    weights(xb, 1);
-                    ptx::tmem_ld_wait(xa);
-                    ptx::tmem_ld_32x32b_x32(t_s + 96, xb);
-                    chunk(xa, 2);
-                    weights(xa, 2);
-                    ptx::tmem_ld_wait(xb);
-                    chunk(xb, 3);
-                    weights(xb, 3);
+                        ptx::tmem_st_32x32b_x16(t_s + 16 * c, p);
+                    }
                     l += (l0.x + l0.y) + (l1.x + l1.y);
                     ptx::tmem_st_wait();
                 }
@@ -492,14 +516,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     ptx::mbar_arrive(p_ready(g));
                 ++done;
             }
-            if (aborted)
+            if (!good)
                 break;
-            const bool mine = n > (two ? 0 : g);  // this warpgroup had slot tiles
-            if (mine) {
-                if (!wait_all(o_done(g), (done - 1u) & 1u)) {
-                    aborted = true;
+            if (n > first) {  // this warpgroup had slot tiles
+                if (!warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort))
                     break;
-                }
                 ptx::tc_fence_after();
             }
             // Columns [c0, c1) of O, as f0 O_0 + f1 O_1 where two warpgroups join.
@@ -511,11 +532,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0)
-                    ptx::mbar_arrive(ptx::smem_u32(&sh.ml_ready));
-                if (!wait_all(ptx::smem_u32(&sh.ml_ready), joins & 1u)) {
-                    aborted = true;
+                    ptx::mbar_arrive(ml_ready);
+                if (!warp_wait(ml_ready, joins & 1u, &sh.abort))
                     break;
-                }
                 ptx::tc_fence_after();
                 const float2 m0 = sh.ml[0][r], m1 = sh.ml[1][r];
                 big = fmaxf(m0.x, m1.x);
@@ -525,83 +544,106 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 c0 = g * (DP / 2);
                 c1 = c0 + DP / 2;
             }
-            const bool whole = w.whole();
-            const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // no slot seen: zeros; NaN stays NaN
+            const bool whole = (part.flags & kWhole) != 0;
             const int slot_row = (two ? g * kTileM : 0) + r;
-            const int64_t part = (int64_t)blockIdx.x * 2 + (w.j0 > 0 ? 0 : 1);
+            const int64_t to = (int64_t)blockIdx.x * 2 + (part.j0 > 0 ? 0 : 1);  // the part's place in the workspace
             if (!whole && valid && c0 == 0)
-                a.part_ml[part * a.split_rows + slot_row] = make_float2(big * sl2, sum);
+                a.part_ml[to * a.split_rows + slot_row] = make_float2(big * sl2, sum);
             if (any) {
-                const int64_t row = w.q.start + i;
-                const int head = w.kv_head * a.group + head_in_group;
-                uint16_t *const dst = a.out.data + row * a.out.row_stride + (int64_t)head * a.out.head_stride;
-                float4 *const po = a.part_o + part * (DP / 4) * a.split_rows + slot_row;
-                const int o_base = two ? g * DP : 0;
+                if (whole) {  // no slot seen: zeros; NaN stays NaN
+                    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+                    f0 *= inv;
+                    f1 *= inv;
+                }
+                const int head = part.kv_head * a.group + (r - pos_in_tile * a.group);
+                uint16_t *const dst = a.out.data + (int64_t)(part.q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
+                float4 *const po = a.part_o + to * (DP / 4) * a.split_rows + slot_row;
+                const uint32_t t_o = lanes + kTmemO + (uint32_t)(two ? g * DP : 0);
 #pragma unroll 1
                 for (int c = c0; c < c1; c += 32) {
-                    float o[32], o1[32];
+                    float o[32];
                     if (n > 0) {
-                        ptx::tmem_ld_32x32b_x32(lanes + kTmemO + (uint32_t)(o_base + c), o);
-                        if (!two && n > 1)
-                            ptx::tmem_ld_32x32b_x32(lanes + kTmemO + (uint32_t)(DP + c), o1);
-                        ptx::tmem_ld_wait();
-                    }
-                    if (n == 0) {
+                        ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)c, o);
+                        ptx::tmem_ld_wait(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            o[k] *= f0;
+                    } else {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
                             o[k] = 0.f;
-                    } else if (!two && n > 1) {
+                    }
+                    if (!two && n > 1) {
+                        float o1[32];
+                        ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)(DP + c), o1);
+                        ptx::tmem_ld_wait(o1);
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
-                            o[k] = f0 * o[k] + f1 * o1[k];
+                            o[k] = fmaf(f1, o1[k], o[k]);
                     }
-                    if (!valid)
-                        continue;
-                    if (whole) {
+                    if (!valid) {
+                    } else if (whole) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 8)
-                            if (c + k < a.b.head_dim) {
-                                uint4 y;
-                                y.x = pack2<kBf16>(o[k] * inv, o[k + 1] * inv);
-                                y.y = pack2<kBf16>(o[k + 2] * inv, o[k + 3] * inv);
-                                y.z = pack2<kBf16>(o[k + 4] * inv, o[k + 5] * inv);
-                                y.w = pack2<kBf16>(o[k + 6] * inv, o[k + 7] * inv);
-                                *reinterpret_cast<uint4 *>(dst + c + k) = y;
-                            }
+                            if (c + k < a.b.head_dim)
+                                *reinterpret_cast<uint4 *>(dst + c + k) =
+                                    make_uint4(pack2<kBf16>(o[k], o[k + 1]), pack2<kBf16>(o[k + 2], o[k + 3]),
+                                               pack2<kBf16>(o[k + 4], o[k + 5]), pack2<kBf16>(o[k + 6], o[k + 7]));
                     } else {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
                             po[(int64_t)((c + k) / 4) * a.split_rows] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
+                    __syncwarp();
                 }
             }
+            __syncwarp();
+            if (lane == 0)
+                done_with();
+            ++reader.count;
             if (!two) {  // both have read both accumulators and (m, l)
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0)
-                    ptx::mbar_arrive(ptx::smem_u32(&sh.ml_done));
-                if (!wait_all(ptx::smem_u32(&sh.ml_done), joins & 1u)) {
-                    aborted = true;
+                    ptx::mbar_arrive(ml_done);
+                if (!warp_wait(ml_done, joins & 1u, &sh.abort))
                     break;
-                }
                 ++joins;
             }
         }
     } else {
-                if (warp == kWarpTma) {
-            // ------------------------------------------------------------ copies
+        ptx::regs_dec<88>();
+        if (warp == kWarpPlan) {
+            plan(a, sh, lane, ok);
+        } else if (warp == kWarpTma) {
+            // -------------------------------------------------------- copies
             constexpr int kHalves = DP / 64;
-            int64_t issued = 0;  // ring slots filled so far
-            uint32_t parts = 0;  // parts of tasks whose Q was loaded
+            uint32_t issued = 0;  // ring slots filled so far; the next one and its phase:
+            int slot = 0;
+            uint32_t phase = 0;
+            uint32_t parts = 0;  // parts whose Q was loaded
             bool aborted = false;
             const int box = lane / kHalves, half = lane % kHalves;  // this lane's copy of a slot tile
-            while (!aborted && w.next(a)) {
-                const int32_t n = w.loads();
+            while (!aborted && __all_sync(0xffffffffu, next_part())) {
+                const Part part = sh.parts[reader.slot()];
+                __syncwarp();
+                if (lane == 0)
+                    done_with();
+                ++reader.count;
+                const int32_t n = part.n;
                 if (n == 0)
                     continue;
-                const bool two = w.t.two;
+                const bool two = (part.flags & kTwo) != 0;
+                // Page numbers: 32 consecutive table entries in the lanes, and the 32 behind them on their way.
+                const int32_t last_entry = (part.kv_end - 1) / a.b.page_size;
+                int32_t window = (part.j0 * kTileN) / a.b.page_size;  // first entry of `near`
+                auto entries = [&](int32_t e0) {
+                    const int32_t e = e0 + lane;
+                    return e <= last_entry ? load_page(a.b, part.seq, e, ok) : -1;
+                };
+                int32_t before = -1, near = entries(window), ahead = entries(window + 32);
                 // Q: the part's one or two tiles
-                if (!__all_sync(0xffffffffu, wait_bounded(q_empty, (parts & 1u) ^ 1u, &sh.abort))) {
+                if (!warp_wait(q_empty, (parts & 1u) ^ 1u, &sh.abort)) {
                     aborted = true;
                     break;
                 }
@@ -611,56 +653,51 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 if (lane < kHalves * (two ? 2 : 1)) {
                     const int tile = lane / kHalves, h = lane % kHalves;
                     ptx::tma_load_3d(sq + (uint32_t)tile * C::kTileBytes + (uint32_t)h * kHalfBytes, &tmQ, q_full, h * 64,
-                                     w.kv_head * a.group, w.q.start + (2 * w.task_pair() + tile) * a.positions);
+                                     part.kv_head * a.group, part.q.start + part.i0 + tile * a.positions);
                 }
                 ++parts;
                 // K and V, in the order in which the MMAs take them: K runs `lead` tiles ahead of V
                 const int lead = two ? 1 : 2;
-                // Page numbers: 32 consecutive table entries in the lanes, and the 32 behind them on their way.
-                const int32_t last_entry = (w.t.kv_end - 1) / a.b.page_size;
-                int32_t window = (w.j0 * kTileN) / a.b.page_size;  // first entry of `near`
-                auto entries = [&](int32_t e0) {
-                    const int32_t e = e0 + lane;
-                    return e <= last_entry ? load_page(a.b, w.seq, e, ok) : -1;
-                };
-                int32_t before = -1, near = entries(window), next = entries(window + 32);
                 auto copy = [&](const CUtensorMap *m, int32_t j) -> bool {
-                    const int s = (int)(issued % C::kSlots);
-                    const uint32_t phase = (uint32_t)(issued / C::kSlots) & 1u;
                     const int32_t first = j * kTileN;
-                    const int32_t boxes = min(a.boxes, (w.t.kv_end - first + a.box_rows - 1) / a.box_rows);
+                    const int32_t boxes = min(a.boxes, (part.kv_end - first + a.box_rows - 1) / a.box_rows);
                     const int32_t at = first + box * a.box_rows;  // this lane's first slot
                     const int32_t entry = at / a.b.page_size;
                     const int32_t e = entry - window;
-                    // entries of this tile lie in `before` (V behind K), `near` or `next`
+                    // entries of this tile lie in `before` (V behind K), `near` or `ahead`
                     const int32_t p0 = __shfl_sync(0xffffffffu, before, e & 31), p1 = __shfl_sync(0xffffffffu, near, e & 31),
-                                  p2 = __shfl_sync(0xffffffffu, next, e & 31);
+                                  p2 = __shfl_sync(0xffffffffu, ahead, e & 31);
                     int32_t page = e < 0 ? p0 : (e < 32 ? p1 : p2);
-                    if (!__all_sync(0xffffffffu, wait_bounded(empty(s), phase ^ 1u, &sh.abort)))
+                    if (!warp_wait(empty(slot), phase ^ 1u, &sh.abort))
                         return false;
                     if (lane == 0)
-                        ptx::mbar_arrive_expect_tx(full(s), (uint32_t)(boxes * kHalves * a.box_rows) * 128u);
+                        ptx::mbar_arrive_expect_tx(full(slot), (uint32_t)(boxes * kHalves * a.box_rows) * 128u);
                     __syncwarp();
                     if (box < boxes) {
                         if (page < 0)
                             page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
-                        ptx::tma_load_4d(slot_addr(s) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u, m,
-                                         full(s), half * 64, at - entry * a.b.page_size, w.kv_head, page);
+                        ptx::tma_load_4d(slot_addr(slot) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u, m,
+                                         full(slot), half * 64, at - entry * a.b.page_size, part.kv_head, page);
                     }
+                    __syncwarp();
                     ++issued;
+                    if (++slot == C::kSlots) {
+                        slot = 0;
+                        phase ^= 1u;
+                    }
                     return true;
                 };
-                for (int32_t i = -lead; i < n && !aborted; ++i) {
-                    if (i >= 0 && !copy(&tmV, w.j0 + i))
+                for (int32_t t = -lead; t < n && !aborted; ++t) {
+                    if (t >= 0 && !copy(&tmV, part.j0 + t))
                         aborted = true;
-                    if (!aborted && i + lead < n) {
-                        const int32_t j = w.j0 + i + lead;
-                        const int32_t e_last = (min(w.t.kv_end, (j + 1) * kTileN) - 1) / a.b.page_size;
+                    if (!aborted && t + lead < n) {
+                        const int32_t j = part.j0 + t + lead;
+                        const int32_t e_last = (min(part.kv_end, (j + 1) * kTileN) - 1) / a.b.page_size;
                         if (e_last - window >= 48) {  // V, up to 3 tiles (24 entries) behind, stays within `before`
                             before = near;
-                            near = next;
+                            near = ahead;
                             window += 32;
-                            next = entries(window + 32);
+                            ahead = entries(window + 32);
                         }
                         if (!copy(&tmK, j))
                             aborted = true;
@@ -670,30 +707,33 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             if (aborted && lane == 0) {  // copies already issued land before the shared memory goes away
                 if (parts > 0)
                     wait_drain(q_full, (parts - 1) & 1u);
-                for (int s = 0; s < C::kSlots && s < issued; ++s)
-                    wait_drain(full(s), (uint32_t)((issued - 1 - s) / C::kSlots) & 1u);
+                for (uint32_t s = 0; s < (uint32_t)C::kSlots && s < issued; ++s)
+                    wait_drain(full((int)s), ((issued - 1 - s) / C::kSlots) & 1u);
             }
             __syncwarp();
         } else if (warp == kWarpMma) {
-            // ------------------------------------------------------------ MMAs, issued by one thread
+            // -------------------------------------------------------- MMAs, issued by one thread
             if (ptx::elect_one()) {
                 const uint32_t id_s = ptx::idesc_f16_f32(kTileM, kTileN, kBf16, false);
                 const uint32_t id_o = ptx::idesc_f16_f32(kTileM, DP, kBf16, true);
-                int64_t taken = 0;  // ring slots taken so far
+                int slot = 0, next_slot = 0;  // ring slot taken last, and the next with its phase
+                uint32_t phase = 0;
                 uint32_t parts = 0, n_zeroed = 0;
-                uint32_t n_p[2] = {0, 0};  // slot tiles of each warpgroup whose P V was issued
+                uint32_t n_p0 = 0, n_p1 = 0;  // slot tiles of each warpgroup whose weights were taken
                 bool aborted = false;
-                int slot = 0;
                 auto take = [&]() -> bool {  // the next ring slot has landed
-                    slot = (int)(taken % C::kSlots);
-                    const bool good = wait_bounded(full(slot), (uint32_t)(taken / C::kSlots) & 1u, &sh.abort);
-                    ++taken;
+                    slot = next_slot;
+                    const bool good = wait_bounded(full(slot), phase, &sh.abort);
+                    if (++next_slot == C::kSlots) {
+                        next_slot = 0;
+                        phase ^= 1u;
+                    }
                     return good;
                 };
                 auto scores = [&](int g, int qt, int ks) {  // S_g = Q_qt K^T
                     const uint64_t da = ptx::sdesc_kmajor_sw128(sq + (uint32_t)qt * C::kTileBytes);
                     const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks));
-    #pragma unroll
+#pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
                         const uint64_t off = (uint64_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
                         ptx::mma_bf16(tmem + kTmemS + (uint32_t)g * kTileN, da + off, db + off, id_s, k != 0);
@@ -702,37 +742,39 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 };
                 auto values = [&](int g, int vs, bool add) {  // O_g (+)= P_g V
                     const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), kHalfBytes);
-    #pragma unroll
+#pragma unroll
                     for (int k = 0; k < kTileN / 16; ++k)
                         ptx::mma_f16_ts(tmem + kTmemO + (uint32_t)(g * DP), tmem + kTmemS + (uint32_t)(g * kTileN + k * 8),
                                         db + (uint64_t)(k * (2048 >> 4)), id_o, (add || k != 0) ? 1u : 0u);
                     ptx::mma_commit(o_done(g));
                 };
                 auto weights = [&](int g) -> bool {  // P_g is in tensor memory
-                    const bool good = wait_bounded(p_ready(g), n_p[g] & 1u, &sh.abort);
-                    ++n_p[g];
+                    uint32_t &count = g ? n_p1 : n_p0;
+                    const bool good = wait_bounded(p_ready(g), count & 1u, &sh.abort);
+                    ++count;
                     ptx::tc_fence_after();
                     return good;
                 };
-                while (!aborted && w.next(a)) {
-                    const int32_t n = w.loads();
+                while (!aborted && next_part()) {
+                    const int32_t n = sh.parts[reader.slot()].n, flags = sh.parts[reader.slot()].flags;
+                    done_with();
+                    ++reader.count;
                     if (n == 0)
                         continue;
-                    const bool two = w.t.two;
+                    const bool two = (flags & kTwo) != 0;
                     const int lead = two ? 1 : 2;
                     if (!wait_bounded(q_full, parts & 1u, &sh.abort)) {
                         aborted = true;
                         break;
                     }
                     ++parts;
-                    for (int32_t i = -lead; i < n && !aborted; ++i) {
-                        const bool last = i + lead == n - 1;
-                        const int g = two ? 0 : (i & 1);
+                    for (int32_t t = -lead; t < n; ++t) {
+                        const int g = two ? 0 : (t & 1);
                         int vs = 0;
-                        if (i >= 0) {
+                        if (t >= 0) {
                             bool good = take();
                             vs = slot;
-                            const bool zeros = i == n - 1 && w.tail();
+                            const bool zeros = t == n - 1 && (flags & kTail) != 0;
                             if (good && zeros)
                                 ptx::mbar_arrive(tail);
                             good = good && weights(g);
@@ -742,12 +784,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                                 aborted = true;
                                 break;
                             }
-                            values(g, vs, i >= lead);
+                            values(g, vs, t >= lead);
                             if (!two)
                                 ptx::mma_commit(empty(vs));
                         }
                         int ks = -1;
-                        if (i + lead < n) {
+                        if (t + lead < n) {
                             if (!take()) {
                                 aborted = true;
                                 break;
@@ -755,19 +797,19 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             ks = slot;
                             scores(g, 0, ks);
                         }
-                        if (two && i >= 0) {
+                        if (two && t >= 0) {
                             if (!weights(1)) {
                                 aborted = true;
                                 break;
                             }
-                            values(1, vs, i > 0);
+                            values(1, vs, t > 0);
                             ptx::mma_commit(empty(vs));
                         }
                         if (ks >= 0) {
                             if (two)
                                 scores(1, 1, ks);
                             ptx::mma_commit(empty(ks));
-                            if (last)
+                            if (t + lead == n - 1)
                                 ptx::mma_commit(q_empty);
                         }
                     }
@@ -776,31 +818,35 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 wait_drain(mma_done, 0);
             }
             __syncwarp();
-        } else if (warp == kWarpTail) {
-            // ------------------------------------------------------------ zeros behind the last slot
+        } else {
+            // -------------------------------------------------------- zeros behind the last slot
             // V of slots that no row sees may be anything, and P = 0 times NaN is not 0.
-            int64_t before = 0;  // ring slots of earlier parts
-                uint32_t tails = 0;
-            bool aborted = false;
-            while (!aborted && w.next(a)) {
-                const int32_t n = w.loads();
+            uint32_t before = 0;  // ring slots of earlier parts, modulo kSlots, and their phase
+            uint32_t wraps = 0, tails = 0;
+            while (__all_sync(0xffffffffu, next_part())) {
+                const int32_t n = sh.parts[reader.slot()].n, flags = sh.parts[reader.slot()].flags;
+                const int32_t kv_end = sh.parts[reader.slot()].kv_end;
+                __syncwarp();
+                if (lane == 0)
+                    done_with();
+                ++reader.count;
                 if (n == 0)
                     continue;
-                before += 2 * n;
-                if (!w.tail())
+                before += 2u * (uint32_t)n;
+                wraps += before / C::kSlots;
+                before %= C::kSlots;
+                if ((flags & kTail) == 0)
                     continue;
-                const int64_t at = before - 1;  // V of the last tile is the part's last slot
-                const int s = (int)(at % C::kSlots);
+                // V of the last tile is the part's last slot
+                const int s = before > 0 ? (int)before - 1 : C::kSlots - 1;
+                const uint32_t phase = (before > 0 ? wraps : wraps - 1u) & 1u;
                 // full(s) alone would not do: it may still be in an earlier phase of the same parity
-            aborted = !wait_bounded(tail, tails++ & 1u, &sh.abort) ||
-                      !wait_bounded(full(s), (uint32_t)(at / C::kSlots) & 1u, &sh.abort);
-                aborted = __any_sync(0xffffffffu, aborted);
-                if (aborted)
+                if (!warp_wait(tail, tails++ & 1u, &sh.abort) || !warp_wait(full(s), phase, &sh.abort))
                     break;
-                const int first = w.t.kv_end & (kTileN - 1);
+                const int first = kv_end & (kTileN - 1);
                 uint8_t *const v = smem_raw + (slot_addr(s) - raw);
                 for (int x = first * 8 + lane; x < kTileN * 8; x += 32)
-    #pragma unroll
+#pragma unroll
                     for (int h = 0; h < DP / 64; ++h)
                         *reinterpret_cast<uint4 *>(v + h * kHalfBytes + x * 16) = make_uint4(0, 0, 0, 0);
                 ptx::fence_proxy_async();
@@ -989,7 +1035,8 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.positions = positions_per_tile(b);
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
-    a.min_units = 2;
+    a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
+    a.min_units = kTaskCost + 2;
     CUtensorMap tq, tk, tv;
     const int64_t q_dims[3] = {b.head_dim, b.n_q_heads, b.n_rows}, q_strides[3] = {1, q.head_stride, q.row_stride};
     const int32_t q_box[3] = {64, a.group, a.positions};
