@@ -12,10 +12,10 @@
 // lengths that are read on the device; a run that starts or ends inside a task leaves its (m, l, O) in the workspace, and
 // combine_kernel joins the runs of such tasks in the order of the slots.
 //
-// A CTA has 12 warps: two softmax warpgroups (one thread per row), and one warp each for the copies (TMA, one box per
-// page and 64 dims), the MMAs, and the zeros behind the last slot.  S lies in tensor memory, 128 columns per warpgroup;
+// A CTA has 12 warps: two softmax warpgroups (one thread per row), and one warp each for the plan, the copies of Q and K,
+// the copies of V (TMA, one box per page and 64 dims), and the MMAs.  S lies in tensor memory, 128 columns per warpgroup;
 // P overwrites it as 16-bit pairs, from where it is the A operand of P V; O lies beside it, DP columns per warpgroup.
-// K and V tiles go through one ring of shared-memory slots in the order in which the MMAs need them.
+// K and V tiles go through a ring of shared-memory slots each.
 //
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
 // 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  m follows
@@ -38,7 +38,7 @@ namespace {
 constexpr int kTileM = 128, kTileN = 128;  // rows and slots of a tile
 constexpr int kSoftmaxThreads = 256;
 constexpr int kAttendThreads = kSoftmaxThreads + 128;
-constexpr int kWarpTma = 8, kWarpMma = 9, kWarpTail = 10, kWarpPlan = 11;
+constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11;
 constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kRecordBytes = 32;        // SplitRecord
 constexpr int kCombineRows = 32;        // rows per combine CTA
@@ -71,6 +71,7 @@ struct AttendArgs {
     uint32_t pair_magic;       // ceil(2^32 / (2 positions))
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
     int32_t min_units;         // a CTA's run is at least this long
+    int32_t wide;              // units may need 64 bits
 };
 
 // Tasks of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256, so that the product with
@@ -88,25 +89,23 @@ __device__ __forceinline__ int32_t task_slots(const AttendArgs &a, const SeqRows
 
 __device__ __forceinline__ int32_t tiles_of(int32_t slots) { return max(1, (slots + kTileN - 1) / kTileN); }
 
-// The cut of `total` units into n runs: the first `more` of them are one unit longer.
+// The cut of `total` units into n runs: the first `more` of them are one unit longer.  U: 32 bits unless the host finds
+// that the units may need more (64-bit arithmetic, divisions above all, is slow and much code).
+template <typename U>
 struct Cut {
-    int64_t total, per, more;
+    U per, more;
     int32_t n;
-    __device__ __forceinline__ Cut(int64_t t, int32_t ctas, int32_t min_units) : total(t)
+    __device__ __forceinline__ Cut(U total, int32_t ctas, U min_units)
     {
-        n = (int32_t)min((int64_t)ctas, max((int64_t)1, quotient(t, min_units)));
-        per = quotient(t, n);
-        more = t - per * n;
+        n = (int32_t)min((U)ctas, max((U)1, total / min_units));
+        per = total / (U)n;
+        more = total - per * (U)n;
     }
-    __device__ __forceinline__ int64_t start(int64_t c) const { return c * per + min(c, more); }
-    __device__ __forceinline__ int32_t run_of(int64_t unit) const
+    __device__ __forceinline__ U start(int32_t c) const { return (U)c * per + min((U)c, more); }
+    __device__ __forceinline__ int32_t run_of(U unit) const
     {
-        const int64_t longer = more * (per + 1);
-        return (int32_t)(unit < longer ? quotient(unit, per + 1) : more + quotient(unit - longer, per));
-    }
-    static __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)  // 64-bit division is slow
-    {
-        return ((x | y) >> 31) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+        const U longer = more * (per + 1);
+        return (int32_t)(unit < longer ? unit / (per + 1) : more + (unit - longer) / per);
     }
 };
 
@@ -126,7 +125,9 @@ struct alignas(16) Part {
 template <int DP>
 struct Config {
     static constexpr uint32_t kTileBytes = (DP / 64) * kHalfBytes;  // 128 rows or slots
-    static constexpr int kSlots = DP == 128 ? 5 : 12;               // ring slots beside the two Q tiles
+    // Ring slots of K and of V, beside the two Q tiles.  V waits for its weights, K for nothing.
+    static constexpr int kSlotsK = DP == 128 ? 2 : 5, kSlotsV = DP == 128 ? 3 : 7;
+    static constexpr int kSlots = kSlotsK + kSlotsV;
     static constexpr uint32_t kRing = kSlots * kTileBytes;
     static constexpr uint32_t kShared = 3072;
     static constexpr uint32_t kSmem = 2 * kTileBytes + kRing + kShared;
@@ -138,7 +139,7 @@ struct alignas(16) Shared {
     uint64_t q_full, q_empty;
     uint64_t full[12], empty[12];
     uint64_t s_full[2], p_ready[2], o_done[2];
-    uint64_t tail, zeroed;  // V of a part's last tile has landed; the slots behind the last one hold zeros
+    uint64_t zeroed[12];  // per ring slot of V: the cache slots behind the last one hold zeros
     uint64_t ml_ready, ml_done;
     uint64_t mma_done;
     uint32_t tmem;
@@ -171,16 +172,38 @@ struct PartReader {
     __device__ __forceinline__ int slot() const { return (int)(count % kParts); }
 };
 
-// The planning warp: cuts the work and hands this CTA's run out part by part.
-__device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, bool &ok)
+template <typename U>
+__device__ __forceinline__ U warp_sum(U x, int width)  // over groups of `width` lanes
+{
+    for (int i = width >> 1; i; i >>= 1)
+        x += __shfl_xor_sync(0xffffffffu, x, i);
+    return x;
+}
+
+template <typename U>
+__device__ __forceinline__ U warp_scan(U x, int lane)  // inclusive
+{
+#pragma unroll
+    for (int i = 1; i < 32; i <<= 1) {
+        const U up = __shfl_up_sync(0xffffffffu, x, i);
+        if (lane >= i)
+            x += up;
+    }
+    return x;
+}
+
+// The planning warp: cuts the work and hands this CTA's run out part by part.  U is unsigned.
+template <typename U>
+__device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
 {
     const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads;
+    bool ok = true;
     int width = 32;  // lanes per sequence
     while (width > 1 && n_seq * width > 32)
         width >>= 1;
     const int per_round = 32 / width, sub = lane & (width - 1);
     SeqRows q;
-    int64_t mine = 0;  // units of this lane's sequence
+    U mine = 0;  // units of this lane's sequence, of one kv head
     auto load_round = [&](int32_t s0) {
         const int32_t s = s0 + lane / width;
         q.n = 0;
@@ -188,49 +211,43 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, 
         if (s < n_seq)
             q = load_seq(a.b, s);
         ok = ok && q.ok;
-        int64_t u = 0;
+        U u = 0;
         const int32_t n_pairs = q.n > 0 ? pairs_of(a, q) : 0;
+#pragma unroll 1
         for (int32_t p = sub; p < n_pairs; p += width)
-            u += tiles_of(task_slots(a, q, p)) + kTaskCost;
-        for (int i = width >> 1; i; i >>= 1)
-            u += __shfl_xor_sync(0xffffffffu, u, i);
-        mine = u * n_kv;
+            u += (U)(tiles_of(task_slots(a, q, p)) + kTaskCost);
+        mine = warp_sum(u, width);
     };
-    int64_t total = 0;
+    U total = 0;
+#pragma unroll 1
     for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
         load_round(s0);
-        int64_t u = sub == 0 ? mine : 0;
-        for (int i = 16; i; i >>= 1)
-            u += __shfl_xor_sync(0xffffffffu, u, i);
-        total += u;
+        total += warp_sum(sub == 0 ? mine : (U)0, 32);
     }
-    const Cut cut(total, (int32_t)gridDim.x, a.min_units);
+    total *= (U)n_kv;
+    const Cut<U> cut(total, (int32_t)gridDim.x, (U)a.min_units);
     const int32_t c = (int32_t)blockIdx.x;
-    int64_t at = cut.start(c);  // the next unit to hand out
-    const int64_t end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
+    U at = cut.start(c);  // the next unit to hand out
+    const U end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
     SplitRecord rec{};
-    int32_t seq = 0, kv_head = 0, pair = 0;
-    int64_t task = 0;  // the unit at which the current task starts
+    int32_t seq = 0, kv_head = 0, pair = 0, n_pairs = 0;
+    U task = 0;  // the unit at which the current task starts
     uint32_t sent = 0;
     bool go = at < end;
     if (go) {
         // the sequence that holds unit `at`
-        int64_t before = 0;
+        U before = 0;
+#pragma unroll 1
         for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
             if (n_seq > per_round)
                 load_round(s0);
-            int64_t pre = sub == 0 ? mine : 0;
-            for (int i = 1; i < 32; i <<= 1) {
-                const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
-                if (lane >= i)
-                    pre += up;
-            }
+            const U pre = warp_scan(sub == 0 ? mine * (U)n_kv : (U)0, lane);
             const unsigned hit = __ballot_sync(0xffffffffu, before + pre > at);
             if (hit) {
                 const int src = __ffs(hit) - 1;  // a sequence's first lane: `pre` grows there only
                 seq = s0 + src / width;
-                task = before + __shfl_sync(0xffffffffu, pre, src) - __shfl_sync(0xffffffffu, mine, src);
                 mine = __shfl_sync(0xffffffffu, mine, src);
+                task = before + __shfl_sync(0xffffffffu, pre, src) - mine * (U)n_kv;
                 q.start = __shfl_sync(0xffffffffu, q.start, src);
                 q.n = __shfl_sync(0xffffffffu, q.n, src);
                 q.kv = __shfl_sync(0xffffffffu, q.kv, src);
@@ -240,55 +257,42 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, 
             before += __shfl_sync(0xffffffffu, pre, 31);
         }
         // its kv head, and by the sum over 32 tasks at a time the task
-        const int64_t head = Cut::quotient(mine, n_kv);
-        kv_head = (int32_t)Cut::quotient(at - task, head);
-        task += kv_head * head;
-        const int32_t n_pairs = pairs_of(a, q);
+        kv_head = (int32_t)((at - task) / mine);
+        task += (U)kv_head * mine;
+        n_pairs = pairs_of(a, q);
+#pragma unroll 1
         for (int32_t p0 = 0; p0 < n_pairs; p0 += 32) {
             const int32_t p = p0 + lane;
-            const int64_t cost = p < n_pairs ? tiles_of(task_slots(a, q, p)) + kTaskCost : 0;
-            int64_t pre = cost;
-            for (int i = 1; i < 32; i <<= 1) {
-                const int64_t up = __shfl_up_sync(0xffffffffu, pre, i);
-                if (lane >= i)
-                    pre += up;
-            }
+            const U cost = p < n_pairs ? (U)(tiles_of(task_slots(a, q, p)) + kTaskCost) : (U)0;
+            const U pre = warp_scan(cost, lane);
             const unsigned hit = __ballot_sync(0xffffffffu, task + pre > at);
             if (hit) {
                 const int src = __ffs(hit) - 1;
                 pair = p0 + src;
-                task += __shfl_sync(0xffffffffu, pre, src) - __shfl_sync(0xffffffffu, cost, src);
+                task += __shfl_sync(0xffffffffu, pre - cost, src);
                 break;
             }
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
-        const int32_t tiles = tiles_of(task_slots(a, q, pair));
-        rec.valid = at - task > kTaskCost;
-        rec.seq = seq;
-        rec.kv_head = kv_head;
-        rec.pair = pair;
-        rec.first = cut.run_of(task + kTaskCost);
-        rec.last = cut.run_of(task + kTaskCost + tiles - 1);
     }
-    if (lane == 0)
-        a.records[c] = rec;
-    int32_t n_pairs = go ? pairs_of(a, q) : 0;
+    const bool starts = go;
+    U first_task = task;
+#pragma unroll 1
     while (true) {
         Part part;
         part.flags = kEnd;
         part.kv_end = part.j0 = part.n = part.i0 = part.pad = 0;
         if (go) {
             const int32_t slots = task_slots(a, q, pair), tiles = tiles_of(slots);
-            // a task's own cost comes before its tiles
-            const int64_t t0 = at - task - kTaskCost, t1 = end - task - kTaskCost;
-            part.j0 = (int32_t)max((int64_t)0, t0);
-            part.n = (int32_t)min((int64_t)tiles, t1) - part.j0;
+            const U tile0 = task + kTaskCost;  // a task's own cost comes before its tiles
+            part.j0 = at > tile0 ? (int32_t)(at - tile0) : 0;
+            part.n = (end > tile0 ? (int32_t)min((U)tiles, end - tile0) : 0) - part.j0;
             part.kv_end = slots;
             part.i0 = pair * 2 * a.positions;
             const bool to_end = part.j0 + part.n == tiles;
             part.flags = (q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
-            task += tiles + kTaskCost;
+            task = tile0 + (U)tiles;
             at = task;
             go = at < end;
         }
@@ -301,15 +305,31 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, 
                 part.n = 0;
             const int slot = (int)(sent % kParts);
             if (!warp_wait(ptx::smem_u32(&sh.part_empty[slot]), ((sent / kParts) & 1u) ^ 1u, &sh.abort))
-                return;
+                break;
             if (lane == 0) {
                 sh.parts[slot] = part;
                 ptx::mbar_arrive(ptx::smem_u32(&sh.part_full[slot]));
             }
+            __syncwarp();
+            if (sent == 0) {  // behind the first part: nobody in this kernel waits for the record
+                if (starts) {
+                    const U tile0 = first_task + kTaskCost;
+                    rec.valid = part.j0 > 0;
+                    rec.seq = seq;
+                    rec.kv_head = kv_head;
+                    rec.pair = pair;
+                    if (rec.valid) {
+                        rec.first = cut.run_of(tile0);
+                        rec.last = cut.run_of(tile0 + (U)tiles_of(part.kv_end) - 1);
+                    }
+                }
+                if (lane == 0)
+                    a.records[c] = rec;
+            }
             ++sent;
         }
         if (last)
-            return;
+            break;
         if (go && ++pair == n_pairs) {
             pair = 0;
             if (++kv_head == n_kv) {
@@ -325,6 +345,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane, 
             }
         }
     }
+    if (!ok)
+        atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
 }
 
 template <int DP, bool kBf16>
@@ -340,13 +362,13 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     auto full = [&](int s) { return ptx::smem_u32(&sh.full[s]); };
     auto empty = [&](int s) { return ptx::smem_u32(&sh.empty[s]); };
+    auto zeroed = [&](int s) { return ptx::smem_u32(&sh.zeroed[s]); };
     auto s_full = [&](int g) { return ptx::smem_u32(&sh.s_full[g]); };
     auto p_ready = [&](int g) { return ptx::smem_u32(&sh.p_ready[g]); };
     auto o_done = [&](int g) { return ptx::smem_u32(&sh.o_done[g]); };
     auto part_full = [&](int s) { return ptx::smem_u32(&sh.part_full[s]); };
     auto part_empty = [&](int s) { return ptx::smem_u32(&sh.part_empty[s]); };
     const uint32_t q_full = ptx::smem_u32(&sh.q_full), q_empty = ptx::smem_u32(&sh.q_empty);
-    const uint32_t tail = ptx::smem_u32(&sh.tail), zeroed = ptx::smem_u32(&sh.zeroed);
     const uint32_t ml_ready = ptx::smem_u32(&sh.ml_ready), ml_done = ptx::smem_u32(&sh.ml_done);
     const uint32_t mma_done = ptx::smem_u32(&sh.mma_done);
     auto slot_addr = [&](int s) { return ring + (uint32_t)s * C::kTileBytes; };
@@ -354,28 +376,27 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < kParts; ++s) {
             ptx::mbar_init(part_full(s), 1);
-            ptx::mbar_init(part_empty(s), 11);  // 8 softmax warps, copies, MMAs, zeros
+            ptx::mbar_init(part_empty(s), 11);  // 8 softmax warps, 2 for the copies, MMAs
         }
         ptx::mbar_init(q_full, 1);
         ptx::mbar_init(q_empty, 1);
         for (int s = 0; s < C::kSlots; ++s) {
             ptx::mbar_init(full(s), 1);
             ptx::mbar_init(empty(s), 1);
+            ptx::mbar_init(zeroed(s), 1);
         }
         for (int g = 0; g < 2; ++g) {
             ptx::mbar_init(s_full(g), 1);
             ptx::mbar_init(p_ready(g), 4);
             ptx::mbar_init(o_done(g), 1);
         }
-        ptx::mbar_init(tail, 1);
-        ptx::mbar_init(zeroed, 1);
         ptx::mbar_init(ml_ready, 8);
         ptx::mbar_init(ml_done, 8);
         ptx::mbar_init(mma_done, 1);
         sh.abort = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == kWarpTma && lane == 0) {
+    if (warp == kWarpK && lane == 0) {
         ptx::prefetch_tensormap(&tmQ);
         ptx::prefetch_tensormap(&tmK);
         ptx::prefetch_tensormap(&tmV);
@@ -614,14 +635,22 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     } else {
         ptx::regs_dec<88>();
         if (warp == kWarpPlan) {
-            plan(a, sh, lane, ok);
-        } else if (warp == kWarpTma) {
-            // -------------------------------------------------------- copies
+            if (a.wide)
+                plan<uint64_t>(a, sh, lane);
+            else
+                plan<uint32_t>(a, sh, lane);
+        } else if (warp == kWarpK || warp == kWarpV) {
+            // -------------------------------------------------------- copies of Q and K, and of V
+            // The issue of small boxes bounds a warp (68 clocks per box of 16 slots x 64 dims from 16 lanes, 174 from one
+            // lane; two warps 39), so there are two, each with a ring of its own.
             constexpr int kHalves = DP / 64;
-            uint32_t issued = 0;  // ring slots filled so far; the next one and its phase:
-            int slot = 0;
+            const bool is_v = warp == kWarpV;
+            const CUtensorMap *const map = is_v ? &tmV : &tmK;
+            const int slot0 = is_v ? C::kSlotsK : 0, slot1 = is_v ? C::kSlots : C::kSlotsK;
+            int slot = slot0;  // the next to fill, and its phase
             uint32_t phase = 0;
-            uint32_t parts = 0;  // parts whose Q was loaded
+            uint32_t issued = 0;  // slots filled so far
+            uint32_t parts = 0;   // parts whose Q was loaded
             bool aborted = false;
             const int box = lane / kHalves, half = lane % kHalves;  // this lane's copy of a slot tile
             while (!aborted && __all_sync(0xffffffffu, next_part())) {
@@ -641,74 +670,76 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     const int32_t e = e0 + lane;
                     return e <= last_entry ? load_page(a.b, part.seq, e, ok) : -1;
                 };
-                int32_t before = -1, near = entries(window), ahead = entries(window + 32);
-                // Q: the part's one or two tiles
-                if (!warp_wait(q_empty, (parts & 1u) ^ 1u, &sh.abort)) {
-                    aborted = true;
-                    break;
+                int32_t near = entries(window), ahead = entries(window + 32);
+                if (!is_v) {  // Q: the part's one or two tiles
+                    if (!warp_wait(q_empty, (parts & 1u) ^ 1u, &sh.abort)) {
+                        aborted = true;
+                        break;
+                    }
+                    if (lane == 0)
+                        ptx::mbar_arrive_expect_tx(q_full,
+                                                   (uint32_t)(two ? 2 : 1) * kHalves * (uint32_t)(a.positions * a.group) * 128u);
+                    __syncwarp();
+                    if (lane < kHalves * (two ? 2 : 1)) {
+                        const int tile = lane / kHalves, h = lane % kHalves;
+                        ptx::tma_load_3d(sq + (uint32_t)tile * C::kTileBytes + (uint32_t)h * kHalfBytes, &tmQ, q_full, h * 64,
+                                         part.kv_head * a.group, part.q.start + part.i0 + tile * a.positions);
+                    }
+                    ++parts;
                 }
-                if (lane == 0)
-                    ptx::mbar_arrive_expect_tx(q_full, (uint32_t)(two ? 2 : 1) * kHalves * (uint32_t)(a.positions * a.group) * 128u);
-                __syncwarp();
-                if (lane < kHalves * (two ? 2 : 1)) {
-                    const int tile = lane / kHalves, h = lane % kHalves;
-                    ptx::tma_load_3d(sq + (uint32_t)tile * C::kTileBytes + (uint32_t)h * kHalfBytes, &tmQ, q_full, h * 64,
-                                     part.kv_head * a.group, part.q.start + part.i0 + tile * a.positions);
-                }
-                ++parts;
-                // K and V, in the order in which the MMAs take them: K runs `lead` tiles ahead of V
-                const int lead = two ? 1 : 2;
-                auto copy = [&](const CUtensorMap *m, int32_t j) -> bool {
-                    const int32_t first = j * kTileN;
+                for (int32_t t = 0; t < n; ++t) {
+                    const int32_t first = (part.j0 + t) * kTileN;
                     const int32_t boxes = min(a.boxes, (part.kv_end - first + a.box_rows - 1) / a.box_rows);
                     const int32_t at = first + box * a.box_rows;  // this lane's first slot
                     const int32_t entry = at / a.b.page_size;
-                    const int32_t e = entry - window;
-                    // entries of this tile lie in `before` (V behind K), `near` or `ahead`
-                    const int32_t p0 = __shfl_sync(0xffffffffu, before, e & 31), p1 = __shfl_sync(0xffffffffu, near, e & 31),
-                                  p2 = __shfl_sync(0xffffffffu, ahead, e & 31);
-                    int32_t page = e < 0 ? p0 : (e < 32 ? p1 : p2);
-                    if (!warp_wait(empty(slot), phase ^ 1u, &sh.abort))
-                        return false;
+                    if ((first + boxes * a.box_rows - 1) / a.b.page_size - window >= 32) {  // no tile straddles the border
+                        near = ahead;
+                        window += 32;
+                        ahead = entries(window + 32);
+                    }
+                    int32_t page = __shfl_sync(0xffffffffu, near, (entry - window) & 31);
+                    if (page < 0)
+                        page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
+                    if (!warp_wait(empty(slot), phase ^ 1u, &sh.abort)) {
+                        aborted = true;
+                        break;
+                    }
                     if (lane == 0)
                         ptx::mbar_arrive_expect_tx(full(slot), (uint32_t)(boxes * kHalves * a.box_rows) * 128u);
                     __syncwarp();
-                    if (box < boxes) {
-                        if (page < 0)
-                            page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
-                        ptx::tma_load_4d(slot_addr(slot) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u, m,
-                                         full(slot), half * 64, at - entry * a.b.page_size, part.kv_head, page);
-                    }
+                    if (box < boxes)
+                        ptx::tma_load_4d(slot_addr(slot) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u,
+                                         map, full(slot), half * 64, at - entry * a.b.page_size, part.kv_head, page);
                     __syncwarp();
                     ++issued;
-                    if (++slot == C::kSlots) {
-                        slot = 0;
-                        phase ^= 1u;
-                    }
-                    return true;
-                };
-                for (int32_t t = -lead; t < n && !aborted; ++t) {
-                    if (t >= 0 && !copy(&tmV, part.j0 + t))
-                        aborted = true;
-                    if (!aborted && t + lead < n) {
-                        const int32_t j = part.j0 + t + lead;
-                        const int32_t e_last = (min(part.kv_end, (j + 1) * kTileN) - 1) / a.b.page_size;
-                        if (e_last - window >= 48) {  // V, up to 3 tiles (24 entries) behind, stays within `before`
-                            before = near;
-                            near = ahead;
-                            window += 32;
-                            ahead = entries(window + 32);
-                        }
-                        if (!copy(&tmK, j))
+                    if (is_v && t == n - 1 && (part.flags & kTail) != 0) {
+                        // V of slots that no row sees may be anything, and P = 0 times NaN is not 0: zeros
+                        if (!warp_wait(full(slot), phase, &sh.abort)) {
                             aborted = true;
+                            break;
+                        }
+                        uint8_t *const v = smem_raw + (slot_addr(slot) - raw);
+                        for (int x = (part.kv_end & (kTileN - 1)) * 8 + lane; x < kTileN * 8; x += 32)
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h)
+                                *reinterpret_cast<uint4 *>(v + h * kHalfBytes + x * 16) = make_uint4(0, 0, 0, 0);
+                        ptx::fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0)
+                            ptx::mbar_arrive(zeroed(slot));
+                    }
+                    if (++slot == slot1) {
+                        slot = slot0;
+                        phase ^= 1u;
                     }
                 }
             }
             if (aborted && lane == 0) {  // copies already issued land before the shared memory goes away
                 if (parts > 0)
                     wait_drain(q_full, (parts - 1) & 1u);
-                for (uint32_t s = 0; s < (uint32_t)C::kSlots && s < issued; ++s)
-                    wait_drain(full((int)s), ((issued - 1 - s) / C::kSlots) & 1u);
+                const uint32_t slots = (uint32_t)(slot1 - slot0);
+                for (uint32_t s = 0; s < slots && s < issued; ++s)
+                    wait_drain(full(slot0 + (int)s), ((issued - 1 - s) / slots) & 1u);
             }
             __syncwarp();
         } else if (warp == kWarpMma) {
@@ -716,20 +747,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             if (ptx::elect_one()) {
                 const uint32_t id_s = ptx::idesc_f16_f32(kTileM, kTileN, kBf16, false);
                 const uint32_t id_o = ptx::idesc_f16_f32(kTileM, DP, kBf16, true);
-                int slot = 0, next_slot = 0;  // ring slot taken last, and the next with its phase
-                uint32_t phase = 0;
-                uint32_t parts = 0, n_zeroed = 0;
+                int k_slot = 0, v_slot = C::kSlotsK;  // the next ring slots, and their phases
+                uint32_t k_phase = 0, v_phase = 0;
+                uint32_t parts = 0;
+                uint32_t zero_phases = 0;  // bit s: phase of zeroed(s)
                 uint32_t n_p0 = 0, n_p1 = 0;  // slot tiles of each warpgroup whose weights were taken
                 bool aborted = false;
-                auto take = [&]() -> bool {  // the next ring slot has landed
-                    slot = next_slot;
-                    const bool good = wait_bounded(full(slot), phase, &sh.abort);
-                    if (++next_slot == C::kSlots) {
-                        next_slot = 0;
-                        phase ^= 1u;
-                    }
-                    return good;
-                };
                 auto scores = [&](int g, int qt, int ks) {  // S_g = Q_qt K^T
                     const uint64_t da = ptx::sdesc_kmajor_sw128(sq + (uint32_t)qt * C::kTileBytes);
                     const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks));
@@ -772,14 +795,18 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         const int g = two ? 0 : (t & 1);
                         int vs = 0;
                         if (t >= 0) {
-                            bool good = take();
-                            vs = slot;
+                            vs = v_slot;
+                            bool good = wait_bounded(full(vs), v_phase, &sh.abort);
+                            if (++v_slot == C::kSlots) {
+                                v_slot = C::kSlotsK;
+                                v_phase ^= 1u;
+                            }
                             const bool zeros = t == n - 1 && (flags & kTail) != 0;
-                            if (good && zeros)
-                                ptx::mbar_arrive(tail);
                             good = good && weights(g);
                             if (good && zeros)
-                                good = wait_bounded(zeroed, n_zeroed++ & 1u, &sh.abort);
+                                good = wait_bounded(zeroed(vs), zero_phases >> vs & 1u, &sh.abort);
+                            if (zeros)
+                                zero_phases ^= 1u << vs;
                             if (!good) {
                                 aborted = true;
                                 break;
@@ -790,11 +817,15 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         }
                         int ks = -1;
                         if (t + lead < n) {
-                            if (!take()) {
+                            ks = k_slot;
+                            if (!wait_bounded(full(ks), k_phase, &sh.abort)) {
                                 aborted = true;
                                 break;
                             }
-                            ks = slot;
+                            if (++k_slot == C::kSlotsK) {
+                                k_slot = 0;
+                                k_phase ^= 1u;
+                            }
                             scores(g, 0, ks);
                         }
                         if (two && t >= 0) {
@@ -818,42 +849,6 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 wait_drain(mma_done, 0);
             }
             __syncwarp();
-        } else {
-            // -------------------------------------------------------- zeros behind the last slot
-            // V of slots that no row sees may be anything, and P = 0 times NaN is not 0.
-            uint32_t before = 0;  // ring slots of earlier parts, modulo kSlots, and their phase
-            uint32_t wraps = 0, tails = 0;
-            while (__all_sync(0xffffffffu, next_part())) {
-                const int32_t n = sh.parts[reader.slot()].n, flags = sh.parts[reader.slot()].flags;
-                const int32_t kv_end = sh.parts[reader.slot()].kv_end;
-                __syncwarp();
-                if (lane == 0)
-                    done_with();
-                ++reader.count;
-                if (n == 0)
-                    continue;
-                before += 2u * (uint32_t)n;
-                wraps += before / C::kSlots;
-                before %= C::kSlots;
-                if ((flags & kTail) == 0)
-                    continue;
-                // V of the last tile is the part's last slot
-                const int s = before > 0 ? (int)before - 1 : C::kSlots - 1;
-                const uint32_t phase = (before > 0 ? wraps : wraps - 1u) & 1u;
-                // full(s) alone would not do: it may still be in an earlier phase of the same parity
-                if (!warp_wait(tail, tails++ & 1u, &sh.abort) || !warp_wait(full(s), phase, &sh.abort))
-                    break;
-                const int first = kv_end & (kTileN - 1);
-                uint8_t *const v = smem_raw + (slot_addr(s) - raw);
-                for (int x = first * 8 + lane; x < kTileN * 8; x += 32)
-#pragma unroll
-                    for (int h = 0; h < DP / 64; ++h)
-                        *reinterpret_cast<uint4 *>(v + h * kHalfBytes + x * 16) = make_uint4(0, 0, 0, 0);
-                ptx::fence_proxy_async();
-                __syncwarp();
-                if (lane == 0)
-                    ptx::mbar_arrive(zeroed);
-            }
         }
     }
     if (!ok)
@@ -1037,6 +1032,8 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.boxes = kTileN / a.box_rows;
     a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
     a.min_units = kTaskCost + 2;
+    const int64_t pairs = b.n_rows / (2 * a.positions) + b.n_seq, tiles = (int64_t)b.table_width * b.page_size / kTileN + 1;
+    a.wide = (double)pairs * (double)(tiles + kTaskCost) * b.n_kv_heads >= 2147483648.0;
     CUtensorMap tq, tk, tv;
     const int64_t q_dims[3] = {b.head_dim, b.n_q_heads, b.n_rows}, q_strides[3] = {1, q.head_stride, q.row_stride};
     const int32_t q_box[3] = {64, a.group, a.positions};

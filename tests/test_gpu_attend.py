@@ -245,3 +245,9 @@ def test_large_batch_matches_the_plain_form():
         # score error (130 u S, S below 64 here: |q||k| scale) twice, 2^-21, n u; weights and result rounded
         tol = (2 * 130 * 2.0 ** -24 * 64 + 2.0 ** -21 + kv * 2.0 ** -24) * 2 * size + 1.01 * 2.0 ** -8 * (size + want.abs())
         assert ((got - want).abs() <= tol).all(), s
+
+
+def test_many_short_parts_with_tails():
+    """Parts of one or two slot tiles, each ending inside a tile, several in flight at once in every CTA."""
+    seqs = [(1, 1 + (37 * i) % 250, (37 * i) % 250) for i in range(700)]
+    run(add_rows(make_kv(CAUSAL, seqs, heads=8, kv_heads=8, dim=128)))
