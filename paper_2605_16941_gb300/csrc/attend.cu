@@ -41,7 +41,7 @@ constexpr int kAttendThreads = kSoftmaxThreads + 128;
 constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11;
 constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kRecordBytes = 32;        // SplitRecord
-constexpr int kCombineRows = 32;        // rows per combine CTA
+constexpr int kCombineThreads = 256;
 constexpr int kSplitRows = 2 * kTileM;  // rows of a task
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
 constexpr int kTaskCost = 2;            // what a task costs beside its slot tiles, in slot tiles
@@ -50,11 +50,13 @@ constexpr uint32_t kTmemS = 0, kTmemO = 2 * kTileN, kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 
 // What combine_kernel needs to know of the task that CTA c's run starts inside (one per CTA).
-struct SplitRecord {
-    int32_t valid;  // an earlier run holds slot tiles of it too
-    int32_t seq, kv_head, pair;
-    int32_t first, last;  // CTAs whose runs hold slot tiles of it
-    int32_t pad[2];
+struct alignas(16) SplitRecord {
+    int32_t last;   // CTAs first .. last hold slot tiles of it
+    int32_t first;  // -1: the run does not start inside a task, or no earlier run holds tiles of it
+    int32_t row;    // the task's first row, and its row positions (up to 2 tiles of them)
+    int32_t positions;
+    int32_t kv_head;
+    int32_t pad[3];
 };
 static_assert(sizeof(SplitRecord) == kRecordBytes, "record size");
 
@@ -229,7 +231,6 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
     const int32_t c = (int32_t)blockIdx.x;
     U at = cut.start(c);  // the next unit to hand out
     const U end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
-    SplitRecord rec{};
     int32_t seq = 0, kv_head = 0, pair = 0, n_pairs = 0;
     U task = 0;  // the unit at which the current task starts
     uint32_t sent = 0;
@@ -311,20 +312,18 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
                 ptx::mbar_arrive(ptx::smem_u32(&sh.part_full[slot]));
             }
             __syncwarp();
-            if (sent == 0) {  // behind the first part: nobody in this kernel waits for the record
-                if (starts) {
+            if (sent == 0 && lane == 0) {  // behind the first part: nobody in this kernel waits for the record
+                SplitRecord rec{};
+                rec.first = -1;
+                if (starts && part.j0 > 0) {
                     const U tile0 = first_task + kTaskCost;
-                    rec.valid = part.j0 > 0;
-                    rec.seq = seq;
+                    rec.first = cut.run_of(tile0);
+                    rec.last = cut.run_of(tile0 + (U)tiles_of(part.kv_end) - 1);
+                    rec.row = q.start + part.i0;
+                    rec.positions = q.n - part.i0;
                     rec.kv_head = kv_head;
-                    rec.pair = pair;
-                    if (rec.valid) {
-                        rec.first = cut.run_of(tile0);
-                        rec.last = cut.run_of(tile0 + (U)tiles_of(part.kv_end) - 1);
-                    }
                 }
-                if (lane == 0)
-                    a.records[c] = rec;
+                a.records[c] = rec;
             }
             ++sent;
         }
@@ -862,11 +861,14 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_DEVICE_TIMEOUT);
 }
 
-// Joins the parts of the tasks that the runs' borders cut: CTA (c, y) takes rows 32 y .. of the task in which run c + 1
-// starts, if that is the first border inside it.  Lanes are rows, warps take columns in turn.
-template <int DP, bool kBf16>
-__global__ void __launch_bounds__(128) combine_kernel(const AttendArgs a)
+// Joins the parts of the tasks that the runs' borders cut: CTA (c, y) takes a share of the task in which run c + 1 starts,
+// if that is the first border inside it.  A thread has one row and `chunks` float4 columns; the lanes are rows, as the
+// parts are stored.  Bound by latency (record, then m and l, then O): the loads of several parts are in flight at once.
+template <int DP, bool kBf16, int kChunks>
+__global__ void __launch_bounds__(kCombineThreads) combine_kernel(const AttendArgs a)
 {
+    constexpr int kColumns = kCombineThreads / 32;              // chunk columns of a CTA
+    constexpr int kShares = DP / 4 / (kColumns * kChunks);      // CTAs per 32 rows
     ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
@@ -877,47 +879,52 @@ __global__ void __launch_bounds__(128) combine_kernel(const AttendArgs a)
     if (c >= kMaxCtas)
         return;
     const SplitRecord rec = a.records[c];
-    if (!rec.valid || rec.first != c - 1)
+    if (rec.first != c - 1)
         return;
-    const int slot_row = (int)blockIdx.y * kCombineRows + ((int)threadIdx.x & 31);
+    const int slot_row = (int)(blockIdx.y / kShares) * 32 + ((int)threadIdx.x & 31);
     const int g = slot_row / kTileM, r = slot_row % kTileM;
-    const SeqRows q = load_seq(a.b, rec.seq);
-    const int32_t i = (2 * rec.pair + g) * a.positions + r / a.group;
-    if (slot_row >= a.split_rows || r >= a.positions * a.group || i >= q.n)
+    const int pos_in_tile = r / a.group, pos = g * a.positions + pos_in_tile;
+    if (pos_in_tile >= a.positions || pos >= rec.positions || slot_row >= a.split_rows)
         return;
-    auto part_of = [&](int32_t k) { return (int64_t)k * 2 + (k == rec.first ? 1 : 0); };
+    // the first part is in its CTA's second place, the others in their first
+    const int64_t stride_o = (int64_t)2 * (DP / 4) * a.split_rows;
+    const float2 *ml = a.part_ml + ((int64_t)rec.first * 2 + 1) * a.split_rows + slot_row;
+    const int chunk0 = ((int)(blockIdx.y % kShares) * kColumns + ((int)threadIdx.x >> 5)) * kChunks;
+    const float4 *po = a.part_o + (((int64_t)rec.first * 2 + 1) * (DP / 4) + chunk0) * a.split_rows + slot_row;
+    const int parts = rec.last - rec.first + 1;
+    auto ml_of = [&](int k) { return k == 0 ? ml : ml + (int64_t)(2 * k - 1) * a.split_rows; };
+    auto o_of = [&](int k) { return k == 0 ? po : po + k * stride_o - (int64_t)(DP / 4) * a.split_rows; };
     float m = -INFINITY;
-    for (int32_t k = rec.first; k <= rec.last; ++k)
-        m = fmaxf(m, a.part_ml[part_of(k) * a.split_rows + slot_row].x);
-    constexpr int kChunks = DP / 16;  // float4 columns per warp
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k)
+        m = fmaxf(m, ml_of(k)->x);
     float4 o[kChunks];
 #pragma unroll
     for (int x = 0; x < kChunks; ++x)
         o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
-    const int w = (int)threadIdx.x >> 5;
-    for (int32_t k = rec.first; k <= rec.last; ++k) {
-        const float2 ml = a.part_ml[part_of(k) * a.split_rows + slot_row];
-        const float f = ml.x == -INFINITY ? 0.f : ptx::ex2(ml.x - m);
-        l += f * ml.y;
-        const float4 *po = a.part_o + part_of(k) * (DP / 4) * a.split_rows + slot_row;
-        if (f == 0.f)
-            continue;  // nothing seen in this part, or nothing left of it
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+        const float2 w = *ml_of(k);
+        const float f = w.x == -INFINITY ? 0.f : ptx::ex2(w.x - m);
+        l += f * w.y;
 #pragma unroll
         for (int x = 0; x < kChunks; ++x) {
-            const float4 y = po[(int64_t)(x * 4 + w) * a.split_rows];
-            o[x].x = fmaf(f, y.x, o[x].x);
-            o[x].y = fmaf(f, y.y, o[x].y);
-            o[x].z = fmaf(f, y.z, o[x].z);
-            o[x].w = fmaf(f, y.w, o[x].w);
+            const float4 y = o_of(k)[(int64_t)x * a.split_rows];
+            if (f != 0.f) {  // else nothing seen in this part, or nothing left of it
+                o[x].x = fmaf(f, y.x, o[x].x);
+                o[x].y = fmaf(f, y.y, o[x].y);
+                o[x].z = fmaf(f, y.z, o[x].z);
+                o[x].w = fmaf(f, y.w, o[x].w);
+            }
         }
     }
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    const int head = rec.kv_head * a.group + r % a.group;
-    uint16_t *const dst = a.out.data + (int64_t)(q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
+    const int head = rec.kv_head * a.group + (r - pos_in_tile * a.group);
+    uint16_t *const dst = a.out.data + (int64_t)(rec.row + pos) * a.out.row_stride + (int64_t)head * a.out.head_stride;
 #pragma unroll
     for (int x = 0; x < kChunks; ++x) {
-        const int col = (x * 4 + w) * 4;
+        const int col = (chunk0 + x) * 4;
         if (col < a.b.head_dim)
             *reinterpret_cast<uint2 *>(dst + col) =
                 make_uint2(pack2<kBf16>(o[x].x * inv, o[x].y * inv), pack2<kBf16>(o[x].z * inv, o[x].w * inv));
@@ -1002,10 +1009,15 @@ int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, 
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, attend_kernel<DP, kBf16>, tq, tk, tv, a) != cudaSuccess)
         return WINO_ERR_CUDA;
-    cfg.gridDim = dim3((unsigned)std::max(1, ctas - 1), (unsigned)((a.split_rows + kCombineRows - 1) / kCombineRows));
-    cfg.blockDim = dim3(128);
+    // Few rows: a chunk per thread; many: four, so that the CTAs (most of which find nothing to do) are resident at once.
+    const bool few = a.split_rows <= 64;
+    const int columns = kCombineThreads / 32 * (few ? 1 : DP / 32);
+    cfg.gridDim = dim3((unsigned)std::max(1, ctas - 1), (unsigned)((a.split_rows + 31) / 32 * (DP / 4 / columns)));
+    cfg.blockDim = dim3(kCombineThreads);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16>, a) == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
+    const cudaError_t e = few ? cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16, 1>, a)
+                              : cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16, DP / 32>, a);
+    return e == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
 }
 
 }  // namespace
