@@ -44,7 +44,7 @@ constexpr int kRecordBytes = 32;        // SplitRecord
 constexpr int kCombineThreads = 256;
 constexpr int kSplitRows = 2 * kTileM;  // rows of a task
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
-constexpr int kTaskCost = 2;            // what a task costs beside its slot tiles, in slot tiles
+constexpr int kTaskCost = 3;            // what a task costs beside its slot tiles, in slot tiles
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemS = 0, kTmemO = 2 * kTileN, kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
@@ -140,7 +140,7 @@ struct alignas(16) Shared {
     uint64_t part_full[kParts], part_empty[kParts];
     uint64_t q_full, q_empty;
     uint64_t full[12], empty[12];
-    uint64_t s_full[2], p_ready[2], o_done[2];
+    uint64_t s_full[2], p_half[2], p_ready[2], o_done[2];
     uint64_t zeroed[12];  // per ring slot of V: the cache slots behind the last one hold zeros
     uint64_t ml_ready, ml_done;
     uint64_t mma_done;
@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     auto zeroed = [&](int s) { return ptx::smem_u32(&sh.zeroed[s]); };
     auto s_full = [&](int g) { return ptx::smem_u32(&sh.s_full[g]); };
     auto p_ready = [&](int g) { return ptx::smem_u32(&sh.p_ready[g]); };
+    auto p_half = [&](int g) { return ptx::smem_u32(&sh.p_half[g]); };
     auto o_done = [&](int g) { return ptx::smem_u32(&sh.o_done[g]); };
     auto part_full = [&](int s) { return ptx::smem_u32(&sh.part_full[s]); };
     auto part_empty = [&](int s) { return ptx::smem_u32(&sh.part_empty[s]); };
@@ -386,6 +387,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         for (int g = 0; g < 2; ++g) {
             ptx::mbar_init(s_full(g), 1);
+            ptx::mbar_init(p_half(g), 4);
             ptx::mbar_init(p_ready(g), 4);
             ptx::mbar_init(o_done(g), 1);
         }
@@ -526,9 +528,18 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
                         }
                         ptx::tmem_st_32x32b_x16(t_s + 16 * c, p);
+                        if (c == 1) {  // the first 64 slots' weights: their half of P V starts
+                            ptx::tmem_st_wait();
+                            ptx::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0)
+                                ptx::mbar_arrive(p_half(g));
+                        }
                     }
                     l += (l0.x + l0.y) + (l1.x + l1.y);
                     ptx::tmem_st_wait();
+                } else if (lane == 0) {
+                    ptx::mbar_arrive(p_half(g));
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -762,20 +773,30 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     ptx::mma_commit(s_full(g));
                 };
-                auto values = [&](int g, int vs, bool add) {  // O_g (+)= P_g V
+                // O_g (+)= P_g V, each half of the slots as soon as its weights are in tensor memory; zeros: V's slots behind
+                // the last one are zeroed first
+                auto values = [&](int g, int vs, bool add, bool zeros) -> bool {
                     const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), kHalfBytes);
+                    uint32_t &count = g ? n_p1 : n_p0;
+                    const uint32_t parity = count++ & 1u;
 #pragma unroll
-                    for (int k = 0; k < kTileN / 16; ++k)
+                    for (int k = 0; k < kTileN / 16; ++k) {
+                        if (k == 0) {
+                            if (!wait_bounded(p_half(g), parity, &sh.abort) ||
+                                (zeros && !wait_bounded(zeroed(vs), zero_phases >> vs & 1u, &sh.abort)))
+                                return false;
+                            ptx::tc_fence_after();
+                        }
+                        if (k == kTileN / 32) {
+                            if (!wait_bounded(p_ready(g), parity, &sh.abort))
+                                return false;
+                            ptx::tc_fence_after();
+                        }
                         ptx::mma_f16_ts(tmem + kTmemO + (uint32_t)(g * DP), tmem + kTmemS + (uint32_t)(g * kTileN + k * 8),
                                         db + (uint64_t)(k * (2048 >> 4)), id_o, (add || k != 0) ? 1u : 0u);
+                    }
                     ptx::mma_commit(o_done(g));
-                };
-                auto weights = [&](int g) -> bool {  // P_g is in tensor memory
-                    uint32_t &count = g ? n_p1 : n_p0;
-                    const bool good = wait_bounded(p_ready(g), count & 1u, &sh.abort);
-                    ++count;
-                    ptx::tc_fence_after();
-                    return good;
+                    return true;
                 };
                 while (!aborted && next_part()) {
                     const int32_t n = sh.parts[reader.slot()].n, flags = sh.parts[reader.slot()].flags;
@@ -793,24 +814,19 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     for (int32_t t = -lead; t < n; ++t) {
                         const int g = two ? 0 : (t & 1);
                         int vs = 0;
+                        bool zeros = false;
                         if (t >= 0) {
                             vs = v_slot;
-                            bool good = wait_bounded(full(vs), v_phase, &sh.abort);
+                            const bool good = wait_bounded(full(vs), v_phase, &sh.abort);
                             if (++v_slot == C::kSlots) {
                                 v_slot = C::kSlotsK;
                                 v_phase ^= 1u;
                             }
-                            const bool zeros = t == n - 1 && (flags & kTail) != 0;
-                            good = good && weights(g);
-                            if (good && zeros)
-                                good = wait_bounded(zeroed(vs), zero_phases >> vs & 1u, &sh.abort);
-                            if (zeros)
-                                zero_phases ^= 1u << vs;
-                            if (!good) {
+                            zeros = t == n - 1 && (flags & kTail) != 0;
+                            if (!good || !values(g, vs, t >= lead, zeros)) {
                                 aborted = true;
                                 break;
                             }
-                            values(g, vs, t >= lead);
                             if (!two)
                                 ptx::mma_commit(empty(vs));
                         }
@@ -828,13 +844,14 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             scores(g, 0, ks);
                         }
                         if (two && t >= 0) {
-                            if (!weights(1)) {
+                            if (!values(1, vs, t > 0, false)) {
                                 aborted = true;
                                 break;
                             }
-                            values(1, vs, t > 0);
                             ptx::mma_commit(empty(vs));
                         }
+                        if (zeros)
+                            zero_phases ^= 1u << vs;
                         if (ks >= 0) {
                             if (two)
                                 scores(1, 1, ks);
