@@ -46,7 +46,7 @@ constexpr int kSplitRows = 2 * kTileM;  // rows of a task
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
 constexpr int kTaskCost = 3;            // what a task costs beside its slot tiles, in slot tiles
 constexpr float kRescaleLog2 = 8.f;
-constexpr uint32_t kTmemS = 0, kTmemO = 2 * kTileN, kTmemAll = 512;
+constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 
 // What combine_kernel needs to know of the task that CTA c's run starts inside (one per CTA).
@@ -132,6 +132,12 @@ struct Config {
     static constexpr int kSlots = kSlotsK + kSlotsV;
     static constexpr uint32_t kRing = kSlots * kTileBytes;
     static constexpr uint32_t kShared = 3072;
+    // Tensor memory columns of warpgroup g: S at kTmemS + g 128, P at kTmemP + g kStrideP, O at kTmemO + g DP.  With 64 dims
+    // P has columns of its own, and the scores of the next tile are computed as soon as S is in registers; with 128
+    // they are taken by O, P overwrites S, and the next scores wait for P V.
+    static constexpr bool kEarly = DP == 64;
+    static constexpr uint32_t kTmemS = 0, kTmemP = kEarly ? 256 : 0, kStrideP = kEarly ? 64 : 128;
+    static constexpr uint32_t kTmemO = kEarly ? 384 : 256;
     static constexpr uint32_t kSmem = 2 * kTileBytes + kRing + kShared;
 };
 
@@ -140,7 +146,7 @@ struct alignas(16) Shared {
     uint64_t part_full[kParts], part_empty[kParts];
     uint64_t q_full, q_empty;
     uint64_t full[12], empty[12];
-    uint64_t s_full[2], p_half[2], p_ready[2], o_done[2];
+    uint64_t s_full[2], s_free[2], p_half[2], p_ready[2], o_done[2];
     uint64_t zeroed[12];  // per ring slot of V: the cache slots behind the last one hold zeros
     uint64_t ml_ready, ml_done;
     uint64_t mma_done;
@@ -364,6 +370,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     auto zeroed = [&](int s) { return ptx::smem_u32(&sh.zeroed[s]); };
     auto s_full = [&](int g) { return ptx::smem_u32(&sh.s_full[g]); };
     auto p_ready = [&](int g) { return ptx::smem_u32(&sh.p_ready[g]); };
+    auto s_free = [&](int g) { return ptx::smem_u32(&sh.s_free[g]); };
     auto p_half = [&](int g) { return ptx::smem_u32(&sh.p_half[g]); };
     auto o_done = [&](int g) { return ptx::smem_u32(&sh.o_done[g]); };
     auto part_full = [&](int s) { return ptx::smem_u32(&sh.part_full[s]); };
@@ -387,6 +394,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         for (int g = 0; g < 2; ++g) {
             ptx::mbar_init(s_full(g), 1);
+            ptx::mbar_init(s_free(g), 4);
             ptx::mbar_init(p_half(g), 4);
             ptx::mbar_init(p_ready(g), 4);
             ptx::mbar_init(o_done(g), 1);
@@ -431,7 +439,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const int g = warp >> 2;               // warpgroup
         const int r = (warp & 3) * 32 + lane;  // row of the tile, its TMEM lane
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_s = lanes + kTmemS + (uint32_t)g * kTileN;
+        const uint32_t t_s = lanes + C::kTmemS + (uint32_t)g * kTileN;
+        const uint32_t t_p = lanes + C::kTmemP + (uint32_t)g * C::kStrideP;
         const int pos_in_tile = r / a.group;
         const float sl2 = a.scale_log2;
         const float rescale = kRescaleLog2 / sl2;
@@ -468,6 +477,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         ptx::tmem_ld_wait(x[c]);
+                    if (C::kEarly) {  // S is free for the next tile's scores
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0)
+                            ptx::mbar_arrive(s_free(g));
+                    }
                     if (__any_sync(0xffffffffu, valid && (lim < kTileN || (hole >= 0 && hole < kTileN)))) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
@@ -490,22 +505,25 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     const float mx = ptx::max3(ptx::max3(y[0], y[1], y[2]), ptx::max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
                     const bool grow = mx > m + (m == -INFINITY ? 0.f : rescale);
-                    if (t != first && __any_sync(0xffffffffu, grow && m != -INFINITY)) {
-                        // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
+                    // P's columns, or O where it has to be rescaled: P V of the tile before is done first
+                    const bool scale_o = t != first && __any_sync(0xffffffffu, grow && m != -INFINITY);
+                    if (scale_o || (C::kEarly && t != first)) {
                         if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
                             break;
                         ptx::tc_fence_after();
+                    }
+                    if (scale_o) {  // the O of earlier tiles is scaled to the new maximum
                         const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
                         l *= f;
 #pragma unroll 1
                         for (int c = 0; c < DP; c += 16) {
                             uint32_t o[16];
-                            ptx::tmem_ld_32x32b_x16(lanes + kTmemO + (uint32_t)(g * DP + c), o);
+                            ptx::tmem_ld_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
                             ptx::tmem_ld_wait();
 #pragma unroll
                             for (int k = 0; k < 16; ++k)
                                 o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            ptx::tmem_st_32x32b_x16(lanes + kTmemO + (uint32_t)(g * DP + c), o);
+                            ptx::tmem_st_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
                         }
                     }
                     if (grow)
@@ -527,7 +545,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             p[k / 2] = pack2<kBf16>(u.x, u.y);
                             p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
                         }
-                        ptx::tmem_st_32x32b_x16(t_s + 16 * c, p);
+                        ptx::tmem_st_32x32b_x16(t_p + 16 * c, p);
                         if (c == 1) {  // the first 64 slots' weights: their half of P V starts
                             ptx::tmem_st_wait();
                             ptx::tc_fence_before();
@@ -538,8 +556,16 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     l += (l0.x + l0.y) + (l1.x + l1.y);
                     ptx::tmem_st_wait();
-                } else if (lane == 0) {
-                    ptx::mbar_arrive(p_half(g));
+                } else {
+                    // A warp without rows arrives as the others do, and no tile ahead of them: with S free early that takes
+                    // the wait for P V of the tile before.
+                    if (C::kEarly && t != first && !(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
+                        break;
+                    if (lane == 0) {
+                        if (C::kEarly)
+                            ptx::mbar_arrive(s_free(g));
+                        ptx::mbar_arrive(p_half(g));
+                    }
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -589,7 +615,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 const int head = part.kv_head * a.group + (r - pos_in_tile * a.group);
                 uint16_t *const dst = a.out.data + (int64_t)(part.q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
                 float4 *const po = a.part_o + to * (DP / 4) * a.split_rows + slot_row;
-                const uint32_t t_o = lanes + kTmemO + (uint32_t)(two ? g * DP : 0);
+                const uint32_t t_o = lanes + C::kTmemO + (uint32_t)(two ? g * DP : 0);
 #pragma unroll 1
                 for (int c = c0; c < c1; c += 32) {
                     float o[32];
@@ -762,16 +788,24 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 uint32_t parts = 0;
                 uint32_t zero_phases = 0;  // bit s: phase of zeroed(s)
                 uint32_t n_p0 = 0, n_p1 = 0;  // slot tiles of each warpgroup whose weights were taken
+                uint32_t n_s0 = 0, n_s1 = 0;  // and whose scores were issued
                 bool aborted = false;
-                auto scores = [&](int g, int qt, int ks) {  // S_g = Q_qt K^T
+                auto scores = [&](int g, int qt, int ks) -> bool {  // S_g = Q_qt K^T
+                    if (C::kEarly) {
+                        uint32_t &count = g ? n_s1 : n_s0;
+                        if (!wait_bounded(s_free(g), (count++ & 1u) ^ 1u, &sh.abort))
+                            return false;
+                        ptx::tc_fence_after();
+                    }
                     const uint64_t da = ptx::sdesc_kmajor_sw128(sq + (uint32_t)qt * C::kTileBytes);
                     const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks));
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
                         const uint64_t off = (uint64_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
-                        ptx::mma_bf16(tmem + kTmemS + (uint32_t)g * kTileN, da + off, db + off, id_s, k != 0);
+                        ptx::mma_bf16(tmem + C::kTmemS + (uint32_t)g * kTileN, da + off, db + off, id_s, k != 0);
                     }
                     ptx::mma_commit(s_full(g));
+                    return true;
                 };
                 // O_g (+)= P_g V, each half of the slots as soon as its weights are in tensor memory; zeros: V's slots behind
                 // the last one are zeroed first
@@ -792,7 +826,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                                 return false;
                             ptx::tc_fence_after();
                         }
-                        ptx::mma_f16_ts(tmem + kTmemO + (uint32_t)(g * DP), tmem + kTmemS + (uint32_t)(g * kTileN + k * 8),
+                        ptx::mma_f16_ts(tmem + C::kTmemO + (uint32_t)(g * DP), tmem + C::kTmemP + (uint32_t)g * C::kStrideP + (uint32_t)(k * 8),
                                         db + (uint64_t)(k * (2048 >> 4)), id_o, (add || k != 0) ? 1u : 0u);
                     }
                     ptx::mma_commit(o_done(g));
@@ -811,53 +845,48 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         break;
                     }
                     ++parts;
+                    // Scores run `lead` tiles ahead of the values.  With S free early, both tiles' scores go out before the
+                    // values; without, each warpgroup's scores behind its own values, which free S.
                     for (int32_t t = -lead; t < n; ++t) {
                         const int g = two ? 0 : (t & 1);
-                        int vs = 0;
-                        bool zeros = false;
-                        if (t >= 0) {
-                            vs = v_slot;
-                            const bool good = wait_bounded(full(vs), v_phase, &sh.abort);
-                            if (++v_slot == C::kSlots) {
-                                v_slot = C::kSlotsK;
-                                v_phase ^= 1u;
-                            }
-                            zeros = t == n - 1 && (flags & kTail) != 0;
-                            if (!good || !values(g, vs, t >= lead, zeros)) {
-                                aborted = true;
-                                break;
-                            }
-                            if (!two)
+                        const bool v_now = t >= 0, k_now = t + lead < n;
+                        const bool zeros = t == n - 1 && (flags & kTail) != 0;
+                        const int vs = v_slot, ks = k_slot;
+                        bool good = true;
+                        if (k_now && C::kEarly)
+                            good = wait_bounded(full(ks), k_phase, &sh.abort) && scores(g, 0, ks) && (!two || scores(1, 1, ks));
+                        if (good && v_now) {
+                            good = wait_bounded(full(vs), v_phase, &sh.abort) && values(g, vs, t >= lead, zeros);
+                            if (good && !two)
                                 ptx::mma_commit(empty(vs));
                         }
-                        int ks = -1;
-                        if (t + lead < n) {
-                            ks = k_slot;
-                            if (!wait_bounded(full(ks), k_phase, &sh.abort)) {
-                                aborted = true;
-                                break;
-                            }
-                            if (++k_slot == C::kSlotsK) {
-                                k_slot = 0;
-                                k_phase ^= 1u;
-                            }
-                            scores(g, 0, ks);
+                        if (good && k_now && !C::kEarly)
+                            good = wait_bounded(full(ks), k_phase, &sh.abort) && scores(g, 0, ks);
+                        if (good && v_now && two) {
+                            good = values(1, vs, t > 0, false);
+                            if (good)
+                                ptx::mma_commit(empty(vs));
                         }
-                        if (two && t >= 0) {
-                            if (!values(1, vs, t > 0, false)) {
-                                aborted = true;
-                                break;
-                            }
-                            ptx::mma_commit(empty(vs));
-                        }
-                        if (zeros)
-                            zero_phases ^= 1u << vs;
-                        if (ks >= 0) {
-                            if (two)
-                                scores(1, 1, ks);
+                        if (good && k_now) {
+                            if (two && !C::kEarly)
+                                good = scores(1, 1, ks);
                             ptx::mma_commit(empty(ks));
                             if (t + lead == n - 1)
                                 ptx::mma_commit(q_empty);
+                        }
+                        if (!good) {
+                            aborted = true;
+                            break;
+                        }
+                        if (zeros)
+                            zero_phases ^= 1u << vs;
+                        if (v_now && ++v_slot == C::kSlots) {
+                            v_slot = C::kSlotsK;
+                            v_phase ^= 1u;
+                        }
+                        if (k_now && ++k_slot == C::kSlotsK) {
+                            k_slot = 0;
+                            k_phase ^= 1u;
                         }
                     }
                 }

@@ -251,3 +251,11 @@ def test_many_short_parts_with_tails():
     """Parts of one or two slot tiles, each ending inside a tile, several in flight at once in every CTA."""
     seqs = [(1, 1 + (37 * i) % 250, (37 * i) % 250) for i in range(700)]
     run(add_rows(make_kv(CAUSAL, seqs, heads=8, kv_heads=8, dim=128)))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_few_rows_over_large_pages(dim):
+    """Most warps without rows, and slot tiles that arrive at once: no warp may run a tile ahead of the others."""
+    for n in (257, 300, 385, 513, 700, 1500):
+        for rows in (1, 3, 40):
+            run(add_rows(make_kv(FULL, [(rows, n, 0)], dim=dim, page=128, layout="heads", seed=n)))
