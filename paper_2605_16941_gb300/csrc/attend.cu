@@ -74,6 +74,8 @@ struct AttendArgs {
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
     int32_t min_units;         // a CTA's run is at least this long
     int32_t wide;              // units may need 64 bits
+    int32_t wide_rows;         // rows of out are 32-byte aligned
+    int32_t page_shift;        // log2(page_size), or -1
 };
 
 // Tasks of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256, so that the product with
@@ -81,6 +83,11 @@ struct AttendArgs {
 __device__ __forceinline__ int32_t pairs_of(const AttendArgs &a, const SeqRows &q)
 {
     return (int32_t)__umulhi((uint32_t)(q.n + 2 * a.positions - 1), a.pair_magic);
+}
+
+__device__ __forceinline__ int32_t page_entry(const AttendArgs &a, int32_t slot)
+{
+    return a.page_shift >= 0 ? slot >> a.page_shift : slot / a.b.page_size;
 }
 
 // Slots that some row of task `pair` sees: its last row sees as many as any.
@@ -505,14 +512,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     const float mx = ptx::max3(ptx::max3(y[0], y[1], y[2]), ptx::max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
                     const bool grow = mx > m + (m == -INFINITY ? 0.f : rescale);
-                    // P's columns, or O where it has to be rescaled: P V of the tile before is done first
-                    const bool scale_o = t != first && __any_sync(0xffffffffu, grow && m != -INFINITY);
-                    if (scale_o || (C::kEarly && t != first)) {
+                    if (t != first && __any_sync(0xffffffffu, grow && m != -INFINITY)) {
+                        // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
                         if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
                             break;
                         ptx::tc_fence_after();
-                    }
-                    if (scale_o) {  // the O of earlier tiles is scaled to the new maximum
                         const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
                         l *= f;
 #pragma unroll 1
@@ -545,15 +549,22 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             p[k / 2] = pack2<kBf16>(u.x, u.y);
                             p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
                         }
-                        ptx::tmem_st_32x32b_x16(t_p + 16 * c, p);
-                        if (c == 1) {  // the first 64 slots' weights: their half of P V starts
+                        if (C::kEarly && c == 0 && t != first) {  // P's columns are free: P V of the tile before is done
+                            if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
+                                break;
+                            ptx::tc_fence_after();
+                        }
+                        if (!C::kEarly && c == 2) {  // the first 64 slots' weights are in place: their half of P V starts
                             ptx::tmem_st_wait();
                             ptx::tc_fence_before();
                             __syncwarp();
                             if (lane == 0)
                                 ptx::mbar_arrive(p_half(g));
                         }
+                        ptx::tmem_st_32x32b_x16(t_p + 16 * c, p);
                     }
+                    if (!good)
+                        break;
                     l += (l0.x + l0.y) + (l1.x + l1.y);
                     ptx::tmem_st_wait();
                 } else {
@@ -561,11 +572,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     // the wait for P V of the tile before.
                     if (C::kEarly && t != first && !(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
                         break;
-                    if (lane == 0) {
-                        if (C::kEarly)
-                            ptx::mbar_arrive(s_free(g));
-                        ptx::mbar_arrive(p_half(g));
-                    }
+                    if (lane == 0)
+                        ptx::mbar_arrive(C::kEarly ? s_free(g) : p_half(g));
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -621,31 +629,45 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     float o[32];
                     if (n > 0) {
                         ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)c, o);
-                        ptx::tmem_ld_wait(o);
+                        if (!two && n > 1) {
+                            float o1[32];
+                            ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)(DP + c), o1);
+                            ptx::tmem_ld_wait(o);
+                            ptx::tmem_ld_wait(o1);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            o[k] *= f0;
+                            for (int k = 0; k < 32; ++k)
+                                o[k] = fmaf(f1, o1[k], f0 * o[k]);
+                        } else {
+                            ptx::tmem_ld_wait(o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                o[k] *= f0;
+                        }
                     } else {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
                             o[k] = 0.f;
                     }
-                    if (!two && n > 1) {
-                        float o1[32];
-                        ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)(DP + c), o1);
-                        ptx::tmem_ld_wait(o1);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            o[k] = fmaf(f1, o1[k], o[k]);
-                    }
                     if (!valid) {
                     } else if (whole) {
+                        // A store covers 32 rows: 32 bytes of each where the rows are aligned for that, else 16 (an
+                        // instruction takes a cycle per row, whatever its width).
+                        uint32_t y[16];
 #pragma unroll
-                        for (int k = 0; k < 32; k += 8)
-                            if (c + k < a.b.head_dim)
-                                *reinterpret_cast<uint4 *>(dst + c + k) =
-                                    make_uint4(pack2<kBf16>(o[k], o[k + 1]), pack2<kBf16>(o[k + 2], o[k + 3]),
-                                               pack2<kBf16>(o[k + 4], o[k + 5]), pack2<kBf16>(o[k + 6], o[k + 7]));
+                        for (int k = 0; k < 16; ++k)
+                            y[k] = pack2<kBf16>(o[2 * k], o[2 * k + 1]);
+#pragma unroll
+                        for (int k = 0; k < 16; k += 8) {
+                            uint16_t *const at = dst + c + 2 * k;
+                            if (a.wide_rows && c + 2 * k + 16 <= a.b.head_dim) {
+                                ptx::st_global_v8(at, &y[k]);
+                            } else {
+                                if (c + 2 * k < a.b.head_dim)
+                                    *reinterpret_cast<uint4 *>(at) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                                if (c + 2 * k + 8 < a.b.head_dim)
+                                    *reinterpret_cast<uint4 *>(at + 8) = make_uint4(y[k + 4], y[k + 5], y[k + 6], y[k + 7]);
+                            }
+                        }
                     } else {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
@@ -699,13 +721,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 if (n == 0)
                     continue;
                 const bool two = (part.flags & kTwo) != 0;
-                // Page numbers: 32 consecutive table entries in the lanes, and the 32 behind them on their way.
-                const int32_t last_entry = (part.kv_end - 1) / a.b.page_size;
-                int32_t window = (part.j0 * kTileN) / a.b.page_size;  // first entry of `near`
-                auto entries = [&](int32_t e0) {
-                    const int32_t e = e0 + lane;
-                    return e <= last_entry ? load_page(a.b, part.seq, e, ok) : -1;
-                };
+                // Page numbers: 32 consecutive table entries in the lanes, and the 32 behind them on their way.  They are
+                // checked where they are used, so that nothing waits for a load before that.
+                const int32_t last_entry = page_entry(a, part.kv_end - 1);
+                int32_t window = page_entry(a, part.j0 * kTileN);  // first entry of `near`
+                const int32_t *const table = a.b.page_table + (int64_t)part.seq * a.b.table_width;
+                auto entries = [&](int32_t e0) { return e0 + lane <= last_entry ? table[e0 + lane] : 0; };
                 int32_t near = entries(window), ahead = entries(window + 32);
                 if (!is_v) {  // Q: the part's one or two tiles
                     if (!warp_wait(q_empty, (parts & 1u) ^ 1u, &sh.abort)) {
@@ -727,15 +748,17 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     const int32_t first = (part.j0 + t) * kTileN;
                     const int32_t boxes = min(a.boxes, (part.kv_end - first + a.box_rows - 1) / a.box_rows);
                     const int32_t at = first + box * a.box_rows;  // this lane's first slot
-                    const int32_t entry = at / a.b.page_size;
-                    if ((first + boxes * a.box_rows - 1) / a.b.page_size - window >= 32) {  // no tile straddles the border
+                    const int32_t entry = page_entry(a, at);
+                    if (page_entry(a, first + boxes * a.box_rows - 1) - window >= 32) {  // no tile straddles the border
                         near = ahead;
                         window += 32;
                         ahead = entries(window + 32);
                     }
                     int32_t page = __shfl_sync(0xffffffffu, near, (entry - window) & 31);
-                    if (page < 0)
+                    if ((uint32_t)page >= (uint32_t)a.b.n_pages) {
+                        ok = ok && box >= boxes;
                         page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
+                    }
                     if (!warp_wait(empty(slot), phase ^ 1u, &sh.abort)) {
                         aborted = true;
                         break;
@@ -807,7 +830,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     ptx::mma_commit(s_full(g));
                     return true;
                 };
-                // O_g (+)= P_g V, each half of the slots as soon as its weights are in tensor memory; zeros: V's slots behind
+                // O_g (+)= P_g V, each half of the slots as soon as its weights are in tensor memory (where nothing waits for
+                // P V but the next scores; with S free early, at once); zeros: V's slots behind
                 // the last one are zeroed first
                 auto values = [&](int g, int vs, bool add, bool zeros) -> bool {
                     const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), kHalfBytes);
@@ -816,12 +840,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 #pragma unroll
                     for (int k = 0; k < kTileN / 16; ++k) {
                         if (k == 0) {
-                            if (!wait_bounded(p_half(g), parity, &sh.abort) ||
+                            if (!wait_bounded(C::kEarly ? p_ready(g) : p_half(g), parity, &sh.abort) ||
                                 (zeros && !wait_bounded(zeroed(vs), zero_phases >> vs & 1u, &sh.abort)))
                                 return false;
                             ptx::tc_fence_after();
                         }
-                        if (k == kTileN / 32) {
+                        if (!C::kEarly && k == kTileN / 32) {
                             if (!wait_bounded(p_ready(g), parity, &sh.abort))
                                 return false;
                             ptx::tc_fence_after();
@@ -1092,6 +1116,12 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.min_units = kTaskCost + 2;
     const int64_t pairs = b.n_rows / (2 * a.positions) + b.n_seq, tiles = (int64_t)b.table_width * b.page_size / kTileN + 1;
     a.wide = (double)pairs * (double)(tiles + kTaskCost) * b.n_kv_heads >= 2147483648.0;
+    a.page_shift = -1;
+    for (int i = 4; i <= 30; ++i)
+        if (b.page_size == 1 << i)
+            a.page_shift = i;
+    a.wide_rows = aligned(out.data, 32) && (b.n_rows == 1 || out.row_stride % 16 == 0) &&
+                  (b.n_q_heads == 1 || out.head_stride % 16 == 0);
     CUtensorMap tq, tk, tv;
     const int64_t q_dims[3] = {b.head_dim, b.n_q_heads, b.n_rows}, q_strides[3] = {1, q.head_stride, q.row_stride};
     const int32_t q_box[3] = {64, a.group, a.positions};
