@@ -4,6 +4,10 @@
 // Angles: t / 2 pi modulo 1 is what matters, and x f in 32 bits loses it for far positions (x = 10^6, f = 1: 0.06
 // radians).  f / 2 pi is taken to a 64-bit fixed-point fraction of a turn once per CTA and pair; its product with the
 // position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.
+//
+// Bound by HBM: every element is read and written once, 16 bytes at a time.  A thread has one row and two 16-byte chunks
+// of a head that hold 8 whole pairs, keeps their cosines and sines in registers, and walks the heads with the loads of
+// four of them in flight.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -18,6 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxRowsPerCta = 8;
 constexpr int kMaxPairs = 64;  // head_dim / 2
+constexpr int kAhead = 4;      // heads of which a thread has loads in flight
 
 struct RopeArgs {
     wino_heads q, q_out, k, v;
@@ -60,23 +65,33 @@ __device__ __forceinline__ uint64_t turn_fraction(double radians)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeArgs a)
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
-    __shared__ float2 cs[kMaxRowsPerCta][kMaxPairs];
-    __shared__ int32_t seq[kMaxRowsPerCta];
-    __shared__ int32_t slot_page[kMaxRowsPerCta], slot_in[kMaxRowsPerCta], pos[kMaxRowsPerCta];
-    __shared__ uint64_t turns[kMaxPairs];
+    return (uint32_t)from_f<T>(lo) | (uint32_t)from_f<T>(hi) << 16;
+}
+
+// a' and b' of one pair.
+__device__ __forceinline__ float2 turn(float a, float b, float2 c)
+{
+    return make_float2(a * c.x - b * c.y, b * c.x + a * c.y);
+}
+
+// What a CTA knows of its rows.
+struct Rows {
+    float2 cs[kMaxRowsPerCta][kMaxPairs];
+    uint64_t turns[kMaxPairs];
+    SeqRows q[kMaxRowsPerCta];
+    int32_t seq[kMaxRowsPerCta];   // -1: a row of no sequence
+    int32_t page[kMaxRowsPerCta];  // -1: not stored
+    int32_t in_page[kMaxRowsPerCta], pos[kMaxRowsPerCta];
+};
+
+__device__ __forceinline__ void find_rows(const RopeArgs &a, Rows &sh, int32_t row0, int32_t n_rows)
+{
     const wino_kv_batch &b = a.b;
-    const int tid = (int)threadIdx.x;
-    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
-    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
-    const int n_pairs = a.rope.rot_dim >> 1;
-    ptx::grid_dep_launch_dependents();
-    ptx::grid_dep_wait();
+    const int tid = (int)threadIdx.x, n_pairs = a.rope.rot_dim >> 1;
     if (tid < kMaxRowsPerCta)
-        seq[tid] = -1;
-    for (int j = tid; j < n_pairs; j += kThreads)
-        turns[j] = turn_fraction(a.rope.freq[j]);
+        sh.seq[tid] = -1;
     __syncthreads();
     bool ok = true;
     for (int32_t s = tid; s < b.n_seq; s += kThreads) {
@@ -84,46 +99,136 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeArgs a)
         ok = ok && q.ok;
         const int32_t r1 = min(n_rows, q.start + q.n - row0);
         if (q.n > 0)
-            for (int32_t r = max(0, q.start - row0); r < r1; ++r)
-                seq[r] = s;
+            for (int32_t r = max(0, q.start - row0); r < r1; ++r) {
+                sh.seq[r] = s;
+                sh.q[r] = q;
+            }
     }
+    for (int j = tid; j < n_pairs; j += kThreads)
+        sh.turns[j] = turn_fraction(a.rope.freq[j]);
     __syncthreads();
-    if (tid < n_rows && seq[tid] >= 0) {
-        const int32_t s = seq[tid];
-        const SeqRows q = load_seq(b, s);
+    if (tid < n_rows && sh.seq[tid] >= 0) {
+        const SeqRows q = sh.q[tid];
         const int32_t i = row0 + tid - q.start, slot = row_slot(b, q, i), cap = b.table_width * b.page_size;
         int32_t page = -1;
         if (a.k.data && slot >= 0) {
             if (slot < cap)
-                page = load_page(b, s, slot / b.page_size, ok);
+                page = load_page(b, sh.seq[tid], slot / b.page_size, ok);
             else
                 ok = false;
         }
-        slot_page[tid] = page;
-        slot_in[tid] = page >= 0 ? slot % b.page_size : 0;
-        pos[tid] = a.rope.positions ? a.rope.positions[row0 + tid]
-                                    : q.base + (b.mask == WINO_MASK_SHADOW && i >= (q.n >> 1) ? i - (q.n >> 1) : i);
+        sh.page[tid] = page;
+        sh.in_page[tid] = page >= 0 ? slot % b.page_size : 0;
+        sh.pos[tid] = a.rope.positions ? a.rope.positions[row0 + tid]
+                                       : q.base + (b.mask == WINO_MASK_SHADOW && i >= (q.n >> 1) ? i - (q.n >> 1) : i);
     }
     if (!ok)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
     __syncthreads();
     for (int x = tid; x < n_rows * n_pairs; x += kThreads) {
         const int r = x / n_pairs, j = x - r * n_pairs;
-        if (seq[r] < 0)
+        if (sh.seq[r] < 0)
             continue;
-        const uint64_t t = turns[j] * (uint64_t)(int64_t)pos[r];
+        const uint64_t t = sh.turns[j] * (uint64_t)(int64_t)sh.pos[r];
         float sn, cn;
         sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &sn, &cn);  // half-turns in [-1, 1)
-        cs[r][j] = make_float2(cn * a.rope.factor, sn * a.rope.factor);
+        sh.cs[r][j] = make_float2(cn * a.rope.factor, sn * a.rope.factor);
     }
     __syncthreads();
-    // one (row, head, dim pair or plain dim) per thread and turn
-    const int heads = (a.q.data ? b.n_q_heads : 0) + (a.k.data ? 2 * b.n_kv_heads : 0);
-    const int D = b.head_dim, nq = a.q.data ? b.n_q_heads : 0;
-    const int units = D - n_pairs;  // pairs, then the plain dims
-    for (int64_t x = tid; x < (int64_t)n_rows * heads * units; x += kThreads) {
+}
+
+// head_dim and rot_dim multiples of 16: two 16-byte chunks of a head per thread and turn, 8 pairs or 16 plain dims.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeArgs a)
+{
+    __shared__ Rows sh;
+    const wino_kv_batch &b = a.b;
+    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
+    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
+    ptx::grid_dep_launch_dependents();
+    ptx::grid_dep_wait();
+    find_rows(a, sh, row0, n_rows);
+    const int items = b.head_dim >> 4, turned = a.rope.rot_dim >> 4;  // of a head
+    const int lanes = items * a.rows_per_cta;                         // (row, item) pairs of the CTA
+    const int slots = kThreads / lanes;                               // heads at a time
+    const int tid = (int)threadIdx.x, r = tid % lanes / items, j = tid % items, h0 = tid / lanes;
+    if (h0 >= slots || r >= n_rows || sh.seq[r] < 0)
+        return;
+    // the item's chunks, in units of 16 bytes: halves j and j + rot / 16, or neighbours
+    const bool turns = j < turned;
+    const int c0 = turns && !a.rope.interleaved ? j : 2 * j;
+    const int c1 = turns && !a.rope.interleaved ? j + turned : 2 * j + 1;
+    float2 cs[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        cs[k] = turns ? sh.cs[r][8 * j + k] : make_float2(0.f, 0.f);
+    const int64_t row = row0 + r;
+    auto walk = [&](const uint16_t *src, int64_t src_stride, uint16_t *dst, int64_t dst_stride, int heads, bool rotate) {
+        for (int h = h0; h < heads; h += kAhead * slots) {
+            uint4 x[kAhead], y[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (h + u * slots < heads) {
+                    const uint4 *p = reinterpret_cast<const uint4 *>(src + (h + u * slots) * src_stride);
+                    x[u] = p[c0];
+                    y[u] = p[c1];
+                }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (h + u * slots < heads) {
+                    if (rotate) {
+                        uint32_t *const v = &x[u].x, *const w = &y[u].x;
+                        if (a.rope.interleaved) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const float2 p = turn(to_f<T>((uint16_t)v[k]), to_f<T>((uint16_t)(v[k] >> 16)), cs[k]);
+                                const float2 q = turn(to_f<T>((uint16_t)w[k]), to_f<T>((uint16_t)(w[k] >> 16)), cs[4 + k]);
+                                v[k] = pack2<T>(p.x, p.y);
+                                w[k] = pack2<T>(q.x, q.y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const float2 p = turn(to_f<T>((uint16_t)v[k]), to_f<T>((uint16_t)w[k]), cs[2 * k]);
+                                const float2 q = turn(to_f<T>((uint16_t)(v[k] >> 16)), to_f<T>((uint16_t)(w[k] >> 16)), cs[2 * k + 1]);
+                                v[k] = pack2<T>(p.x, q.x);
+                                w[k] = pack2<T>(p.y, q.y);
+                            }
+                        }
+                    }
+                    uint4 *const d = reinterpret_cast<uint4 *>(dst + (h + u * slots) * dst_stride);
+                    d[c0] = x[u];
+                    d[c1] = y[u];
+                }
+        }
+    };
+    if (a.q.data)
+        walk(a.q.data + row * a.q.row_stride, a.q.head_stride, a.q_out.data + row * a.q_out.row_stride, a.q_out.head_stride,
+             b.n_q_heads, turns);
+    if (sh.page[r] >= 0) {
+        const int64_t at = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride;
+        walk(a.k.data + row * a.k.row_stride, a.k.head_stride, b.k_cache + at, b.head_stride, b.n_kv_heads, turns);
+        walk(a.v.data + row * a.v.row_stride, a.v.head_stride, b.v_cache + at, b.head_stride, b.n_kv_heads, false);
+    }
+}
+
+// Any other dims: one pair or plain dim per thread and turn.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rope_append_any_kernel(const RopeArgs a)
+{
+    __shared__ Rows sh;
+    const wino_kv_batch &b = a.b;
+    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
+    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
+    ptx::grid_dep_launch_dependents();
+    ptx::grid_dep_wait();
+    find_rows(a, sh, row0, n_rows);
+    const int n_pairs = a.rope.rot_dim >> 1, nq = a.q.data ? b.n_q_heads : 0;
+    const int heads = nq + (a.k.data ? 2 * b.n_kv_heads : 0);
+    const int units = b.head_dim - n_pairs;  // pairs, then the plain dims
+    for (int64_t x = threadIdx.x; x < (int64_t)n_rows * heads * units; x += kThreads) {
         const int u = (int)(x % units), h = (int)(x / units % heads), r = (int)(x / units / heads);
-        if (seq[r] < 0)
+        if (sh.seq[r] < 0)
             continue;
         const int64_t row = row0 + r;
         const uint16_t *src;
@@ -133,23 +238,22 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeArgs a)
             src = a.q.data + row * a.q.row_stride + h * a.q.head_stride;
             dst = a.q_out.data + row * a.q_out.row_stride + h * a.q_out.head_stride;
         } else {
-            if (slot_page[r] < 0)
+            if (sh.page[r] < 0)
                 continue;
             const bool is_k = h - nq < b.n_kv_heads;
             const int hk = is_k ? h - nq : h - nq - b.n_kv_heads;
             const wino_heads &w = is_k ? a.k : a.v;
             src = w.data + row * w.row_stride + hk * w.head_stride;
-            dst = (is_k ? b.k_cache : b.v_cache) + (int64_t)slot_page[r] * b.page_stride +
-                  (int64_t)slot_in[r] * b.slot_stride + hk * b.head_stride;
+            dst = (is_k ? b.k_cache : b.v_cache) + (int64_t)sh.page[r] * b.page_stride +
+                  (int64_t)sh.in_page[r] * b.slot_stride + hk * b.head_stride;
             rotate = is_k;
         }
         if (u < n_pairs) {
             const int i0 = a.rope.interleaved ? 2 * u : u, i1 = a.rope.interleaved ? 2 * u + 1 : u + n_pairs;
             if (rotate) {
-                const float2 c = cs[r][u];
-                const float p = to_f<T>(src[i0]), q = to_f<T>(src[i1]);
-                dst[i0] = from_f<T>(p * c.x - q * c.y);
-                dst[i1] = from_f<T>(q * c.x + p * c.y);
+                const float2 p = turn(to_f<T>(src[i0]), to_f<T>(src[i1]), sh.cs[r][u]);
+                dst[i0] = from_f<T>(p.x);
+                dst[i1] = from_f<T>(p.y);
             } else {
                 dst[i0] = src[i0];
                 dst[i1] = src[i1];
@@ -177,7 +281,8 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     a.b = b;
     a.rope = rope;
     a.status = status;
-    a.rows_per_cta = std::max(1, std::min(kMaxRowsPerCta, b.n_rows / 1024));
+    // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads.
+    a.rows_per_cta = b.n_rows >= 1024 ? 4 : (b.n_rows >= 512 ? 2 : 1);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
     cfg.blockDim = dim3(kThreads);
@@ -187,8 +292,11 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return b.dtype == WINO_BF16 ? cudaLaunchKernelEx(&cfg, rope_append_kernel<__nv_bfloat16>, a)
-                                : cudaLaunchKernelEx(&cfg, rope_append_kernel<__half>, a);
+    if (b.head_dim % 16 == 0 && rope.rot_dim % 16 == 0)
+        return b.dtype == WINO_BF16 ? cudaLaunchKernelEx(&cfg, rope_append_kernel<__nv_bfloat16>, a)
+                                    : cudaLaunchKernelEx(&cfg, rope_append_kernel<__half>, a);
+    return b.dtype == WINO_BF16 ? cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__nv_bfloat16>, a)
+                                : cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__half>, a);
 }
 
 }  // namespace wino
