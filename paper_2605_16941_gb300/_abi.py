@@ -342,9 +342,17 @@ def wino_decode(W, tokens, params: WinoParams, n_blocks: int, hidden, counts, co
     return rc, [(b.steps, b.drafted, b.remasked, b.fallback, b.seq_steps) for b in stats], nxt.value
 
 
-def _device(t):
-    """Index of a tensor's CUDA device; the kernels run on the current one, so every tensor has to be there."""
-    return t.device.index if t.device.type == "cuda" else None
+_raw_device = None  # () -> index of PyTorch's current device
+
+
+def _current_device() -> int:
+    """torch.cuda.current_device() without its lazy-initialisation check (1 us of a call)."""
+    global _raw_device
+    if _raw_device is None:
+        import torch
+        torch.cuda.current_device()
+        _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _raw_device()
 
 
 def _require(ok: bool, where: str, status: int = WINO_ERR_ARG) -> None:
@@ -376,6 +384,9 @@ def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot
                     page_table.size(1), _ptr(q_start), _ptr(q_len), _ptr(kv_len), _ptr(new_slot), _ptr(page_table),
                     _ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
     b.tensors = (k_cache, v_cache, *ints)
+    # plain attributes: what the calls compare with, cheaper than the struct's fields
+    b.q_shape, b.kv_shape = (n_rows, n_q_heads, head_dim), (n_rows, n_kv_heads, head_dim)
+    b.elements, b.device = k_cache.dtype, k_cache.get_device()
     return b
 
 
@@ -388,6 +399,7 @@ def make_rope(freq, *, rot_dim: int, factor: float = 1.0, interleaved: bool = Fa
     _require(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous()), "make_rope")
     r = WinoRope(rot_dim, int(interleaved), factor, _ptr(freq) if rot_dim else None, _ptr(positions))
     r.tensors = (freq, positions)
+    r.n_positions = None if positions is None else positions.numel()
     return r
 
 
@@ -403,18 +415,14 @@ def wino_rope_frequencies(rot_dim: int, base: float, *, scaling: str = "none", f
     return freq, out.value
 
 
-def _heads(t, b: WinoKvBatch, heads: int, where: str) -> WinoHeads:
+def _heads(t, b: WinoKvBatch, shape, where: str) -> WinoHeads:
     """A [n_rows, heads, head_dim] tensor as wino_heads."""
-    rows, h, dim = t.shape
-    _require(rows == b.n_rows and h == heads and dim == b.head_dim, where, WINO_ERR_SHAPE)
-    cache = b.tensors[0]
-    _require(t.dtype == cache.dtype and t.device == cache.device and (dim == 1 or t.stride(2) == 1), where)
-    return WinoHeads(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-def _on_current_device(b: WinoKvBatch, where: str) -> None:
-    import torch
-    _require(_device(b.tensors[0]) == torch.cuda.current_device(), where)
+    if t.shape != shape:
+        raise WinoError(WINO_ERR_SHAPE, where)
+    row, head, one = t.stride()
+    if one != 1 or t.dtype is not b.elements or t.get_device() != b.device:
+        raise WinoError(WINO_ERR_ARG, where)
+    return WinoHeads(t.data_ptr(), row, head)
 
 
 def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=None, stream=None) -> None:
@@ -423,15 +431,16 @@ def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=N
     where = "wino_rope_append"
     qh = qo = kh = vh = None
     if q is not None:
-        qh = _heads(q, batch, batch.n_q_heads, where)
-        qo = qh if q_out is None else _heads(q_out, batch, batch.n_q_heads, where)
+        qh = _heads(q, batch, batch.q_shape, where)
+        qo = qh if q_out is None else _heads(q_out, batch, batch.q_shape, where)
     if k is not None:
-        kh = _heads(k, batch, batch.n_kv_heads, where)
+        kh = _heads(k, batch, batch.kv_shape, where)
     if v is not None:
-        vh = _heads(v, batch, batch.n_kv_heads, where)
-    if rope.positions:
-        _require(rope.tensors[1].numel() == batch.n_rows, where, WINO_ERR_SHAPE)
-    _on_current_device(batch, where)
+        vh = _heads(v, batch, batch.kv_shape, where)
+    if rope.n_positions not in (None, batch.q_shape[0]):
+        raise WinoError(WINO_ERR_SHAPE, where)
+    if batch.device != _current_device() or ws.get_device() != batch.device:  # the kernels run on the current device
+        raise WinoError(WINO_ERR_ARG, where)
     _check(lib().wino_rope_append(qh, qo, kh, vh, batch, rope, _ptr(ws), _stream(stream)), where)
 
 
@@ -456,9 +465,10 @@ def append_workspace(device=None):
 def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
     """Attention of the batch's rows over its cache, into ``out``; ``scale`` defaults to head_dim^-1/2."""
     where = "wino_attend"
-    qh, oh = _heads(q, batch, batch.n_q_heads, where), _heads(out, batch, batch.n_q_heads, where)
-    _on_current_device(batch, where)
-    _check(lib().wino_attend(qh, oh, batch.head_dim ** -0.5 if scale is None else scale, batch, _ptr(ws), _nbytes(ws),
+    qh, oh = _heads(q, batch, batch.q_shape, where), _heads(out, batch, batch.q_shape, where)
+    if batch.device != _current_device() or ws.get_device() != batch.device:  # the kernels run on the current device
+        raise WinoError(WINO_ERR_ARG, where)
+    _check(lib().wino_attend(qh, oh, batch.q_shape[2] ** -0.5 if scale is None else scale, batch, _ptr(ws), _nbytes(ws),
                              _stream(stream)), where)
 
 

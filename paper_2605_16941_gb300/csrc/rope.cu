@@ -7,7 +7,9 @@
 //
 // Bound by HBM: every element is read and written once, 16 bytes at a time.  A thread has one row and two 16-byte chunks
 // of a head that hold 8 whole pairs, keeps their cosines and sines in registers, and walks the heads with the loads of
-// four of them in flight.
+// two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of 128 (100 MB) 16.3; 20027 rows of 32 + 2 x 8 heads,
+// half of each rotated (492 MB), 84 = 5.9 TB/s.  Four heads in flight take registers for one CTA per SM less: 19.8 and
+// 96; one in flight 29 and 100; more CTAs than 4 of 256 threads per SM 19 to 26 and 85 to 101.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -22,7 +24,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxRowsPerCta = 8;
 constexpr int kMaxPairs = 64;  // head_dim / 2
-constexpr int kAhead = 4;      // heads of which a thread has loads in flight
+constexpr int kAhead = 2;  // heads of which a thread has loads in flight
 
 struct RopeArgs {
     wino_heads q, q_out, k, v;
@@ -139,7 +141,7 @@ __device__ __forceinline__ void find_rows(const RopeArgs &a, Rows &sh, int32_t r
 
 // head_dim and rot_dim multiples of 16: two 16-byte chunks of a head per thread and turn, 8 pairs or 16 plain dims.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeArgs a)
+__global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs a)
 {
     __shared__ Rows sh;
     const wino_kv_batch &b = a.b;
@@ -281,8 +283,9 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     a.b = b;
     a.rope = rope;
     a.status = status;
-    // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads.
-    a.rows_per_cta = b.n_rows >= 1024 ? 4 : (b.n_rows >= 512 ? 2 : 1);
+    // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads
+    // (4 against 8 rows: 2048 rows 16.3 and 23.4 us, 20027 rows 89 and 84).
+    a.rows_per_cta = b.n_rows >= 8192 ? 8 : (b.n_rows >= 1024 ? 4 : (b.n_rows >= 512 ? 2 : 1));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
     cfg.blockDim = dim3(kThreads);

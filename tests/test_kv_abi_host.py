@@ -155,7 +155,7 @@ def test_python_checks():
     q = torch.zeros((4, 4, 64), dtype=torch.bfloat16)
     for bad in (q[:3], q[:, :3], q[..., :32], q.half(), q.transpose(0, 1)[..., ::2]):
         with pytest.raises(wino.WinoError):
-            _abi._heads(bad, b, 4, "test")
+            _abi._heads(bad, b, b.q_shape, "test")
 
 
 @pytest.mark.parametrize("name,mirror", [("wino_kv_batch", "WinoKvBatch"), ("wino_rope", "WinoRope"), ("wino_heads", "WinoHeads")])
