@@ -1113,7 +1113,7 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
     a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
-    a.min_units = kTaskCost + 2;
+    a.min_units = kTaskCost;
     const int64_t pairs = b.n_rows / (2 * a.positions) + b.n_seq, tiles = (int64_t)b.table_width * b.page_size / kTileN + 1;
     a.wide = (double)pairs * (double)(tiles + kTaskCost) * b.n_kv_heads >= 2147483648.0;
     a.page_shift = -1;
