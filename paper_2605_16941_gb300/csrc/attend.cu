@@ -9,8 +9,9 @@
 // even and odd slot tiles instead, each with its own m, l and O, joined at the end.
 //
 // Work.  A task costs one unit per slot tile.  The units of all tasks in order are cut into equal runs, one per CTA, from
-// lengths that are read on the device; a run that starts or ends inside a task leaves its (m, l, O) in the workspace, and
-// combine_kernel joins the runs of such tasks in the order of the slots.
+// lengths that are read on the device.  The parts of a task that several runs hold are joined in a binary tree over their
+// order: of two neighbours, whichever is done first leaves its (m, l, O) in the workspace, and the other goes on with the
+// join.  No CTA waits for another, the tree does not depend on who is first, and each softmax warp joins its own rows.
 //
 // A CTA has 12 warps: two softmax warpgroups (one thread per row), and one warp each for the plan, the copies of Q and K,
 // the copies of V (TMA, one box per page and 64 dims), and the MMAs.  S lies in tensor memory, 128 columns per warpgroup;
@@ -40,35 +41,22 @@ constexpr int kSoftmaxThreads = 256;
 constexpr int kAttendThreads = kSoftmaxThreads + 128;
 constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11;
 constexpr int kMaxCtas = 160;           // an SM each
-constexpr int kRecordBytes = 32;        // SplitRecord
-constexpr int kCombineThreads = 256;
-constexpr int kSplitRows = 2 * kTileM;  // rows of a task
+constexpr int kLevels = 8;              // of the tree over the parts of a task: 2^8 >= kMaxCtas
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
 constexpr int kTaskCost = 3;            // what a task costs beside its slot tiles, in slot tiles
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 
-// What combine_kernel needs to know of the task that CTA c's run starts inside (one per CTA).
-struct alignas(16) SplitRecord {
-    int32_t last;   // CTAs first .. last hold slot tiles of it
-    int32_t first;  // -1: the run does not start inside a task, or no earlier run holds tiles of it
-    int32_t row;    // the task's first row, and its row positions (up to 2 tiles of them)
-    int32_t positions;
-    int32_t kv_head;
-    int32_t pad[3];
-};
-static_assert(sizeof(SplitRecord) == kRecordBytes, "record size");
-
 struct AttendArgs {
     wino_heads q, out;
     wino_kv_batch b;
     float scale_log2;  // scale * log2(e)
     StatusWords *status;
-    SplitRecord *records;  // [kMaxCtas]
-    float2 *part_ml;       // [kMaxCtas][2][split_rows]: m (log2 units), l
-    float4 *part_o;        // [kMaxCtas][2][DP / 4][split_rows]
-    int32_t split_rows;
+    int32_t *nodes;   // [kMaxCtas][kLevels][8 warps], zero between calls: how many of a node's two children are there
+    float2 *part_ml;  // [kMaxCtas][2][2 quarters][32 lanes]: m, l of the rows of a warp
+    float4 *part_o;   // [kMaxCtas][2][2 quarters][piece / 4][32 lanes]
+    int32_t quarters, piece;   // warps of a warpgroup with rows at most, columns that a warp keeps at most
     int32_t group, positions;  // query heads per kv head, row positions per tile
     uint32_t pair_magic;       // ceil(2^32 / (2 positions))
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
@@ -127,7 +115,7 @@ struct alignas(16) Part {
     int32_t j0, n;   // n = 0: nothing to see, the rows get zeros
     int32_t seq, kv_head;
     int32_t i0;      // the sequence's row of the first position
-    int32_t pad;
+    int32_t first, last;  // without kWhole: the CTAs whose runs hold slot tiles of the task
     SeqRows q;
 };
 
@@ -289,13 +277,11 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
     }
-    const bool starts = go;
-    U first_task = task;
 #pragma unroll 1
     while (true) {
         Part part;
         part.flags = kEnd;
-        part.kv_end = part.j0 = part.n = part.i0 = part.pad = 0;
+        part.kv_end = part.j0 = part.n = part.i0 = part.first = part.last = 0;
         if (go) {
             const int32_t slots = task_slots(a, q, pair), tiles = tiles_of(slots);
             const U tile0 = task + kTaskCost;  // a task's own cost comes before its tiles
@@ -306,6 +292,10 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             const bool to_end = part.j0 + part.n == tiles;
             part.flags = (q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
+            if ((part.flags & kWhole) == 0 && part.n > 0) {
+                part.first = cut.run_of(tile0);
+                part.last = cut.run_of(tile0 + (U)tiles - 1);
+            }
             task = tile0 + (U)tiles;
             at = task;
             go = at < end;
@@ -325,19 +315,6 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
                 ptx::mbar_arrive(ptx::smem_u32(&sh.part_full[slot]));
             }
             __syncwarp();
-            if (sent == 0 && lane == 0) {  // behind the first part: nobody in this kernel waits for the record
-                SplitRecord rec{};
-                rec.first = -1;
-                if (starts && part.j0 > 0) {
-                    const U tile0 = first_task + kTaskCost;
-                    rec.first = cut.run_of(tile0);
-                    rec.last = cut.run_of(tile0 + (U)tiles_of(part.kv_end) - 1);
-                    rec.row = q.start + part.i0;
-                    rec.positions = q.n - part.i0;
-                    rec.kv_head = kv_head;
-                }
-                a.records[c] = rec;
-            }
             ++sent;
         }
         if (last)
@@ -359,6 +336,87 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
     }
     if (!ok)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
+}
+
+// Joins this warp's rows of a part with the task's other parts: climbs the tree over parts first .. last while the other
+// child of a node is there already, and leaves what it has got where it is not.  O is in tensor memory (columns [c0, c1)
+// from t_o), m (units of S) and l in registers; true: they are the whole task's now.
+__device__ __forceinline__ bool join_parts(const AttendArgs &a, const Part &part, uint32_t t_o, int c0, int c1, int warp_piece,
+                                           int warp, int lane, float &m, float &l, float sl2)
+{
+    const int32_t n = part.last - part.first + 1;
+    int32_t i = (int32_t)blockIdx.x - part.first;  // this subtree among those of its level
+    const int64_t floats4 = a.piece / 4 * 32;
+    auto place = [&](int32_t cta) {  // where the subtree whose first part is CTA cta's lies
+        return ((int64_t)cta * 2 + (cta == part.first ? 1 : 0)) * (2 * a.quarters) + warp_piece;
+    };
+#pragma unroll 1
+    for (int level = 0; (1 << level) < n; ++level, i >>= 1) {
+        if ((i & 1) == 0 && ((i + 1) << level) >= n)
+            continue;  // no right neighbour
+        int32_t *const node = a.nodes + ((part.first + ((i & ~1) << level)) * kLevels + level) * 8 + warp;
+        int32_t there = 0;
+        if (lane == 0)
+            there = ptx::ld_acquire(node);
+        there = __shfl_sync(0xffffffffu, there, 0);
+        if (!there) {
+            const int64_t to = place(part.first + (i << level));
+            a.part_ml[to * 32 + lane] = make_float2(m, l);
+            float4 *const po = a.part_o + to * floats4 + lane;
+#pragma unroll 1
+            for (int c = c0; c < c1; c += 32) {
+                float o[32];
+                ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)c, o);
+                ptx::tmem_ld_wait(o);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4)
+                    po[(c - c0 + k) / 4 * 32] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            }
+            __threadfence();
+            __syncwarp();
+            if (lane == 0)
+                there = atomicAdd(node, 1);
+            there = __shfl_sync(0xffffffffu, there, 0);
+            if (!there)
+                return false;
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0)
+            *node = 0;  // for the next call
+        const int64_t from = place(part.first + ((i ^ 1) << level));
+        const float2 ml = __ldcg(&a.part_ml[from * 32 + lane]);
+        const float4 *const po = a.part_o + from * floats4 + lane;
+        const float big = fmaxf(m, ml.x);
+        const float f = m == -INFINITY ? 0.f : ptx::ex2((m - big) * sl2);
+        const float h = ml.x == -INFINITY ? 0.f : ptx::ex2((ml.x - big) * sl2);
+        const bool left = (i & 1) == 0;  // the sum's rounding does not depend on who joins: left child in the fma
+#pragma unroll 1
+        for (int c = c0; c < c1; c += 32) {
+            float4 y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                y[k] = __ldcg(&po[((c - c0) / 4 + k) * 32]);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t o[16];
+                ptx::tmem_ld_32x32b_x16(t_o + (uint32_t)(c + 16 * half), o);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float own = __uint_as_float(o[k]);
+                    const float4 &q = y[4 * half + k / 4];
+                    const float other = k % 4 == 0 ? q.x : (k % 4 == 1 ? q.y : (k % 4 == 2 ? q.z : q.w));
+                    o[k] = __float_as_uint(left ? fmaf(f, own, h * other) : fmaf(h, other, f * own));
+                }
+                ptx::tmem_st_32x32b_x16(t_o + (uint32_t)(c + 16 * half), o);
+            }
+        }
+        ptx::tmem_st_wait();
+        l = left ? fmaf(f, l, h * ml.y) : fmaf(h, ml.y, f * l);
+        m = big;
+    }
+    return true;
 }
 
 template <int DP, bool kBf16>
@@ -609,71 +667,84 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 c0 = g * (DP / 2);
                 c1 = c0 + DP / 2;
             }
-            const bool whole = (part.flags & kWhole) != 0;
-            const int slot_row = (two ? g * kTileM : 0) + r;
-            const int64_t to = (int64_t)blockIdx.x * 2 + (part.j0 > 0 ? 0 : 1);  // the part's place in the workspace
-            if (!whole && valid && c0 == 0)
-                a.part_ml[to * a.split_rows + slot_row] = make_float2(big * sl2, sum);
             if (any) {
-                if (whole) {  // no slot seen: zeros; NaN stays NaN
+                const uint32_t t_o = lanes + C::kTmemO + (uint32_t)(two ? g * DP : 0);
+                bool mine = true;  // this warp ends the task
+                if ((part.flags & kWhole) == 0) {
+                    if (!two) {  // O_0 becomes the joined O, in this warpgroup's columns
+#pragma unroll 1
+                        for (int c = c0; c < c1; c += 16) {
+                            uint32_t o[16], o1[16];
+                            ptx::tmem_ld_32x32b_x16(t_o + (uint32_t)c, o);
+                            if (n > 1)
+                                ptx::tmem_ld_32x32b_x16(t_o + (uint32_t)(DP + c), o1);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                const float y = __uint_as_float(o[k]) * f0;
+                                o[k] = __float_as_uint(n > 1 ? fmaf(f1, __uint_as_float(o1[k]), y) : y);
+                            }
+                            ptx::tmem_st_32x32b_x16(t_o + (uint32_t)c, o);
+                        }
+                        ptx::tmem_st_wait();
+                        f0 = 1.f;
+                        f1 = 0.f;
+                    }
+                    mine = join_parts(a, part, t_o, c0, c1, g * a.quarters + (warp & 3), warp, lane, big, sum, sl2);
+                }
+                if (mine) {  // no slot seen: zeros; NaN stays NaN
                     const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
                     f0 *= inv;
                     f1 *= inv;
-                }
-                const int head = part.kv_head * a.group + (r - pos_in_tile * a.group);
-                uint16_t *const dst = a.out.data + (int64_t)(part.q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
-                float4 *const po = a.part_o + to * (DP / 4) * a.split_rows + slot_row;
-                const uint32_t t_o = lanes + C::kTmemO + (uint32_t)(two ? g * DP : 0);
+                    const bool both = !two && n > 1 && (part.flags & kWhole) != 0;
+                    const int head = part.kv_head * a.group + (r - pos_in_tile * a.group);
+                    uint16_t *const dst =
+                        a.out.data + (int64_t)(part.q.start + i) * a.out.row_stride + (int64_t)head * a.out.head_stride;
 #pragma unroll 1
-                for (int c = c0; c < c1; c += 32) {
-                    float o[32];
-                    if (n > 0) {
-                        ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)c, o);
-                        if (!two && n > 1) {
-                            float o1[32];
-                            ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)(DP + c), o1);
-                            ptx::tmem_ld_wait(o);
-                            ptx::tmem_ld_wait(o1);
+                    for (int c = c0; c < c1; c += 32) {
+                        float o[32];
+                        if (n > 0) {
+                            ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)c, o);
+                            if (both) {
+                                float o1[32];
+                                ptx::tmem_ld_32x32b_x32(t_o + (uint32_t)(DP + c), o1);
+                                ptx::tmem_ld_wait(o);
+                                ptx::tmem_ld_wait(o1);
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                o[k] = fmaf(f1, o1[k], f0 * o[k]);
-                        } else {
-                            ptx::tmem_ld_wait(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                o[k] *= f0;
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            o[k] = 0.f;
-                    }
-                    if (!valid) {
-                    } else if (whole) {
-                        // A store covers 32 rows: 32 bytes of each where the rows are aligned for that, else 16 (an
-                        // instruction takes a cycle per row, whatever its width).
-                        uint32_t y[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            y[k] = pack2<kBf16>(o[2 * k], o[2 * k + 1]);
-#pragma unroll
-                        for (int k = 0; k < 16; k += 8) {
-                            uint16_t *const at = dst + c + 2 * k;
-                            if (a.wide_rows && c + 2 * k + 16 <= a.b.head_dim) {
-                                ptx::st_global_v8(at, &y[k]);
+                                for (int k = 0; k < 32; ++k)
+                                    o[k] = fmaf(f1, o1[k], f0 * o[k]);
                             } else {
-                                if (c + 2 * k < a.b.head_dim)
-                                    *reinterpret_cast<uint4 *>(at) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
-                                if (c + 2 * k + 8 < a.b.head_dim)
-                                    *reinterpret_cast<uint4 *>(at + 8) = make_uint4(y[k + 4], y[k + 5], y[k + 6], y[k + 7]);
+                                ptx::tmem_ld_wait(o);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    o[k] *= f0;
+                            }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                o[k] = 0.f;
+                        }
+                        if (valid) {
+                            // A store covers 32 rows: 32 bytes of each where the rows are aligned for that, else 16.
+                            uint32_t y[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                y[k] = pack2<kBf16>(o[2 * k], o[2 * k + 1]);
+#pragma unroll
+                            for (int k = 0; k < 16; k += 8) {
+                                uint16_t *const at = dst + c + 2 * k;
+                                if (a.wide_rows && c + 2 * k + 16 <= a.b.head_dim) {
+                                    ptx::st_global_v8(at, &y[k]);
+                                } else {
+                                    if (c + 2 * k < a.b.head_dim)
+                                        *reinterpret_cast<uint4 *>(at) = make_uint4(y[k], y[k + 1], y[k + 2], y[k + 3]);
+                                    if (c + 2 * k + 8 < a.b.head_dim)
+                                        *reinterpret_cast<uint4 *>(at + 8) = make_uint4(y[k + 4], y[k + 5], y[k + 6], y[k + 7]);
+                                }
                             }
                         }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            po[(int64_t)((c + k) / 4) * a.split_rows] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             }
             __syncwarp();
@@ -929,100 +1000,43 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         ptx::tmem_dealloc(tmem, kTmemAll);
     if (threadIdx.x == 0 && sh.abort)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_DEVICE_TIMEOUT);
-}
-
-// Joins the parts of the tasks that the runs' borders cut: CTA (c, y) takes a share of the task in which run c + 1 starts,
-// if that is the first border inside it.  A thread has one row and `chunks` float4 columns; the lanes are rows, as the
-// parts are stored.  Bound by latency (record, then m and l, then O): the loads of several parts are in flight at once.
-template <int DP, bool kBf16, int kChunks>
-__global__ void __launch_bounds__(kCombineThreads) combine_kernel(const AttendArgs a)
-{
-    constexpr int kColumns = kCombineThreads / 32;              // chunk columns of a CTA
-    constexpr int kShares = DP / 4 / (kColumns * kChunks);      // CTAs per 32 rows
-    ptx::grid_dep_launch_dependents();
-    ptx::grid_dep_wait();
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        a.status->last = a.status->current;
-        a.status->current = WINO_OK;
-    }
-    const int32_t c = (int32_t)blockIdx.x + 1;
-    if (c >= kMaxCtas)
-        return;
-    const SplitRecord rec = a.records[c];
-    if (rec.first != c - 1)
-        return;
-    const int slot_row = (int)(blockIdx.y / kShares) * 32 + ((int)threadIdx.x & 31);
-    const int g = slot_row / kTileM, r = slot_row % kTileM;
-    const int pos_in_tile = r / a.group, pos = g * a.positions + pos_in_tile;
-    if (pos_in_tile >= a.positions || pos >= rec.positions || slot_row >= a.split_rows)
-        return;
-    // the first part is in its CTA's second place, the others in their first
-    const int64_t stride_o = (int64_t)2 * (DP / 4) * a.split_rows;
-    const float2 *ml = a.part_ml + ((int64_t)rec.first * 2 + 1) * a.split_rows + slot_row;
-    const int chunk0 = ((int)(blockIdx.y % kShares) * kColumns + ((int)threadIdx.x >> 5)) * kChunks;
-    const float4 *po = a.part_o + (((int64_t)rec.first * 2 + 1) * (DP / 4) + chunk0) * a.split_rows + slot_row;
-    const int parts = rec.last - rec.first + 1;
-    auto ml_of = [&](int k) { return k == 0 ? ml : ml + (int64_t)(2 * k - 1) * a.split_rows; };
-    auto o_of = [&](int k) { return k == 0 ? po : po + k * stride_o - (int64_t)(DP / 4) * a.split_rows; };
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k)
-        m = fmaxf(m, ml_of(k)->x);
-    float4 o[kChunks];
-#pragma unroll
-    for (int x = 0; x < kChunks; ++x)
-        o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-        const float2 w = *ml_of(k);
-        const float f = w.x == -INFINITY ? 0.f : ptx::ex2(w.x - m);
-        l += f * w.y;
-#pragma unroll
-        for (int x = 0; x < kChunks; ++x) {
-            const float4 y = o_of(k)[(int64_t)x * a.split_rows];
-            if (f != 0.f) {  // else nothing seen in this part, or nothing left of it
-                o[x].x = fmaf(f, y.x, o[x].x);
-                o[x].y = fmaf(f, y.y, o[x].y);
-                o[x].z = fmaf(f, y.z, o[x].z);
-                o[x].w = fmaf(f, y.w, o[x].w);
-            }
+    // The last CTA publishes the outcome and clears it for the next call, and after a failure the nodes too, which parts
+    // that never came may have left.
+    int32_t failed = 0;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&a.status->finished, 1u) + 1u == gridDim.x) {
+            __threadfence();
+            failed = atomicExch(&a.status->current, (int32_t)WINO_OK);
+            a.status->last = failed;
+            a.status->finished = 0;
         }
     }
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    const int head = rec.kv_head * a.group + (r - pos_in_tile * a.group);
-    uint16_t *const dst = a.out.data + (int64_t)(rec.row + pos) * a.out.row_stride + (int64_t)head * a.out.head_stride;
-#pragma unroll
-    for (int x = 0; x < kChunks; ++x) {
-        const int col = (chunk0 + x) * 4;
-        if (col < a.b.head_dim)
-            *reinterpret_cast<uint2 *>(dst + col) =
-                make_uint2(pack2<kBf16>(o[x].x * inv, o[x].y * inv), pack2<kBf16>(o[x].z * inv, o[x].w * inv));
-    }
+    if (__syncthreads_or(failed))
+        for (int x = (int)threadIdx.x; x < kMaxCtas * kLevels * 8; x += kAttendThreads)
+            a.nodes[x] = 0;
 }
 
 // ---------------------------------------------------------------- host
 
 int32_t positions_per_tile(const wino_kv_batch &b) { return kTileM / (b.n_q_heads / b.n_kv_heads); }
 
-int32_t split_rows(const wino_kv_batch &b)
-{
-    const int32_t g = b.n_q_heads / b.n_kv_heads;
-    return b.n_rows <= positions_per_tile(b) ? (b.n_rows * g + 31) / 32 * 32 : kSplitRows;
-}
-
 struct Scratch {
-    size_t records, ml, o, total;
+    int32_t quarters, piece;
+    size_t ml, o, total;
 };
 
 Scratch scratch_layout(const wino_kv_batch &b)
 {
-    const size_t dp = b.head_dim <= 64 ? 64 : 128, rows = (size_t)split_rows(b) * 2 * kMaxCtas;
+    const int32_t dp = b.head_dim <= 64 ? 64 : 128;
+    const bool small = b.n_rows <= positions_per_tile(b);  // then no task has rows in its second tile
     Scratch s{};
-    s.records = 0;
-    s.ml = round_up(kMaxCtas * sizeof(SplitRecord), 256);
-    s.o = s.ml + rows * sizeof(float2);
-    s.total = s.o + rows * dp * sizeof(float);
+    s.quarters = small ? (b.n_rows * (b.n_q_heads / b.n_kv_heads) + 31) / 32 : 4;
+    s.piece = small ? dp / 2 : dp;
+    const size_t warps = (size_t)kMaxCtas * 2 * 2 * (size_t)s.quarters;
+    s.ml = (size_t)kMaxCtas * kLevels * 8 * sizeof(int32_t);
+    s.o = s.ml + warps * 32 * sizeof(float2);
+    s.total = s.o + warps * 32 * (size_t)s.piece * sizeof(float);
     return s;
 }
 
@@ -1079,15 +1093,7 @@ int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, 
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, attend_kernel<DP, kBf16>, tq, tk, tv, a) != cudaSuccess)
         return WINO_ERR_CUDA;
-    // Few rows: a chunk per thread; many: four, so that the CTAs (most of which find nothing to do) are resident at once.
-    const bool few = a.split_rows <= 64;
-    const int columns = kCombineThreads / 32 * (few ? 1 : DP / 32);
-    cfg.gridDim = dim3((unsigned)std::max(1, ctas - 1), (unsigned)((a.split_rows + 31) / 32 * (DP / 4 / columns)));
-    cfg.blockDim = dim3(kCombineThreads);
-    cfg.dynamicSmemBytes = 0;
-    const cudaError_t e = few ? cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16, 1>, a)
-                              : cudaLaunchKernelEx(&cfg, combine_kernel<DP, kBf16, DP / 32>, a);
-    return e == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
+    return WINO_OK;
 }
 
 }  // namespace
@@ -1104,10 +1110,11 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.b = b;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.status = status;
-    a.records = reinterpret_cast<SplitRecord *>(scratch + L.records);
+    a.nodes = reinterpret_cast<int32_t *>(scratch);
     a.part_ml = reinterpret_cast<float2 *>(scratch + L.ml);
     a.part_o = reinterpret_cast<float4 *>(scratch + L.o);
-    a.split_rows = split_rows(b);
+    a.quarters = L.quarters;
+    a.piece = L.piece;
     a.group = b.n_q_heads / b.n_kv_heads;
     a.positions = positions_per_tile(b);
     a.box_rows = std::min(b.page_size, kTileN);

@@ -200,6 +200,14 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
+// A 32-bit value that another CTA may have stored, with what it wrote before.
+__device__ __forceinline__ int32_t ld_acquire(const int32_t *p)
+{
+    int32_t v;
+    asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // 32 bytes to a 32-byte aligned global address.
 __device__ __forceinline__ void st_global_v8(void *p, const uint32_t *v)
 {
