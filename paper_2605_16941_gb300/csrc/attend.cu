@@ -44,6 +44,7 @@ constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kLevels = 8;              // of the tree over the parts of a task: 2^8 >= kMaxCtas
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
 constexpr int kTaskCost = 3;            // what a task costs beside its slot tiles, in slot tiles
+constexpr int kSnap = 2;                // a cut this near to a task's border (in slot tiles) is moved there
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
@@ -99,6 +100,12 @@ struct Cut {
         more = total - per * (U)n;
     }
     __device__ __forceinline__ U start(int32_t c) const { return (U)c * per + min((U)c, more); }
+    // A start inside the task [t0, t1), moved to the task's border where that is near: joining parts costs more than it
+    // evens out.
+    static __device__ __forceinline__ U snap(U unit, U t0, U t1)
+    {
+        return unit < t0 + kTaskCost + kSnap ? t0 : (t1 < unit + kSnap ? t1 : unit);
+    }
     __device__ __forceinline__ int32_t run_of(U unit) const
     {
         const U longer = more * (per + 1);
@@ -276,6 +283,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             }
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
+        // a start that moves to the task's end belongs to the next one, which the walk below finds
+        at = Cut<U>::snap(at, task, task + (U)(tiles_of(task_slots(a, q, pair)) + kTaskCost));
     }
 #pragma unroll 1
     while (true) {
@@ -284,27 +293,29 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         part.kv_end = part.j0 = part.n = part.i0 = part.first = part.last = 0;
         if (go) {
             const int32_t slots = task_slots(a, q, pair), tiles = tiles_of(slots);
-            const U tile0 = task + kTaskCost;  // a task's own cost comes before its tiles
+            const U tile0 = task + kTaskCost, next = tile0 + (U)tiles;  // a task's own cost comes before its tiles
+            const U stop = end >= next ? next : Cut<U>::snap(end, task, next);
             part.j0 = at > tile0 ? (int32_t)(at - tile0) : 0;
-            part.n = (end > tile0 ? (int32_t)min((U)tiles, end - tile0) : 0) - part.j0;
+            part.n = (stop > tile0 ? (int32_t)(stop - tile0) : 0) - part.j0;
             part.kv_end = slots;
             part.i0 = pair * 2 * a.positions;
-            const bool to_end = part.j0 + part.n == tiles;
+            const bool to_end = stop == next;
             part.flags = (q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
             if ((part.flags & kWhole) == 0 && part.n > 0) {
-                part.first = cut.run_of(tile0);
-                part.last = cut.run_of(tile0 + (U)tiles - 1);
+                // the cuts that stay inside the task are those of starts in [tile0 + kSnap, next - kSnap]
+                part.first = cut.run_of(tile0 + kSnap - 1);
+                part.last = cut.run_of(next - kSnap);
             }
-            task = tile0 + (U)tiles;
-            at = task;
+            task = next;
+            at = max(at, next);
             go = at < end;
         }
         part.seq = seq;
         part.kv_head = kv_head;
         part.q = q;
         const bool last = (part.flags & kEnd) != 0;
-        if (last || part.n > 0) {  // a run may end within a task's own cost
+        if (last || part.n > 0) {  // a run may hold none of a task's tiles
             if (part.kv_end == 0)
                 part.n = 0;
             const int slot = (int)(sent % kParts);
@@ -391,12 +402,20 @@ __device__ __forceinline__ bool join_parts(const AttendArgs &a, const Part &part
         const float f = m == -INFINITY ? 0.f : ptx::ex2((m - big) * sl2);
         const float h = ml.x == -INFINITY ? 0.f : ptx::ex2((ml.x - big) * sl2);
         const bool left = (i & 1) == 0;  // the sum's rounding does not depend on who joins: left child in the fma
+        float4 y[8], next[8];  // the neighbour's 32 columns at hand, and the 32 behind them on their way
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            next[k] = __ldcg(&po[k * 32]);
 #pragma unroll 1
         for (int c = c0; c < c1; c += 32) {
-            float4 y[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                y[k] = __ldcg(&po[((c - c0) / 4 + k) * 32]);
+                y[k] = next[k];
+            if (c + 32 < c1) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    next[k] = __ldcg(&po[((c + 32 - c0) / 4 + k) * 32]);
+            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t o[16];
@@ -1120,7 +1139,7 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
     a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
-    a.min_units = kTaskCost;
+    a.min_units = L.piece * L.quarters >= 256 ? 6 : 3;
     const int64_t pairs = b.n_rows / (2 * a.positions) + b.n_seq, tiles = (int64_t)b.table_width * b.page_size / kTileN + 1;
     a.wide = (double)pairs * (double)(tiles + kTaskCost) * b.n_kv_heads >= 2147483648.0;
     a.page_shift = -1;
