@@ -87,29 +87,43 @@ __device__ __forceinline__ int32_t task_slots(const AttendArgs &a, const SeqRows
 
 __device__ __forceinline__ int32_t tiles_of(int32_t slots) { return max(1, (slots + kTileN - 1) / kTileN); }
 
-// The cut of `total` units into n runs: the first `more` of them are one unit longer.  U: 32 bits unless the host finds
-// that the units may need more (64-bit arithmetic, divisions above all, is slow and much code).
+// The cut of `total` units into n runs: run c starts at unit floor(c total / n).  U: 32 bits unless the host finds that the
+// units may need more (64-bit arithmetic, divisions above all, is slow and much code).
 template <typename U>
 struct Cut {
-    U per, more;
-    int32_t n;
-    __device__ __forceinline__ Cut(U total, int32_t ctas, U min_units)
+    U total, per;
+    int32_t n, more;  // total = n per + more
+    float inv_n;
+    // Up to as many tasks as CTAs: a multiple of the tasks, so that tasks of one length are cut alike.
+    __device__ __forceinline__ Cut(U units, U tasks, int32_t ctas, U min_units) : total(units)
     {
         n = (int32_t)min((U)ctas, max((U)1, total / min_units));
+        if (tasks > 0 && tasks <= (U)n)
+            n -= n % (int32_t)tasks;
         per = total / (U)n;
-        more = total - per * (U)n;
+        more = (int32_t)(total - per * (U)n);
+        inv_n = 1.f / (float)n;
     }
-    __device__ __forceinline__ U start(int32_t c) const { return (U)c * per + min((U)c, more); }
+    // c more < 2^15 and n <= 160: the quotient's distance from an integer, at least 1 / (2 n), is far above its rounding
+    __device__ __forceinline__ U start(int32_t c) const
+    {
+        return (U)c * per + (U)(int32_t)(((float)(c * more) + 0.5f) * inv_n);
+    }
+    // The run that holds a unit: off by one at most from the quotient in fp32.
+    __device__ __forceinline__ int32_t run_of(U unit) const
+    {
+        int32_t c = min(n - 1, (int32_t)((float)unit * ((float)n / (float)total)));
+        while (start(c) > unit)
+            --c;
+        while (c + 1 < n && start(c + 1) <= unit)
+            ++c;
+        return c;
+    }
     // A start inside the task [t0, t1), moved to the task's border where that is near: joining parts costs more than it
     // evens out.
     static __device__ __forceinline__ U snap(U unit, U t0, U t1)
     {
         return unit < t0 + kTaskCost + kSnap ? t0 : (t1 < unit + kSnap ? t1 : unit);
-    }
-    __device__ __forceinline__ int32_t run_of(U unit) const
-    {
-        const U longer = more * (per + 1);
-        return (int32_t)(unit < longer ? unit / (per + 1) : more + (unit - longer) / per);
     }
 };
 
@@ -213,7 +227,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         width >>= 1;
     const int per_round = 32 / width, sub = lane & (width - 1);
     SeqRows q;
-    U mine = 0;  // units of this lane's sequence, of one kv head
+    U mine = 0;           // units of this lane's sequence, of one kv head
+    int32_t n_pairs = 0;  // and its tasks
     auto load_round = [&](int32_t s0) {
         const int32_t s = s0 + lane / width;
         q.n = 0;
@@ -222,24 +237,26 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             q = load_seq(a.b, s);
         ok = ok && q.ok;
         U u = 0;
-        const int32_t n_pairs = q.n > 0 ? pairs_of(a, q) : 0;
+        const int32_t n_pairs_of_lane = q.n > 0 ? pairs_of(a, q) : 0;
 #pragma unroll 1
-        for (int32_t p = sub; p < n_pairs; p += width)
+        for (int32_t p = sub; p < n_pairs_of_lane; p += width)
             u += (U)(tiles_of(task_slots(a, q, p)) + kTaskCost);
         mine = warp_sum(u, width);
+        n_pairs = n_pairs_of_lane;
     };
-    U total = 0;
+    U total = 0, tasks = 0;
 #pragma unroll 1
     for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
         load_round(s0);
         total += warp_sum(sub == 0 ? mine : (U)0, 32);
+        tasks += warp_sum(sub == 0 ? (U)n_pairs : (U)0, 32);
     }
     total *= (U)n_kv;
-    const Cut<U> cut(total, (int32_t)gridDim.x, (U)a.min_units);
+    const Cut<U> cut(total, tasks * (U)n_kv, (int32_t)gridDim.x, (U)a.min_units);
     const int32_t c = (int32_t)blockIdx.x;
     U at = cut.start(c);  // the next unit to hand out
     const U end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
-    int32_t seq = 0, kv_head = 0, pair = 0, n_pairs = 0;
+    int32_t seq = 0, kv_head = 0, pair = 0;
     U task = 0;  // the unit at which the current task starts
     uint32_t sent = 0;
     bool go = at < end;
@@ -247,7 +264,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         // the sequence that holds unit `at`
         U before = 0;
 #pragma unroll 1
-        for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
+        for (int32_t s0 = 0; s0 < n_seq && n_seq > 1; s0 += per_round) {  // one sequence: every lane has it
             if (n_seq > per_round)
                 load_round(s0);
             const U pre = warp_scan(sub == 0 ? mine * (U)n_kv : (U)0, lane);
@@ -261,6 +278,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
                 q.n = __shfl_sync(0xffffffffu, q.n, src);
                 q.kv = __shfl_sync(0xffffffffu, q.kv, src);
                 q.base = __shfl_sync(0xffffffffu, q.base, src);
+                n_pairs = __shfl_sync(0xffffffffu, n_pairs, src);
                 break;
             }
             before += __shfl_sync(0xffffffffu, pre, 31);
@@ -268,9 +286,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         // its kv head, and by the sum over 32 tasks at a time the task
         kv_head = (int32_t)((at - task) / mine);
         task += (U)kv_head * mine;
-        n_pairs = pairs_of(a, q);
 #pragma unroll 1
-        for (int32_t p0 = 0; p0 < n_pairs; p0 += 32) {
+        for (int32_t p0 = 0; p0 < n_pairs && n_pairs > 1; p0 += 32) {
             const int32_t p = p0 + lane;
             const U cost = p < n_pairs ? (U)(tiles_of(task_slots(a, q, p)) + kTaskCost) : (U)0;
             const U pre = warp_scan(cost, lane);
@@ -569,11 +586,16 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                     if (__any_sync(0xffffffffu, valid && (lim < kTileN || (hole >= 0 && hole < kTileN)))) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                        for (int c = 0; c < 4; ++c) {  // bit k: the row sees column 32 c + k
+                            const int here = lim - 32 * c, not_here = hole - 32 * c;
+                            uint32_t seen = here >= 32 ? 0xffffffffu : (here > 0 ? (1u << here) - 1u : 0u);
+                            if (not_here >= 0 && not_here < 32)
+                                seen &= ~(1u << not_here);
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                if (32 * c + k >= lim || 32 * c + k == hole)
+                                if ((seen & (1u << k)) == 0)
                                     x[c][k] = -INFINITY;
+                        }
                     }
                     float y[8];
 #pragma unroll
