@@ -48,6 +48,12 @@ constexpr int kSnap = 2;                // a cut this near to a task's border (i
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
+// Where slot row r, dims 64 h .. 64 h + 63 of a K or V tile lie: (r / 8) group + h half + (r % 8) 128 bytes.  With 128 dims
+// one copy brings both halves of a page's rows, interleaved by groups of 8 rows, if the cache's strides let one
+// coordinate of the tensor map count heads and pages (`joint`); else each half has a copy and a block of its own.
+struct TileLayout {
+    uint32_t group, half;
+};
 
 struct AttendArgs {
     wino_heads q, out;
@@ -65,6 +71,9 @@ struct AttendArgs {
     int32_t wide;              // units may need 64 bits
     int32_t wide_rows;         // rows of out are 32-byte aligned
     int32_t page_shift;        // log2(page_size), or -1
+    int32_t joint;             // heads per page in the tensor map's last coordinate, page * joint + head; 0: two coordinates
+    int32_t end;               // a coordinate behind the cache's last page
+    TileLayout tile;
 };
 
 // Tasks of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256, so that the product with
@@ -822,7 +831,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             uint32_t issued = 0;  // slots filled so far
             uint32_t parts = 0;   // parts whose Q was loaded
             bool aborted = false;
-            const int box = lane / kHalves, half = lane % kHalves;  // this lane's copy of a slot tile
+            const int halves = a.joint ? 1 : kHalves;                // copies per page
+            const int box = lane / halves, half = lane % halves;  // this lane's copy of a slot tile
             while (!aborted && __all_sync(0xffffffffu, next_part())) {
                 const Part part = sh.parts[reader.slot()];
                 __syncwarp();
@@ -869,7 +879,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     int32_t page = __shfl_sync(0xffffffffu, near, (entry - window) & 31);
                     if ((uint32_t)page >= (uint32_t)a.b.n_pages) {
                         ok = ok && box >= boxes;
-                        page = a.b.n_pages;  // a bad entry: behind the cache, read as zeros
+                        page = -1;  // a bad entry: behind the cache, read as zeros
                     }
                     if (!warp_wait(empty(slot), phase ^ 1u, &sh.abort)) {
                         aborted = true;
@@ -878,9 +888,16 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     if (lane == 0)
                         ptx::mbar_arrive_expect_tx(full(slot), (uint32_t)(boxes * kHalves * a.box_rows) * 128u);
                     __syncwarp();
-                    if (box < boxes)
-                        ptx::tma_load_4d(slot_addr(slot) + (uint32_t)half * kHalfBytes + (uint32_t)(box * a.box_rows) * 128u,
-                                         map, full(slot), half * 64, at - entry * a.b.page_size, part.kv_head, page);
+                    if (box < boxes) {
+                        const uint32_t dst = slot_addr(slot) + (uint32_t)half * a.tile.half +
+                                             (uint32_t)(box * a.box_rows / 8) * a.tile.group;
+                        const int32_t in_page = at - entry * a.b.page_size;
+                        if (a.joint)
+                            ptx::tma_load_5d(dst, map, full(slot), 0, 0, 0, in_page >> 3,
+                                             page < 0 ? a.end : page * a.joint + part.kv_head);
+                        else
+                            ptx::tma_load_4d(dst, map, full(slot), half * 64, in_page, part.kv_head, page < 0 ? a.end : page);
+                    }
                     __syncwarp();
                     ++issued;
                     if (is_v && t == n - 1 && (part.flags & kTail) != 0) {
@@ -892,8 +909,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         uint8_t *const v = smem_raw + (slot_addr(slot) - raw);
                         for (int x = (part.kv_end & (kTileN - 1)) * 8 + lane; x < kTileN * 8; x += 32)
 #pragma unroll
-                            for (int h = 0; h < kHalves; ++h)
-                                *reinterpret_cast<uint4 *>(v + h * kHalfBytes + x * 16) = make_uint4(0, 0, 0, 0);
+                            for (int h = 0; h < kHalves; ++h)  // 8 pieces of 16 bytes per row, 64 per group
+                                *reinterpret_cast<uint4 *>(v + (x >> 6) * a.tile.group + h * a.tile.half + (x & 63) * 16) =
+                                    make_uint4(0, 0, 0, 0);
                         ptx::fence_proxy_async();
                         __syncwarp();
                         if (lane == 0)
@@ -933,12 +951,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         ptx::tc_fence_after();
                     }
                     const uint64_t da = ptx::sdesc_kmajor_sw128(sq + (uint32_t)qt * C::kTileBytes);
-                    const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks));
+                    const uint64_t db = ptx::sdesc_kmajor_sw128(slot_addr(ks), a.tile.group);
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const uint64_t off = (uint64_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
-                        ptx::mma_bf16(tmem + C::kTmemS + (uint32_t)g * kTileN, da + off, db + off, id_s, k != 0);
-                    }
+                    for (int k = 0; k < DP / 16; ++k)
+                        ptx::mma_bf16(tmem + C::kTmemS + (uint32_t)g * kTileN,
+                                      da + (uint64_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2),
+                                      db + (uint64_t)((k >> 2) * (a.tile.half >> 4) + (k & 3) * 2), id_s, k != 0);
                     ptx::mma_commit(s_full(g));
                     return true;
                 };
@@ -946,7 +964,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                 // P V but the next scores; with S free early, at once); zeros: V's slots behind
                 // the last one are zeroed first
                 auto values = [&](int g, int vs, bool add, bool zeros) -> bool {
-                    const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), kHalfBytes);
+                    const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), a.tile.half, a.tile.group);
                     uint32_t &count = g ? n_p1 : n_p0;
                     const uint32_t parity = count++ & 1u;
 #pragma unroll
@@ -963,7 +981,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             ptx::tc_fence_after();
                         }
                         ptx::mma_f16_ts(tmem + C::kTmemO + (uint32_t)(g * DP), tmem + C::kTmemP + (uint32_t)g * C::kStrideP + (uint32_t)(k * 8),
-                                        db + (uint64_t)(k * (2048 >> 4)), id_o, (add || k != 0) ? 1u : 0u);
+                                        db + (uint64_t)(k * (a.tile.group >> 3)), id_o, (add || k != 0) ? 1u : 0u);
                     }
                     ptx::mma_commit(o_done(g));
                     return true;
@@ -1088,8 +1106,8 @@ int encode(CUtensorMap *m, int32_t dtype, const void *ptr, int rank, const int64
     auto fn = encode_fn();
     if (!fn)
         return WINO_ERR_CUDA;
-    cuuint64_t d[4], st[3];
-    cuuint32_t bx[4], es[4] = {1, 1, 1, 1};
+    cuuint64_t d[5], st[4];
+    cuuint32_t bx[5], es[5] = {1, 1, 1, 1, 1};
     for (int i = 0; i < rank; ++i) {
         d[i] = (cuuint64_t)dims[i];
         bx[i] = (cuuint32_t)box[i];
@@ -1173,14 +1191,43 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     CUtensorMap tq, tk, tv;
     const int64_t q_dims[3] = {b.head_dim, b.n_q_heads, b.n_rows}, q_strides[3] = {1, q.head_stride, q.row_stride};
     const int32_t q_box[3] = {64, a.group, a.positions};
-    const int64_t kv_dims[4] = {b.head_dim, b.page_size, b.n_kv_heads, b.n_pages};
-    const int64_t kv_strides[4] = {1, b.slot_stride, b.head_stride, b.page_stride};
-    const int32_t kv_box[4] = {64, a.box_rows, 1, 1};
     int rc;
-    if ((rc = encode(&tq, b.dtype, q.data, 3, q_dims, q_strides, q_box)) != WINO_OK ||
-        (rc = encode(&tk, b.dtype, b.k_cache, 4, kv_dims, kv_strides, kv_box)) != WINO_OK ||
-        (rc = encode(&tv, b.dtype, b.v_cache, 4, kv_dims, kv_strides, kv_box)) != WINO_OK)
+    if ((rc = encode(&tq, b.dtype, q.data, 3, q_dims, q_strides, q_box)) != WINO_OK)
         return rc;
+    // Heads and pages in one coordinate: pages a whole number of heads apart, every index below 2^31.  Only at 128 dims:
+    // the map's inner extents are whole halves, and a narrower head's second half would run into its neighbour.
+    int64_t per_page = 0, joint_stride = b.head_stride;
+    if (b.n_kv_heads == 1) {
+        per_page = 1;
+        joint_stride = b.page_stride;
+    } else if (b.n_pages == 1) {
+        per_page = b.n_kv_heads;
+    } else if (b.page_stride % b.head_stride == 0) {
+        per_page = b.page_stride / b.head_stride;
+    }
+    const int64_t last = (b.n_pages - 1) * per_page + b.n_kv_heads;
+    const bool joint = b.head_dim == 128 && per_page > 0 && last < (int64_t(1) << 31) - 1 && b.slot_stride < (int64_t(1) << 35);
+    a.joint = joint ? (int32_t)per_page : 0;
+    a.end = joint ? (int32_t)last : b.n_pages;
+    a.tile = joint ? TileLayout{2048u, 1024u} : TileLayout{1024u, kHalfBytes};
+    for (int i = 0; i < 2; ++i) {
+        CUtensorMap *const m = i ? &tv : &tk;
+        const uint16_t *const cache = i ? b.v_cache : b.k_cache;
+        if (joint) {
+            const int64_t dims[5] = {64, 8, 2, b.page_size / 8, last};
+            const int64_t strides[5] = {1, b.slot_stride, 64, 8 * b.slot_stride,
+                                        joint_stride};
+            const int32_t box[5] = {64, 8, 2, a.box_rows / 8, 1};
+            rc = encode(m, b.dtype, cache, 5, dims, strides, box);
+        } else {
+            const int64_t dims[4] = {b.head_dim, b.page_size, b.n_kv_heads, b.n_pages};
+            const int64_t strides[4] = {1, b.slot_stride, b.head_stride, b.page_stride};
+            const int32_t box[4] = {64, a.box_rows, 1, 1};
+            rc = encode(m, b.dtype, cache, 4, dims, strides, box);
+        }
+        if (rc != WINO_OK)
+            return rc;
+    }
     const int ctas = std::min(sm_count, kMaxCtas);
     if (b.head_dim <= 64)
         return b.dtype == WINO_BF16 ? launch<64, true>(tq, tk, tv, a, ctas, stream)

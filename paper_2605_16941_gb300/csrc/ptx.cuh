@@ -278,7 +278,7 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
         : "memory");
 }
 
-// 3-D and 4-D forms without a cache hint, innermost coordinate first.
+// 3-D to 5-D forms without a cache hint, innermost coordinate first.
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int32_t c0, int32_t c1,
                                             int32_t c2)
 {
@@ -296,6 +296,16 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *m, 
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
         " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int32_t c0, int32_t c1,
+                                            int32_t c2, int32_t c3, int32_t c4)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
         : "memory");
 }
 
@@ -477,15 +487,15 @@ __device__ __forceinline__ void tmem_ld_wait(float (&x)[32])
 // 128-byte swizzling: rows of 64 elements (128 B), 8-row swizzle atoms of
 // 1024 B stacked along M/N.  Fields: start address >> 4 (bits 0-13), leading
 // byte offset >> 4 (bits 16-29; unused for swizzled K-major), stride byte
-// offset >> 4 (bits 32-45) = 1024 B between 8-row groups, descriptor version
+// offset >> 4 (bits 32-45) = 1024 B (or `group`) between 8-row groups, descriptor version
 // 1 (bits 46-47), base offset 0 (tile bases are 1024-B aligned), layout type
 // 2 = 128-byte swizzle (bits 61-63).
-__device__ __forceinline__ uint64_t sdesc_kmajor_sw128(uint32_t smem_addr)
+__device__ __forceinline__ uint64_t sdesc_kmajor_sw128(uint32_t smem_addr, uint32_t group = 1024u)
 {
     uint64_t d = 0;
     d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
     d |= static_cast<uint64_t>(1u) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
+    d |= static_cast<uint64_t>(group >> 4) << 32;
     d |= static_cast<uint64_t>(1u) << 46;
     d |= static_cast<uint64_t>(2u) << 61;
     return d;
@@ -500,14 +510,14 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(uint32_t M, uint32_t N)
 }
 
 // Shared-memory matrix descriptor for an MN-major 16-bit tile written by TMA with 128-byte swizzling: K rows of 64
-// M/N elements (128 B), 8-row atoms of 1024 B stacked along K (stride byte offset), and `mn_stride` bytes from one
-// block of 64 M/N elements to the next (leading byte offset).  The other fields as above.
-__device__ __forceinline__ uint64_t sdesc_mnmajor_sw128(uint32_t smem_addr, uint32_t mn_stride)
+// M/N elements (128 B), 8-row atoms of 1024 B `group` bytes apart along K (stride byte offset), and `mn_stride` bytes
+// from one block of 64 M/N elements to the next (leading byte offset).  The other fields as above.
+__device__ __forceinline__ uint64_t sdesc_mnmajor_sw128(uint32_t smem_addr, uint32_t mn_stride, uint32_t group)
 {
     uint64_t d = 0;
     d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
     d |= static_cast<uint64_t>(mn_stride >> 4) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
+    d |= static_cast<uint64_t>(group >> 4) << 32;
     d |= static_cast<uint64_t>(1u) << 46;
     d |= static_cast<uint64_t>(2u) << 61;
     return d;

@@ -259,3 +259,27 @@ def test_few_rows_over_large_pages(dim):
     for n in (257, 300, 385, 513, 700, 1500):
         for rows in (1, 3, 40):
             run(add_rows(make_kv(FULL, [(rows, n, 0)], dim=dim, page=128, layout="heads", seed=n)))
+
+
+@pytest.mark.parametrize("kv_heads", [1, 3])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("layout", ["slots", "heads", "head_major", "odd"])
+def test_cache_strides(layout, page, kv_heads):
+    """Caches of 128 dims whose pages are a whole number of heads apart, and such as are not."""
+    c = make_kv(CAUSAL, [(3, 300, 297), (1, 77, 76)], heads=2 * kv_heads, kv_heads=kv_heads, dim=128, page=page)
+    P, S, H, D = c.k_cache.shape
+    caches = []
+    for t in (c.k_cache, c.v_cache):
+        if layout == "heads":
+            new = torch.empty((P, H, S, D), dtype=BF, device="cuda").transpose(1, 2)
+        elif layout == "head_major":  # all pages of a head together
+            new = torch.empty((H, P, S, D), dtype=BF, device="cuda").permute(1, 2, 0, 3)
+        elif layout == "odd":  # gaps of 8 elements behind heads, of 24 behind slots, of 40 behind pages
+            st = (S * (H * (D + 8) + 24) + 40, H * (D + 8) + 24, D + 8, 1)
+            new = torch.empty(P * st[0], dtype=BF, device="cuda").as_strided((P, S, H, D), st)
+        else:
+            new = torch.empty_like(t)
+        caches.append(new.copy_(t))
+    c.k_cache, c.v_cache = caches
+    c.batch = wino.make_kv_batch(*caches, c.table_dev, *c.ints, n_rows=c.n_rows, n_q_heads=c.heads, mask=CAUSAL)
+    run(add_rows(c))
