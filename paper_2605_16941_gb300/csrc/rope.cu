@@ -5,8 +5,8 @@
 // radians).  f / 2 pi is taken to a 64-bit fixed-point fraction of a turn once per CTA and pair; its product with the
 // position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.
 //
-// Bound by HBM: every element is read and written once, 16 bytes at a time.  A thread has one row and two 16-byte chunks
-// of a head that hold 8 whole pairs, keeps their cosines and sines in registers, and walks the heads with the loads of
+// Bound by HBM: every element is read and written once, 16 bytes at a time (8 where head_dim or rot_dim is no multiple of
+// 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in registers, and walks the heads with the loads of
 // two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of 128 (100 MB) 16.3; 20027 rows of 32 + 2 x 8 heads,
 // half of each rotated (492 MB), 84 = 5.9 TB/s.  Four heads in flight take registers for one CTA per SM less: 19.8 and
 // 96; one in flight 29 and 100; more CTAs than 4 of 256 threads per SM 19 to 26 and 85 to 101.
@@ -139,8 +139,20 @@ __device__ __forceinline__ void find_rows(const RopeArgs &a, Rows &sh, int32_t r
     __syncthreads();
 }
 
-// head_dim and rot_dim multiples of 16: two 16-byte chunks of a head per thread and turn, 8 pairs or 16 plain dims.
-template <typename T>
+// Chunks of kWords 32-bit words; head_dim and rot_dim multiples of two chunks: two chunks of a head per thread and turn, which
+// hold whole pairs, or plain dims.
+template <int kWords>
+struct Chunk;
+template <>
+struct Chunk<4> {
+    using type = uint4;
+};
+template <>
+struct Chunk<2> {
+    using type = uint2;
+};
+
+template <typename T, int kWords>
 __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs a)
 {
     __shared__ Rows sh;
@@ -150,28 +162,30 @@ __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs
     ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();
     find_rows(a, sh, row0, n_rows);
-    const int items = b.head_dim >> 4, turned = a.rope.rot_dim >> 4;  // of a head
+    using V = typename Chunk<kWords>::type;
+    constexpr int kDims = 4 * kWords;  // of two chunks
+    const int items = b.head_dim / kDims, turned = a.rope.rot_dim / kDims;  // of a head
     const int lanes = items * a.rows_per_cta;                         // (row, item) pairs of the CTA
     const int slots = kThreads / lanes;                               // heads at a time
     const int tid = (int)threadIdx.x, r = tid % lanes / items, j = tid % items, h0 = tid / lanes;
     if (h0 >= slots || r >= n_rows || sh.seq[r] < 0)
         return;
-    // the item's chunks, in units of 16 bytes: halves j and j + rot / 16, or neighbours
+    // the item's chunks: halves j and j + turned, or neighbours
     const bool turns = j < turned;
     const int c0 = turns && !a.rope.interleaved ? j : 2 * j;
     const int c1 = turns && !a.rope.interleaved ? j + turned : 2 * j + 1;
-    float2 cs[8];
+    float2 cs[2 * kWords];
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        cs[k] = turns ? sh.cs[r][8 * j + k] : make_float2(0.f, 0.f);
+    for (int k = 0; k < 2 * kWords; ++k)
+        cs[k] = turns ? sh.cs[r][2 * kWords * j + k] : make_float2(0.f, 0.f);
     const int64_t row = row0 + r;
     auto walk = [&](const uint16_t *src, int64_t src_stride, uint16_t *dst, int64_t dst_stride, int heads, bool rotate) {
         for (int h = h0; h < heads; h += kAhead * slots) {
-            uint4 x[kAhead], y[kAhead];
+            V x[kAhead], y[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
                 if (h + u * slots < heads) {
-                    const uint4 *p = reinterpret_cast<const uint4 *>(src + (h + u * slots) * src_stride);
+                    const V *p = reinterpret_cast<const V *>(src + (h + u * slots) * src_stride);
                     x[u] = p[c0];
                     y[u] = p[c1];
                 }
@@ -182,15 +196,15 @@ __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs
                         uint32_t *const v = &x[u].x, *const w = &y[u].x;
                         if (a.rope.interleaved) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
+                            for (int k = 0; k < kWords; ++k) {
                                 const float2 p = turn(to_f<T>((uint16_t)v[k]), to_f<T>((uint16_t)(v[k] >> 16)), cs[k]);
-                                const float2 q = turn(to_f<T>((uint16_t)w[k]), to_f<T>((uint16_t)(w[k] >> 16)), cs[4 + k]);
+                                const float2 q = turn(to_f<T>((uint16_t)w[k]), to_f<T>((uint16_t)(w[k] >> 16)), cs[kWords + k]);
                                 v[k] = pack2<T>(p.x, p.y);
                                 w[k] = pack2<T>(q.x, q.y);
                             }
                         } else {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
+                            for (int k = 0; k < kWords; ++k) {
                                 const float2 p = turn(to_f<T>((uint16_t)v[k]), to_f<T>((uint16_t)w[k]), cs[2 * k]);
                                 const float2 q = turn(to_f<T>((uint16_t)(v[k] >> 16)), to_f<T>((uint16_t)(w[k] >> 16)), cs[2 * k + 1]);
                                 v[k] = pack2<T>(p.x, q.x);
@@ -198,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs
                             }
                         }
                     }
-                    uint4 *const d = reinterpret_cast<uint4 *>(dst + (h + u * slots) * dst_stride);
+                    V *const d = reinterpret_cast<V *>(dst + (h + u * slots) * dst_stride);
                     d[c0] = x[u];
                     d[c1] = y[u];
                 }
@@ -295,11 +309,15 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    const bool bf16 = b.dtype == WINO_BF16;
     if (b.head_dim % 16 == 0 && rope.rot_dim % 16 == 0)
-        return b.dtype == WINO_BF16 ? cudaLaunchKernelEx(&cfg, rope_append_kernel<__nv_bfloat16>, a)
-                                    : cudaLaunchKernelEx(&cfg, rope_append_kernel<__half>, a);
-    return b.dtype == WINO_BF16 ? cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__nv_bfloat16>, a)
-                                : cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__half>, a);
+        return bf16 ? cudaLaunchKernelEx(&cfg, rope_append_kernel<__nv_bfloat16, 4>, a)
+                    : cudaLaunchKernelEx(&cfg, rope_append_kernel<__half, 4>, a);
+    if (rope.rot_dim % 8 == 0)  // and so is head_dim
+        return bf16 ? cudaLaunchKernelEx(&cfg, rope_append_kernel<__nv_bfloat16, 2>, a)
+                    : cudaLaunchKernelEx(&cfg, rope_append_kernel<__half, 2>, a);
+    return bf16 ? cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__nv_bfloat16>, a)
+                : cudaLaunchKernelEx(&cfg, rope_append_any_kernel<__half>, a);
 }
 
 }  // namespace wino
