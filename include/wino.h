@@ -281,8 +281,8 @@ WINO_API int wino_step_static_scratch(const uint16_t *H, const uint16_t *W, int6
  * blocks first_block .. n_blocks-1 are decoded left to right, block b starting
  * at position p->blk_start + b * p->blk_len; each block is stepped with
  * wino_step until none of its positions is MASK in any sequence.  The
- * hidden states of every step come from the caller (the transformer forward
- * with the shadow-block attention mask is outside this library):
+ * hidden states of every step come from the caller, who runs the transformer's
+ * layers (wino_rope_append and wino_attend are their attention):
  *   hidden(user, k, blk_start) returns the device bf16 rows of global step k
  *   for the block at blk_start, laid out as wino_step's H, and must stay
  *   valid until the next call of `hidden` or the return of wino_decode;
@@ -458,8 +458,10 @@ WINO_API int wino_rope_append(const wino_heads *q, const wino_heads *q_out, cons
 
 /*
  * Workspace of wino_attend for this batch: status words and room for the parts
- * of rows whose slots are spread over several CTAs.  Depends on the heads, the
- * head dim and (below 256 rows times heads) n_rows only, on no length.
+ * of rows whose slots are spread over several CTAs (up to 43 MB).  Depends on
+ * the heads, the head dim and, up to 128 rows times heads of a kv head, on
+ * n_rows, on no length; it serves every batch of the same heads and dim with no
+ * more rows.
  */
 WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
 

@@ -8,15 +8,17 @@ finishes the block.  The
 only device-to-host traffic per step is the [n_seq, 3] counts array, read to
 decide whether the block is finished (plus the token state when a trajectory
 is recorded).  The hidden states of each step come
-from a caller-supplied function (the transformer forward with the
-shadow-block attention mask is outside this library).
+from a caller-supplied function that runs the transformer's layers;
+``BlockCache`` gives it the paged cache, the rotation and the attention
+under the shadow-block mask that those layers need.
 """
 from __future__ import annotations
 
 from dataclasses import dataclass, field
 from typing import Callable
 
-from ._abi import (WINO_ERR_MAX_STEPS, WINO_OK, WinoError, make_params, wino_decode, wino_step,
+from ._abi import (WINO_ERR_MAX_STEPS, WINO_MASK_FULL, WINO_MASK_SHADOW, WINO_OK, WinoError, WinoKvBatch, WinoRope,
+                   attend_workspace, make_kv_batch, make_params, wino_attend, wino_decode, wino_rope_append, wino_step,
                    wino_workspace_size_step)
 
 
@@ -205,3 +207,65 @@ def decode_native(W, tokens, *, prompt_len: int, blk_len: int, n_blocks: int, ta
     stats.total_steps = nxt - start_step
     stats.next_step = nxt
     return stats
+
+
+class BlockCache:
+    """The paged key and value caches of a decode's layers, for ``hidden`` functions of ``decode`` and ``decode_native``.
+
+    Every sequence has room for ``seq_len`` slots, one per position, and behind them for the shadow block's ``blk_len``.
+    ``context(start, end)`` describes the rows of positions start .. end - 1 of every sequence, [s][position], which see
+    each other and everything before them: the prompt, or a block that is done, taken into the cache once.
+    ``step(blk_start)`` describes the rows of a step as ``wino_step`` wants their hidden states, [s][kind][l] (with
+    ``no_shadow`` [s][l]): block rows see the context and the block, shadow rows these and the shadow block but for the
+    position that they verify (Sec. 4.2.2).  Within a layer, ``append`` rotates q (in place) and stores k and v, then
+    ``attend`` reads what the rows see.  Calls on one stream at a time: the layers share a workspace.
+    """
+
+    def __init__(self, n_layers: int, n_seq: int, seq_len: int, blk_len: int, n_q_heads: int, n_kv_heads: int,
+                 head_dim: int, *, page_size: int = 64, dtype=None, device="cuda", no_shadow: bool = False):
+        import torch
+        self.n_layers, self.n_seq, self.seq_len, self.blk_len = n_layers, n_seq, seq_len, blk_len
+        self.n_q_heads, self.no_shadow = n_q_heads, no_shadow
+        width = -(-(seq_len + blk_len) // page_size)
+        shape = (n_layers, n_seq * width, n_kv_heads, page_size, head_dim)
+        dtype = torch.bfloat16 if dtype is None else dtype
+        self.k, self.v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        self.page_table = torch.arange(n_seq * width, dtype=torch.int32, device=device).view(n_seq, width)
+        self._ws = None
+
+    def _batches(self, rows: int, kv_len: int, new_slot: int, mask: int) -> list[WinoKvBatch]:
+        import torch
+        ints = torch.empty((4, self.n_seq), dtype=torch.int32, device=self.page_table.device)
+        torch.arange(0, self.n_seq * rows, rows, dtype=torch.int32, device=ints.device, out=ints[0])
+        for i, x in enumerate((rows, kv_len, new_slot)):
+            ints[i + 1].fill_(x)
+        return [make_kv_batch(self.k[i].transpose(1, 2), self.v[i].transpose(1, 2), self.page_table, *ints,
+                              n_rows=self.n_seq * rows, n_q_heads=self.n_q_heads, mask=mask)
+                for i in range(self.n_layers)]
+
+    def context(self, start: int, end: int) -> list[WinoKvBatch]:
+        """Per layer, the batch of positions [start, end)."""
+        if not 0 <= start < end <= self.seq_len:
+            raise ValueError(f"positions [{start}, {end}) of {self.seq_len}")
+        return self._batches(end - start, end, start, WINO_MASK_FULL)
+
+    def step(self, blk_start: int) -> list[WinoKvBatch]:
+        """Per layer, the batch of a step on the block at ``blk_start``."""
+        end = blk_start + self.blk_len
+        if not 0 <= blk_start or end > self.seq_len:
+            raise ValueError(f"block [{blk_start}, {end}) of {self.seq_len}")
+        if self.no_shadow:
+            return self._batches(self.blk_len, end, blk_start, WINO_MASK_FULL)
+        return self._batches(2 * self.blk_len, end, blk_start, WINO_MASK_SHADOW)
+
+    def _workspace(self, batch: WinoKvBatch):
+        # the batches of one cache differ in their rows alone; a workspace of many rows serves fewer too
+        if self._ws is None or self._ws[0] < batch.n_rows:
+            self._ws = (batch.n_rows, attend_workspace(batch))
+        return self._ws[1]
+
+    def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope, stream=None) -> None:
+        wino_rope_append(q, k, v, batch, rope, self._workspace(batch), stream=stream)
+
+    def attend(self, q, out, batch: WinoKvBatch, *, scale: float | None = None, stream=None) -> None:
+        wino_attend(q, out, batch, self._workspace(batch), scale=scale, stream=stream)
