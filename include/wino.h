@@ -473,9 +473,12 @@ WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
  *   q, out  [n_rows, n_q_heads, head_dim]; out shares no element with q or the
  *           cache
  *   scale   finite, > 0 (commonly head_dim^-1/2)
- *   ws      256-byte aligned, zero-filled before its first use; calls that may
- *           overlap on the GPU need workspaces of their own
- * The result does not depend on the order in which CTAs run.
+ *   ws      256-byte aligned, zero-filled before its first use, used by
+ *           wino_attend and wino_rope_append only; calls that may overlap on
+ *           the GPU need workspaces of their own
+ * The result does not depend on the order in which CTAs run.  WINO_ERR_SHAPE
+ * also for sizes at which the work could not be counted in 62 bits (n_seq
+ * times n_rows times slots beyond any real batch).
  */
 WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b, void *ws,
                          size_t ws_bytes, void *stream);

@@ -14,9 +14,19 @@
 // join.  No CTA waits for another, the tree does not depend on who is first, and each softmax warp joins its own rows.
 //
 // A CTA has 12 warps: two softmax warpgroups (one thread per row), and one warp each for the plan, the copies of Q and K,
-// the copies of V (TMA, one box per page and 64 dims), and the MMAs.  S lies in tensor memory, 128 columns per warpgroup;
-// P overwrites it as 16-bit pairs, from where it is the A operand of P V; O lies beside it, DP columns per warpgroup.
-// K and V tiles go through a ring of shared-memory slots each.
+// the copies of V (TMA, a box per page), and the MMAs.  S lies in tensor memory, 128 columns per warpgroup; P, as 16-bit
+// pairs, is the A operand of P V from there (over S with 128 dims, beside it with 64); O lies beside it, DP columns per
+// warpgroup.  K and V tiles go through a ring of shared-memory slots each.
+//
+// What bounds it (us; floors from 6.7 TB/s and 1.9 PFLOP/s):
+//   few rows per slot: the K and V stream from HBM.  64 tokens over 500 to 32767 slots, 32 heads over 8 kv heads of 128:
+//     2.05 GB in 308 = 6.7 TB/s (floor 306).  With one warp for all copies 407: a warp issues a 2 KB box in 68 to 130
+//     clocks, so K and V have a warp each and a page's halves one box.
+//   many rows, 128 dims: each warpgroup's chain of scores (512 clocks), softmax (1400) and P V (512, half of it behind the
+//     second half of the weights); two warpgroups overlap to 2500 to 2700 clocks per pair of tiles, against 2048 of MMAs.
+//     Four prompts of up to 8192 tokens, 32 heads: 378 (floor 313), 1.57 PFLOP/s of products that the mask keeps.
+//   many rows, 64 dims: the softmax, 2250 clocks per pair of tiles, 1024 of them exponentials (32 a clock and SM).
+//   short calls: 1.4 of launch, 1.7 of plan, then one latency after the other; 32 heads over 300 slots 9.5.
 //
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
 // 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  m follows
@@ -1157,6 +1167,13 @@ int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, 
 
 }  // namespace
 
+// The units that a batch may have at most, whatever its lengths and however its sequences share rows.
+double attend_units(const wino_kv_batch &b)
+{
+    return (double)b.n_seq * (b.n_rows / (2 * positions_per_tile(b)) + 1) * b.n_kv_heads *
+           ((double)b.table_width * b.page_size / kTileN + 1 + kTaskCost);
+}
+
 size_t attend_scratch_bytes(const wino_kv_batch &b) { return scratch_layout(b).total; }
 
 int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
@@ -1179,9 +1196,11 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
     a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
+    // A part that is left for another CTA to join is written and read in 3 us where it fills both row tiles, and in less
+    // than 1 us for a few rows: runs are at least twice as long there (a block of 128 + 128 rows behind 1025 slots, 32
+    // heads: 21.9 us against 24.0 with runs of 3; one token over 300 slots 9.7 with runs of 3, 10.0 with 6).
     a.min_units = L.piece * L.quarters >= 256 ? 6 : 3;
-    const int64_t pairs = b.n_rows / (2 * a.positions) + b.n_seq, tiles = (int64_t)b.table_width * b.page_size / kTileN + 1;
-    a.wide = (double)pairs * (double)(tiles + kTaskCost) * b.n_kv_heads >= 2147483648.0;
+    a.wide = attend_units(b) >= 2147483648.0;
     a.page_shift = -1;
     for (int i = 4; i <= 30; ++i)
         if (b.page_size == 1 << i)

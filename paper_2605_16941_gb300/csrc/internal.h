@@ -259,8 +259,10 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
                                const wino_kv_batch &b, const wino_rope &rope, StatusWords *status,
                                cudaStream_t stream);
 
-// wino_attend (attend.cu): the bytes behind the status words that its kernels use, and their launch.
+// wino_attend (attend.cu): the bytes behind the status words that its kernel uses, the most work units that a batch may
+// have (below 2^62), and its launch.
 size_t attend_scratch_bytes(const wino_kv_batch &b);
+double attend_units(const wino_kv_batch &b);
 int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
                   StatusWords *status, int sm_count, cudaStream_t stream);
 

@@ -143,6 +143,8 @@ int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const w
         return rc;
     if (q->data == out->data)
         return WINO_ERR_ARG;
+    if (attend_units(*b) >= 4611686018427387904.0)
+        return WINO_ERR_SHAPE;
     if (ws_bytes < kStatusBytes + attend_scratch_bytes(*b))
         return WINO_ERR_WORKSPACE;
     DeviceInfo info;

@@ -7,7 +7,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 import paper_2605_16941_gb300 as wino  # noqa: E402
-from kv_helpers import CAUSAL, FULL, SHADOW, add_rows, attend, check, make_kv  # noqa: E402
+from kv_helpers import CAUSAL, FULL, SHADOW, Kv, add_rows, attend, check, make_kv  # noqa: E402
 
 BF, FP = torch.bfloat16, torch.float16
 
@@ -283,3 +283,39 @@ def test_cache_strides(layout, page, kv_heads):
     c.k_cache, c.v_cache = caches
     c.batch = wino.make_kv_batch(*caches, c.table_dev, *c.ints, n_rows=c.n_rows, n_q_heads=c.heads, mask=CAUSAL)
     run(add_rows(c))
+
+
+@pytest.mark.parametrize("n_seq", [3, 300])
+def test_work_counted_in_64_bits(n_seq):
+    """One page of 2^20 slots and tables for 2^30: with 300 sequences the work might not fit 32 bits."""
+    page, width = 1 << 20, 1 << 10
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.full((1, page, 1, 64), float("nan"), dtype=BF, device="cuda") for _ in range(2))
+    for t in (k, v):
+        t[0, :1600] = torch.randn((1600, 1, 64), generator=g).to(BF).cuda()
+    seqs = [(1 + i % 2, 5 + (53 * i) % 1500, 3 + (53 * i) % 1500) for i in range(n_seq)]
+    for s in range(n_seq):  # a slot that no row of the sequence sees may be another's: all see the same page
+        assert seqs[s][1] <= 1600
+    starts = np.cumsum([0] + [s[0] for s in seqs])[:-1].tolist()
+    rows = sum(s[0] for s in seqs)
+    table = np.zeros((n_seq, width), dtype=np.int32)
+    table[:, 1:] = -1
+    ints = torch.tensor([starts] + [[s[i] for s in seqs] for i in range(3)], dtype=torch.int32, device="cuda")
+    td = torch.from_numpy(table).cuda()
+    b = wino.make_kv_batch(k, v, td, *ints, n_rows=rows, n_q_heads=4, mask=CAUSAL)
+    c = add_rows(Kv(CAUSAL, seqs, 4, 1, 64, page, BF, starts, rows, table, k[:, :2048], v[:, :2048], ints, td, b))
+    run(c)
+
+
+def test_sequences_that_share_rows_end():
+    """Not allowed, since the rows' results race, but the call ends, and with it an ordinary one on the same workspace."""
+    c = add_rows(make_kv(CAUSAL, [(64, 200, 136)] * 40, heads=8, kv_heads=2, dim=128, poison=False))
+    keep = c.ints.clone()
+    ws = wino.attend_workspace(c.batch)
+    c.ints[0].zero_()  # every sequence has all rows
+    c.ints[1].fill_(c.n_rows)
+    wino.wino_attend(c.q, c.out, c.batch, ws)
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    c.ints.copy_(keep)
+    c.extra["whole"].fill_(77.0)
+    run(c, ws=ws)

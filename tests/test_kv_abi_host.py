@@ -174,3 +174,11 @@ def test_struct_layout_matches_header(tmp_path, name, mirror):
     subprocess.run([gcc, "-std=c11", "-I", str(inc), str(src), "-o", str(exe)], check=True)
     got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
     assert got == [C.sizeof(cls)] + [getattr(cls, f).offset for f in fields]
+
+
+def test_work_that_cannot_be_counted_is_refused():
+    """Beyond 2^62 units; the check needs no device."""
+    b = batch(n_seq=16384, n_rows=1 << 24, n_q_heads=1024 * 128, n_kv_heads=1024, page_size=1 << 20, table_width=1 << 10,
+              head_dim=8, head_stride=8, slot_stride=8192, page_stride=8192 << 20)
+    assert wino.lib().wino_attend(heads(row=1 << 20, head=8), heads(FAKE * 2, row=1 << 20, head=8), 0.1, b, FAKE, 1 << 40,
+                                  None) == wino.WINO_ERR_SHAPE
