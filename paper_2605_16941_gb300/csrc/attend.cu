@@ -182,6 +182,7 @@ struct alignas(16) Shared {
     uint64_t q_full, q_empty;
     uint64_t full[12], empty[12];
     uint64_t s_full[2], s_free[2], p_half[2], p_ready[2], o_done[2];
+    uint64_t lead[4];  // warpgroup 0's warp of this quarter is half through its first tile's weights
     uint64_t zeroed[12];  // per ring slot of V: the cache slots behind the last one hold zeros
     uint64_t ml_ready, ml_done;
     uint64_t mma_done;
@@ -519,6 +520,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             ptx::mbar_init(p_ready(g), 4);
             ptx::mbar_init(o_done(g), 1);
         }
+        for (int k = 0; k < 4; ++k)
+            ptx::mbar_init(ptx::smem_u32(&sh.lead[k]), 1);
         ptx::mbar_init(ml_ready, 8);
         ptx::mbar_init(ml_done, 8);
         ptx::mbar_init(mma_done, 1);
@@ -566,6 +569,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const float rescale = kRescaleLog2 / sl2;
         uint32_t done = 0;   // slot tiles of this warpgroup so far
         uint32_t joins = 0;  // joined parts so far
+        uint32_t leads = 0;  // parts with both row tiles so far
         while (__all_sync(0xffffffffu, next_part())) {
             const Part &part = sh.parts[reader.slot()];
             const bool two = (part.flags & kTwo) != 0;
@@ -587,6 +591,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             bool good = true;
             for (; t < n; t += step, lim -= step * kTileN, hole -= step * kTileN) {
                 if (!(good = warp_wait(s_full(g), done & 1u, &sh.abort)))
+                    break;
+                if (C::kEarly && two && g == 1 && t == 0 &&
+                    !(good = warp_wait(ptx::smem_u32(&sh.lead[warp & 3]), leads & 1u, &sh.abort)))
                     break;
                 if (any) {
                     ptx::tc_fence_after();
@@ -667,6 +674,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                             p[k / 2] = pack2<kBf16>(u.x, u.y);
                             p[k / 2 + 1] = pack2<kBf16>(v.x, v.y);
                         }
+                        if (C::kEarly && c == 1 && two && g == 0 && t == 0 && lane == 0)
+                            ptx::mbar_arrive(ptx::smem_u32(&sh.lead[warp & 3]));
                         if (C::kEarly && c == 0 && t != first) {  // P's columns are free: P V of the tile before is done
                             if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
                                 break;
@@ -692,6 +701,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         break;
                     if (lane == 0)
                         ptx::mbar_arrive(C::kEarly ? s_free(g) : p_half(g));
+                    if (C::kEarly && two && g == 0 && t == 0 && lane == 0)
+                        ptx::mbar_arrive(ptx::smem_u32(&sh.lead[warp & 3]));
                 }
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -701,6 +712,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             }
             if (!good)
                 break;
+            leads += C::kEarly && two && n > 0 ? 1u : 0u;
             if (n > first) {  // this warpgroup had slot tiles
                 if (!warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort))
                     break;
