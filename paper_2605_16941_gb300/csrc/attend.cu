@@ -75,7 +75,7 @@ struct AttendArgs {
     float4 *part_o;   // [kMaxCtas][2][2 quarters][piece / 4][32 lanes]
     int32_t quarters, piece;   // warps of a warpgroup with rows at most, columns that a warp keeps at most
     int32_t group, positions;  // query heads per kv head, row positions per tile
-    uint32_t pair_magic;       // ceil(2^32 / (2 positions))
+    uint32_t magic[2];         // ceil(2^32 / w) for tasks of w = positions and of 2 positions
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
     int32_t min_units;         // a CTA's run is at least this long
     int32_t wide;              // units may need 64 bits
@@ -86,11 +86,12 @@ struct AttendArgs {
     TileLayout tile;
 };
 
-// Tasks of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256, so that the product with
-// pair_magic is the quotient (its error is below 2^24 / 2^32 < 1 / 256).
-__device__ __forceinline__ int32_t pairs_of(const AttendArgs &a, const SeqRows &q)
+// Tasks of `tiles` row tiles (1 or 2) of one kv head of a sequence.  A row count is at most 2^24 and 2 positions at most 256,
+// so that the product with the magic number is the quotient (its error is below 2^24 / 2^32 < 1 / 256).
+__device__ __forceinline__ int32_t tasks_of(const AttendArgs &a, const SeqRows &q, int32_t tiles)
 {
-    return (int32_t)__umulhi((uint32_t)(q.n + 2 * a.positions - 1), a.pair_magic);
+    const int32_t w = tiles * a.positions;
+    return w == 1 ? q.n : (int32_t)__umulhi((uint32_t)(q.n + w - 1), a.magic[tiles - 1]);
 }
 
 __device__ __forceinline__ int32_t page_entry(const AttendArgs &a, int32_t slot)
@@ -98,10 +99,10 @@ __device__ __forceinline__ int32_t page_entry(const AttendArgs &a, int32_t slot)
     return a.page_shift >= 0 ? slot >> a.page_shift : slot / a.b.page_size;
 }
 
-// Slots that some row of task `pair` sees: its last row sees as many as any.
-__device__ __forceinline__ int32_t task_slots(const AttendArgs &a, const SeqRows &q, int32_t pair)
+// Slots that some row of task `x` sees: its last row sees as many as any.
+__device__ __forceinline__ int32_t task_slots(const AttendArgs &a, const SeqRows &q, int32_t tiles, int32_t x)
 {
-    return row_sees(a.b, q, min(q.n, (pair + 1) * 2 * a.positions) - 1).lim;
+    return row_sees(a.b, q, min(q.n, (x + 1) * tiles * a.positions) - 1).lim;
 }
 
 __device__ __forceinline__ int32_t tiles_of(int32_t slots) { return max(1, (slots + kTileN - 1) / kTileN); }
@@ -113,12 +114,16 @@ struct Cut {
     U total, per;
     int32_t n, more;  // total = n per + more
     float inv_n;
-    // Up to as many tasks as CTAs: a multiple of the tasks, so that tasks of one length are cut alike.
+    // Up to as many tasks as CTAs: a multiple of the tasks, so that tasks of one length are cut alike, unless that makes the
+    // runs longer by more than joining a part costs.
     __device__ __forceinline__ Cut(U units, U tasks, int32_t ctas, U min_units) : total(units)
     {
         n = (int32_t)min((U)ctas, max((U)1, total / min_units));
-        if (tasks > 0 && tasks <= (U)n)
-            n -= n % (int32_t)tasks;
+        if (tasks > 0 && tasks <= (U)n) {
+            const int32_t whole = n - n % (int32_t)tasks;
+            if (total / (U)whole - total / (U)n < min_units)
+                n = whole;
+        }
         per = total / (U)n;
         more = (int32_t)(total - per * (U)n);
         inv_n = 1.f / (float)n;
@@ -247,8 +252,9 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         width >>= 1;
     const int per_round = 32 / width, sub = lane & (width - 1);
     SeqRows q;
-    U mine = 0;           // units of this lane's sequence, of one kv head
-    int32_t n_pairs = 0;  // and its tasks
+    U mine = 0;             // units of this lane's sequence, of one kv head
+    int32_t n_tasks = 0;    // and its tasks
+    int32_t row_tiles = 2;  // of a task
     auto load_round = [&](int32_t s0) {
         const int32_t s = s0 + lane / width;
         q.n = 0;
@@ -256,20 +262,34 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         if (s < n_seq)
             q = load_seq(a.b, s);
         ok = ok && q.ok;
-        U u = 0;
-        const int32_t n_pairs_of_lane = q.n > 0 ? pairs_of(a, q) : 0;
-#pragma unroll 1
-        for (int32_t p = sub; p < n_pairs_of_lane; p += width)
-            u += (U)(tiles_of(task_slots(a, q, p)) + kTaskCost);
-        mine = warp_sum(u, width);
-        n_pairs = n_pairs_of_lane;
     };
-    U total = 0, tasks = 0;
+    auto count = [&]() {
+        U u = 0;
+        n_tasks = q.n > 0 ? tasks_of(a, q, row_tiles) : 0;
 #pragma unroll 1
-    for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
-        load_round(s0);
-        total += warp_sum(sub == 0 ? mine : (U)0, 32);
-        tasks += warp_sum(sub == 0 ? (U)n_pairs : (U)0, 32);
+        for (int32_t x = sub; x < n_tasks; x += width)
+            u += (U)(tiles_of(task_slots(a, q, row_tiles, x)) + kTaskCost);
+        mine = warp_sum(u, width);
+    };
+    U total, tasks;
+#pragma unroll 1
+    while (true) {
+        total = tasks = 0;
+#pragma unroll 1
+        for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
+            if (row_tiles == 2 || n_seq > per_round)
+                load_round(s0);
+            count();
+            total += warp_sum(sub == 0 ? mine : (U)0, 32);
+            tasks += warp_sum(sub == 0 ? (U)n_tasks : (U)0, 32);
+        }
+        // Few and short tasks: one row tile each gives twice as many, for twice the copies of K and V, and fewer parts to
+        // join.  256 rows of each of 32 heads behind 1025 / 4097 / 16385 slots (runs of 3 / 8 / 28 units): 17.9 / 28.7 / 99.9 us
+        // with one row tile, 23.3 / 33.5 / 68.3 with two; 64 rows of 4 heads to each of 8 behind 8193 (14): 40.4 and 42.5.
+        if (row_tiles == 1 || a.b.n_rows <= a.positions || tasks * (U)n_kv * 2 > (U)gridDim.x ||
+            total * (U)n_kv > (U)gridDim.x * 16)
+            break;
+        row_tiles = 1;
     }
     total *= (U)n_kv;
     const Cut<U> cut(total, tasks * (U)n_kv, (int32_t)gridDim.x, (U)a.min_units);
@@ -285,8 +305,10 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         U before = 0;
 #pragma unroll 1
         for (int32_t s0 = 0; s0 < n_seq && n_seq > 1; s0 += per_round) {  // one sequence: every lane has it
-            if (n_seq > per_round)
+            if (n_seq > per_round) {
                 load_round(s0);
+                count();
+            }
             const U pre = warp_scan(sub == 0 ? mine * (U)n_kv : (U)0, lane);
             const unsigned hit = __ballot_sync(0xffffffffu, before + pre > at);
             if (hit) {
@@ -298,7 +320,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
                 q.n = __shfl_sync(0xffffffffu, q.n, src);
                 q.kv = __shfl_sync(0xffffffffu, q.kv, src);
                 q.base = __shfl_sync(0xffffffffu, q.base, src);
-                n_pairs = __shfl_sync(0xffffffffu, n_pairs, src);
+                n_tasks = __shfl_sync(0xffffffffu, n_tasks, src);
                 break;
             }
             before += __shfl_sync(0xffffffffu, pre, 31);
@@ -307,9 +329,9 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         kv_head = (int32_t)((at - task) / mine);
         task += (U)kv_head * mine;
 #pragma unroll 1
-        for (int32_t p0 = 0; p0 < n_pairs && n_pairs > 1; p0 += 32) {
+        for (int32_t p0 = 0; p0 < n_tasks && n_tasks > 1; p0 += 32) {
             const int32_t p = p0 + lane;
-            const U cost = p < n_pairs ? (U)(tiles_of(task_slots(a, q, p)) + kTaskCost) : (U)0;
+            const U cost = p < n_tasks ? (U)(tiles_of(task_slots(a, q, row_tiles, p)) + kTaskCost) : (U)0;
             const U pre = warp_scan(cost, lane);
             const unsigned hit = __ballot_sync(0xffffffffu, task + pre > at);
             if (hit) {
@@ -321,7 +343,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
         // a start that moves to the task's end belongs to the next one, which the walk below finds
-        at = Cut<U>::snap(at, task, task + (U)(tiles_of(task_slots(a, q, pair)) + kTaskCost));
+        at = Cut<U>::snap(at, task, task + (U)(tiles_of(task_slots(a, q, row_tiles, pair)) + kTaskCost));
     }
 #pragma unroll 1
     while (true) {
@@ -329,15 +351,15 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         part.flags = kEnd;
         part.kv_end = part.j0 = part.n = part.i0 = part.first = part.last = 0;
         if (go) {
-            const int32_t slots = task_slots(a, q, pair), tiles = tiles_of(slots);
+            const int32_t slots = task_slots(a, q, row_tiles, pair), tiles = tiles_of(slots);
             const U tile0 = task + kTaskCost, next = tile0 + (U)tiles;  // a task's own cost comes before its tiles
             const U stop = end >= next ? next : Cut<U>::snap(end, task, next);
             part.j0 = at > tile0 ? (int32_t)(at - tile0) : 0;
             part.n = (stop > tile0 ? (int32_t)(stop - tile0) : 0) - part.j0;
             part.kv_end = slots;
-            part.i0 = pair * 2 * a.positions;
+            part.i0 = pair * row_tiles * a.positions;
             const bool to_end = stop == next;
-            part.flags = (q.n - part.i0 > a.positions ? kTwo : 0) |
+            part.flags = (row_tiles == 2 && q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
             if ((part.flags & kWhole) == 0 && part.n > 0) {
                 // the cuts that stay inside the task are those of starts in [tile0 + kSnap, next - kSnap]
@@ -367,7 +389,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         }
         if (last)
             break;
-        if (go && ++pair == n_pairs) {
+        if (go && ++pair == n_tasks) {
             pair = 0;
             if (++kv_head == n_kv) {
                 kv_head = 0;
@@ -378,7 +400,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
                         q = load_seq(a.b, seq);
                 } while (q.n == 0 && seq < n_seq);
                 go = q.n > 0;
-                n_pairs = go ? pairs_of(a, q) : 0;
+                n_tasks = go ? tasks_of(a, q, row_tiles) : 0;
             }
         }
     }
@@ -1207,11 +1229,15 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
     a.positions = positions_per_tile(b);
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
-    a.pair_magic = (uint32_t)(((uint64_t(1) << 32) + 2 * a.positions - 1) / (2 * a.positions));
-    // A part that is left for another CTA to join is written and read in 3 us where it fills both row tiles, and in less
-    // than 1 us for a few rows: runs are at least twice as long there (a block of 128 + 128 rows behind 1025 slots, 32
-    // heads: 21.9 us against 24.0 with runs of 3; one token over 300 slots 9.7 with runs of 3, 10.0 with 6).
-    a.min_units = L.piece * L.quarters >= 256 ? 6 : 3;
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t w = (uint64_t)(i + 1) * a.positions;
+        a.magic[i] = (uint32_t)(((uint64_t(1) << 32) + w - 1) / w);
+    }
+    // A part that is left for another CTA to join is written and read in 2 to 3 us where all warps have rows, and in less
+    // than 1 us for a few rows, so that runs are longer there.  Runs of 6 / 8 / 12 at least: 18.4 / 17.0 / 17.0 us for a
+    // block of 128 + 128 rows behind 1025 slots (32 heads), 26.7 / 25.8 / 28.7 for 16 of 32 + 32; a few rows, one token over
+    // 300 slots, runs of 3 / 8: 9.7 / 14.9.
+    a.min_units = L.piece * L.quarters >= 256 ? 8 : 3;
     a.wide = attend_units(b) >= 2147483648.0;
     a.page_shift = -1;
     for (int i = 4; i <= 30; ++i)

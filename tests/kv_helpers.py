@@ -192,3 +192,39 @@ def rotated(x, pos, freq, rot, interleaved, factor):
 
 def frequencies(rot, base=10000.0):
     return np.array([base ** (-2.0 * j / rot) for j in range(rot // 2)])
+
+
+def check_on_device(c: Kv, scale=None):
+    """As check, the definition evaluated in 64 bits by torch on the GPU: for batches of many rows."""
+    scale = c.dim ** -0.5 if scale is None else scale
+    h, group = half_step(c.dtype), c.heads // c.kv_heads
+    for s, (n, kv, new) in enumerate(c.seqs):
+        held = held_slots(c.mask, n, kv, new)
+        if n == 0:
+            continue
+        if held == 0:
+            assert (c.out[c.starts[s]:c.starts[s] + n] == 0).all(), f"sequence {s}"
+            continue
+        j = torch.arange(held, device="cuda")
+        i = torch.arange(n, device="cuda")[:, None]
+        page = c.table_dev[s].long()[j // c.page]
+        K, V = (t[page, j % c.page].double().repeat_interleave(group, 1) for t in (c.k_cache, c.v_cache))
+        q = c.q[c.starts[s]:c.starts[s] + n].double()
+        if c.mask == FULL:
+            seen = (j < kv).expand(n, held)
+        elif c.mask == CAUSAL:
+            seen = (j <= new + i) & (j < kv)
+        else:
+            seen = torch.where(i >= n // 2, j != new + i - n // 2, j < kv)
+        x = torch.einsum("rhc,jhc->hrj", q, K) * scale
+        p = torch.softmax(x.masked_fill(~seen[None], -torch.inf), -1)
+        p = torch.where(seen.any(-1)[None, :, None], p, 0.0)  # a row that sees nothing
+        want, A = torch.einsum("hrj,jhc->rhc", p, V), torch.einsum("hrj,jhc->rhc", p, V.abs())
+        size = torch.einsum("rhc,jhc->hrj", q.abs(), K.abs()).amax(-1).T[..., None] * scale
+        err = (c.dim + 2) * U * size
+        tol = (2 * err + 2.0 ** -21 + held * U) * 2 * A + 1.01 * h * (A + want.abs())
+        if c.dtype == torch.float16:
+            tol += held * 2.0 ** -25 * V.abs().max() + 2.0 ** -25
+        got = c.out[c.starts[s]:c.starts[s] + n].double()
+        d = (got - want).abs()
+        assert (d <= tol + 1e-30).all(), f"sequence {s}: off by {d.max()}"
