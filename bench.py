@@ -688,7 +688,7 @@ def run_loop(args):
     """The whole semi-autoregressive decode of a workload (config 5: B = 16, gen 256 in 8 blocks of 32),
     until no MASK remains, through the loop driver: every step is one wino_step plus the host read of
     the counts that decides whether the block is done.  The hidden states of each global step (the
-    model's forward is outside this library) are drawn once, in an untimed first pass, and kept in
+    model's forward is not run here) are drawn once, in an untimed first pass, and kept in
     device memory; the timed pass replays the same decode from the same initial state."""
     import numpy as np
     import torch

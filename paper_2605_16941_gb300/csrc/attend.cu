@@ -40,7 +40,7 @@
 #include <cuda_fp16.h>
 
 #include "kv_batch.cuh"
-#include "ptx.cuh"
+#include "ptx_attend.cuh"
 #include "wait.cuh"
 
 namespace wino {

@@ -4,7 +4,6 @@
 #include <cstddef>
 #include <cstdint>
 #include <cuda.h>
-#include <cudaTypedefs.h>  // PFN_cuTensorMapEncodeTiled
 #include <cuda_runtime.h>
 
 #include "wino.h"
@@ -65,17 +64,6 @@ constexpr uint32_t kVmSmemOverhead = 1024 /* ring alignment slack */ + kVmBarrie
 constexpr uint32_t kVmRingCapacity = kScoreSmemMax - kVmSmemOverhead;
 
 constexpr int kMaxBlkLen = 1024;
-
-// ---------------------------------------------------------------- host helpers of the entry points (wino_abi.cu)
-
-struct DeviceInfo {
-    int sm_count = 0;
-    bool supported = false;
-};
-int device_info(DeviceInfo *out);  // of the current device; WINO_ERR_UNSUPPORTED on others than 10.3
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn();
-inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // Rows of a sequence up to which a cluster of CTAs ends a step (finish_step_kernel, which states why); longer
 // sequences hand their rows over through tickets (finish_kernel).
@@ -253,18 +241,6 @@ cudaError_t launch_gather_compact(const uint16_t *H, uint16_t *Hc, const int32_t
 
 // Wp[k][v][c] = W[v][64k + c] (wino_lm_head_panels); d a multiple of 64, (d/64) * V <= 2^30.
 cudaError_t launch_panels(const uint16_t *W, uint16_t *Wp, int64_t d, int64_t V, cudaStream_t stream);
-
-// wino_rope_append: rows' rotation and the cache's writes (rope.cu).
-cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
-                               const wino_kv_batch &b, const wino_rope &rope, StatusWords *status,
-                               cudaStream_t stream);
-
-// wino_attend (attend.cu): the bytes behind the status words that its kernel uses, the most work units that a batch may
-// have (below 2^62), and its launch.
-size_t attend_scratch_bytes(const wino_kv_batch &b);
-double attend_units(const wino_kv_batch &b);
-int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
-                  StatusWords *status, int sm_count, cudaStream_t stream);
 
 cudaError_t launch_draft_verify(int32_t *tokens, const int32_t *argmax, const float *pmax, const float *ptarget,
                                 const wino_params &p, int32_t *counts, int8_t *flags, cudaStream_t stream);

@@ -1,7 +1,7 @@
 // kv_abi.cu -- the extern "C" entry points over a paged cache (see include/wino.h): host-side checks and launches.
 #include <cmath>
 
-#include "internal.h"
+#include "kv.h"
 #include "trace.h"
 
 namespace wino {

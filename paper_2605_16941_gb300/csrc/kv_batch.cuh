@@ -2,7 +2,7 @@
 // array is checked here before it becomes an address, and what fails is left out and recorded.
 #pragma once
 
-#include "internal.h"
+#include "kv.h"
 
 namespace wino {
 

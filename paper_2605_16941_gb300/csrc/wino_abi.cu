@@ -11,7 +11,7 @@
 
 #include <cudaTypedefs.h>  // PFN_cuTensorMapEncodeTiled
 
-#include "internal.h"
+#include "kv.h"
 #include "trace.h"
 
 namespace wino {
