@@ -5,8 +5,8 @@
 //
 // Rows.  The G query heads of a kv head share its K and V, so a tile of M = 128 rows is floor(128 / G) row positions times
 // G heads.  A task is one sequence, one kv head and two such tiles: both tiles multiply every K and V tile that is
-// staged.  Where a task has rows in its first tile only (single tokens, short blocks), its two softmax warpgroups take
-// even and odd slot tiles instead, each with its own m, l and O, joined at the end.
+// staged.  Where a task has rows in its first tile only (single tokens, short blocks, or all tasks of a call that has few),
+// its two softmax warpgroups take even and odd slot tiles instead, each with its own m, l and O, joined at the end.
 //
 // Work.  A task costs one unit per slot tile.  The units of all tasks in order are cut into equal runs, one per CTA, from
 // lengths that are read on the device.  The parts of a task that several runs hold are joined in a binary tree over their
@@ -152,7 +152,7 @@ struct Cut {
 };
 
 // One part of a task, as the planning warp hands it to the others: slot tiles [j0, j0 + n) of one sequence, kv head and
-// pair of row tiles.
+// one or two row tiles.
 enum : int32_t { kTwo = 1, kTail = 2, kWhole = 4, kEnd = 8 };
 struct alignas(16) Part {
     int32_t flags;   // kTwo: rows in both tiles; kTail: the last tile ends behind kv_end; kWhole: the task's only part
@@ -296,7 +296,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
     const int32_t c = (int32_t)blockIdx.x;
     U at = cut.start(c);  // the next unit to hand out
     const U end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
-    int32_t seq = 0, kv_head = 0, pair = 0;
+    int32_t seq = 0, kv_head = 0, index = 0;  // the current task: `index` among its kv head's
     U task = 0;  // the unit at which the current task starts
     uint32_t sent = 0;
     bool go = at < end;
@@ -336,14 +336,14 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             const unsigned hit = __ballot_sync(0xffffffffu, task + pre > at);
             if (hit) {
                 const int src = __ffs(hit) - 1;
-                pair = p0 + src;
+                index = p0 + src;
                 task += __shfl_sync(0xffffffffu, pre - cost, src);
                 break;
             }
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
         // a start that moves to the task's end belongs to the next one, which the walk below finds
-        at = Cut<U>::snap(at, task, task + (U)(tiles_of(task_slots(a, q, row_tiles, pair)) + kTaskCost));
+        at = Cut<U>::snap(at, task, task + (U)(tiles_of(task_slots(a, q, row_tiles, index)) + kTaskCost));
     }
 #pragma unroll 1
     while (true) {
@@ -351,13 +351,13 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         part.flags = kEnd;
         part.kv_end = part.j0 = part.n = part.i0 = part.first = part.last = 0;
         if (go) {
-            const int32_t slots = task_slots(a, q, row_tiles, pair), tiles = tiles_of(slots);
+            const int32_t slots = task_slots(a, q, row_tiles, index), tiles = tiles_of(slots);
             const U tile0 = task + kTaskCost, next = tile0 + (U)tiles;  // a task's own cost comes before its tiles
             const U stop = end >= next ? next : Cut<U>::snap(end, task, next);
             part.j0 = at > tile0 ? (int32_t)(at - tile0) : 0;
             part.n = (stop > tile0 ? (int32_t)(stop - tile0) : 0) - part.j0;
             part.kv_end = slots;
-            part.i0 = pair * row_tiles * a.positions;
+            part.i0 = index * row_tiles * a.positions;
             const bool to_end = stop == next;
             part.flags = (row_tiles == 2 && q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
@@ -389,8 +389,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         }
         if (last)
             break;
-        if (go && ++pair == n_tasks) {
-            pair = 0;
+        if (go && ++index == n_tasks) {
+            index = 0;
             if (++kv_head == n_kv) {
                 kv_head = 0;
                 do {  // there are units left, so there is a sequence with rows
@@ -875,7 +875,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             uint32_t issued = 0;  // slots filled so far
             uint32_t parts = 0;   // parts whose Q was loaded
             bool aborted = false;
-            const int halves = a.joint ? 1 : kHalves;                // copies per page
+            const int halves = a.joint ? 1 : kHalves;             // copies per page
             const int box = lane / halves, half = lane % halves;  // this lane's copy of a slot tile
             while (!aborted && __all_sync(0xffffffffu, next_part())) {
                 const Part part = sh.parts[reader.slot()];
@@ -1004,9 +1004,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     ptx::mma_commit(s_full(g));
                     return true;
                 };
-                // O_g (+)= P_g V, each half of the slots as soon as its weights are in tensor memory (where nothing waits for
-                // P V but the next scores; with S free early, at once); zeros: V's slots behind
-                // the last one are zeroed first
+                // O_g (+)= P_g V.  Where the next scores wait for it, each half of the slots as soon as its weights are in
+                // tensor memory.  zeros: V's slots behind the last one are zeroed first.
                 auto values = [&](int g, int vs, bool add, bool zeros) -> bool {
                     const uint64_t db = ptx::sdesc_mnmajor_sw128(slot_addr(vs), a.tile.half, a.tile.group);
                     uint32_t &count = g ? n_p1 : n_p0;
@@ -1024,7 +1023,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                                 return false;
                             ptx::tc_fence_after();
                         }
-                        ptx::mma_f16_ts(tmem + C::kTmemO + (uint32_t)(g * DP), tmem + C::kTmemP + (uint32_t)g * C::kStrideP + (uint32_t)(k * 8),
+                        ptx::mma_f16_ts(tmem + C::kTmemO + (uint32_t)(g * DP),
+                                        tmem + C::kTmemP + (uint32_t)g * C::kStrideP + (uint32_t)(k * 8),
                                         db + (uint64_t)(k * (a.tile.group >> 3)), id_o, (add || k != 0) ? 1u : 0u);
                     }
                     ptx::mma_commit(o_done(g));

@@ -6,10 +6,11 @@
 // position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.
 //
 // Bound by HBM: every element is read and written once, 16 bytes at a time (8 where head_dim or rot_dim is no multiple of
-// 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in registers, and walks the heads with the loads of
-// two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of 128 (100 MB) 16.3; 20027 rows of 32 + 2 x 8 heads,
-// half of each rotated (492 MB), 84 = 5.9 TB/s.  Four heads in flight take registers for one CTA per SM less: 19.8 and
-// 96; one in flight 29 and 100; more CTAs than 4 of 256 threads per SM 19 to 26 and 85 to 101.
+// 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in
+// registers, and walks the heads with the loads of two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of
+// 128 (100 MB) 16.3; 20027 rows of 32 + 2 x 8 heads, half of each rotated (492 MB), 84 = 5.9 TB/s.  Four heads in flight take
+// registers for one CTA per SM less: 19.8 and 96; one in flight 29 and 100; more CTAs than 4 of 256 threads per SM 19 to 26
+// and 85 to 101.
 #include <algorithm>
 
 #include <cuda_bf16.h>

@@ -218,7 +218,8 @@ class BlockCache:
     ``step(blk_start)`` describes the rows of a step as ``wino_step`` wants their hidden states, [s][kind][l] (with
     ``no_shadow`` [s][l]): block rows see the context and the block, shadow rows these and the shadow block but for the
     position that they verify (Sec. 4.2.2).  Within a layer, ``append`` rotates q (in place) and stores k and v, then
-    ``attend`` reads what the rows see.  Calls on one stream at a time: the layers share a workspace.
+    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share a workspace, so a
+    decode keeps to one stream.
     """
 
     def __init__(self, n_layers: int, n_seq: int, seq_len: int, blk_len: int, n_q_heads: int, n_kv_heads: int,
@@ -264,8 +265,8 @@ class BlockCache:
             self._ws = (batch.n_rows, attend_workspace(batch))
         return self._ws[1]
 
-    def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope, stream=None) -> None:
-        wino_rope_append(q, k, v, batch, rope, self._workspace(batch), stream=stream)
+    def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope) -> None:
+        wino_rope_append(q, k, v, batch, rope, self._workspace(batch))
 
-    def attend(self, q, out, batch: WinoKvBatch, *, scale: float | None = None, stream=None) -> None:
-        wino_attend(q, out, batch, self._workspace(batch), scale=scale, stream=stream)
+    def attend(self, q, out, batch: WinoKvBatch, *, scale: float | None = None) -> None:
+        wino_attend(q, out, batch, self._workspace(batch), scale=scale)
