@@ -344,3 +344,30 @@ def test_sequences_that_share_rows_end():
     c.ints.copy_(keep)
     c.extra["whole"].fill_(77.0)
     run(c, ws=ws)
+
+
+def test_16384_sequences():
+    """The most sequences a batch may have, of which some are checked."""
+    seqs = [(1 + i % 3, 1 + (29 * i) % 50, (29 * i) % 50 - i % 3) for i in range(16384)]
+    c = add_rows(make_kv(CAUSAL, seqs, heads=2, kv_heads=1, dim=8))
+    ws = attend(c)
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    check(c, only=set(range(0, 16384, 331)) | {16383})
+    assert not (c.out == 77.0).all(-1).any()
+
+
+def test_failure_is_reported_once_and_cleared():
+    """An error recorded for a call (planted here as a CTA would record a timeout, with nodes that parts which never came
+    would have left) is published, and the next call on the workspace starts clean."""
+    c = add_rows(make_kv(CAUSAL, [(3, 3000, 2997)], heads=4, kv_heads=1, dim=128))
+    ws = wino.attend_workspace(c.batch)
+    run(c, ws=ws)
+    words = ws.view(torch.int32)
+    words[0] = wino.WINO_ERR_DEVICE_TIMEOUT
+    words[64:64 + 160 * 64] = 1  # behind the 256 bytes of status words
+    wino.wino_attend(c.q, c.out, c.batch, ws)
+    assert wino.wino_read_device_status(ws) == wino.WINO_ERR_DEVICE_TIMEOUT
+    assert (words[64:64 + 160 * 64] == 0).all() and words[0] == 0 and words[2] == 0
+    c.extra["whole"].fill_(77.0)
+    run(c, ws=ws)
