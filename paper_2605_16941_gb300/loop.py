@@ -218,8 +218,8 @@ class BlockCache:
     ``step(blk_start)`` describes the rows of a step as ``wino_step`` wants their hidden states, [s][kind][l] (with
     ``no_shadow`` [s][l]): block rows see the context and the block, shadow rows these and the shadow block but for the
     position that they verify (Sec. 4.2.2).  Within a layer, ``append`` rotates q (in place) and stores k and v, then
-    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share a workspace, so a
-    decode keeps to one stream.
+    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws`` (of
+    which ``wino_read_device_status`` reads what the device found wrong), so a decode keeps to one stream.
     """
 
     def __init__(self, n_layers: int, n_seq: int, seq_len: int, blk_len: int, n_q_heads: int, n_kv_heads: int,
@@ -232,7 +232,9 @@ class BlockCache:
         dtype = torch.bfloat16 if dtype is None else dtype
         self.k, self.v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
         self.page_table = torch.arange(n_seq * width, dtype=torch.int32, device=device).view(n_seq, width)
-        self._ws = None
+        # one for the batches of any rows, never replaced: a captured call goes on using it
+        most = self._batches(min(seq_len + blk_len, (1 << 24) // n_seq), 0, 0, WINO_MASK_FULL)
+        self.ws = attend_workspace(most[0])
 
     def _batches(self, rows: int, kv_len: int, new_slot: int, mask: int) -> list[WinoKvBatch]:
         import torch
@@ -259,14 +261,8 @@ class BlockCache:
             return self._batches(self.blk_len, end, blk_start, WINO_MASK_FULL)
         return self._batches(2 * self.blk_len, end, blk_start, WINO_MASK_SHADOW)
 
-    def _workspace(self, batch: WinoKvBatch):
-        # the batches of one cache differ in their rows alone; a workspace of many rows serves fewer too
-        if self._ws is None or self._ws[0] < batch.n_rows:
-            self._ws = (batch.n_rows, attend_workspace(batch))
-        return self._ws[1]
-
     def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope) -> None:
-        wino_rope_append(q, k, v, batch, rope, self._workspace(batch))
+        wino_rope_append(q, k, v, batch, rope, self.ws)
 
     def attend(self, q, out, batch: WinoKvBatch, *, scale: float | None = None) -> None:
-        wino_attend(q, out, batch, self._workspace(batch), scale=scale)
+        wino_attend(q, out, batch, self.ws, scale=scale)

@@ -52,7 +52,7 @@ class Model:
 
     def check_layer(self, i, b, mask, seqs, positions, before, q, o):
         torch.cuda.synchronize()
-        assert wino.wino_read_device_status(self.cache._workspace(b)) == wino.WINO_OK
+        assert wino.wino_read_device_status(self.cache.ws) == wino.WINO_OK
         kc, vc = self.cache.k[i].transpose(1, 2), self.cache.v[i].transpose(1, 2)
         table = self.cache.page_table.cpu().numpy()
         page = self.cache.k.size(3)
@@ -186,3 +186,25 @@ def test_block_cache_refuses_positions_outside():
     for s in (-1, 33):
         with pytest.raises(ValueError):
             cache.step(s)
+
+
+def test_captured_step_outlives_a_larger_context():
+    """The cache's workspace stays where a captured step found it, whatever rows come later."""
+    cache = loop.BlockCache(1, 2, 200, 8, 4, 2, 64, page_size=16)
+    cache.k.normal_()
+    cache.v.normal_()
+    at = cache.ws.data_ptr()
+    batch = cache.step(96)[0]
+    q, o, want = (torch.randn((32, 4, 64)).to(BF).cuda() for _ in range(3))
+    cache.attend(q, want, batch)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.attend(q, o, batch)
+    big = cache.context(104, 200)[0]
+    x = torch.randn((192, 4, 64)).to(BF).cuda()
+    y = torch.zeros_like(x)
+    cache.attend(x, y, big)
+    g.replay()
+    torch.cuda.synchronize()
+    assert cache.ws.data_ptr() == at and torch.equal(o, want) and y.abs().sum() > 0
+    assert wino.wino_read_device_status(cache.ws) == wino.WINO_OK
