@@ -387,6 +387,7 @@ def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot
     # plain attributes: what the calls compare with, cheaper than the struct's fields
     b.q_shape, b.kv_shape = (n_rows, n_q_heads, head_dim), (n_rows, n_kv_heads, head_dim)
     b.elements, b.device = k_cache.dtype, k_cache.get_device()
+    b.devices = {b.device}
     return b
 
 
@@ -394,11 +395,14 @@ def make_rope(freq, *, rot_dim: int, factor: float = 1.0, interleaved: bool = Fa
     """wino_rope; ``freq`` is a device float64 [rot_dim / 2] tensor (None for rot_dim = 0), ``positions`` device int32
     [n_rows] or None."""
     import torch
-    _require(rot_dim == 0 or (freq.dtype == torch.float64 and freq.is_contiguous() and freq.numel() == rot_dim // 2),
-             "make_rope", WINO_ERR_SHAPE)
+    if rot_dim == 0:
+        freq = None
+    _require(rot_dim == 0 or (freq is not None and freq.dtype == torch.float64 and freq.is_contiguous() and
+                              freq.numel() == rot_dim // 2), "make_rope", WINO_ERR_SHAPE)
     _require(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous()), "make_rope")
-    r = WinoRope(rot_dim, int(interleaved), factor, _ptr(freq) if rot_dim else None, _ptr(positions))
+    r = WinoRope(rot_dim, int(interleaved), factor, _ptr(freq), _ptr(positions))
     r.tensors = (freq, positions)
+    r.devices = {t.get_device() for t in r.tensors if t is not None}
     r.n_positions = None if positions is None else positions.numel()
     return r
 
@@ -439,7 +443,10 @@ def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=N
         vh = _heads(v, batch, batch.kv_shape, where)
     if rope.n_positions not in (None, batch.q_shape[0]):
         raise WinoError(WINO_ERR_SHAPE, where)
-    if batch.device != _current_device() or ws.get_device() != batch.device:  # the kernels run on the current device
+    if _nbytes(ws) < STATUS_BYTES:
+        raise WinoError(WINO_ERR_WORKSPACE, where)
+    # the kernels run on the current device; wino_rope_frequencies' values are on the host
+    if not rope.devices <= batch.devices or batch.device != _current_device() or ws.get_device() != batch.device:
         raise WinoError(WINO_ERR_ARG, where)
     _check(lib().wino_rope_append(qh, qo, kh, vh, batch, rope, _ptr(ws), _stream(stream)), where)
 

@@ -134,7 +134,7 @@ int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const w
                 size_t ws_bytes, void *stream)
 {
     const Range range("wino_attend");
-    if (!ws || !aligned(ws, kStatusBytes) || !(scale > 0.f) || !std::isfinite(scale))
+    if (!ws || !aligned(ws, kStatusBytes) || !(scale > 0.f) || !(scale < 0x1p127f))
         return WINO_ERR_ARG;
     int rc = check_batch(b);
     if (rc != WINO_OK)

@@ -5,6 +5,7 @@ import math
 import shutil
 import subprocess
 from pathlib import Path
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -72,7 +73,7 @@ def test_attend_refusals():
     assert call(ws=FAKE + 16) == A
     assert call(q=heads(None)) == A and call(q=heads(FAKE + 8)) == A and call(out=heads(FAKE * 2 + 2)) == A
     assert call(out=heads()) == A  # onto q
-    for scale in (0.0, -1.0, math.inf, math.nan):
+    for scale in (0.0, -1.0, 2.0 ** 127, math.inf, math.nan):
         assert call(scale=scale) == A, scale
     for q in (heads(row=260), heads(row=56), heads(head=60), heads(head=0), heads(row=1 << 37)):
         assert call(q=q) == S and call(out=wino.WinoHeads(FAKE * 2, q.row_stride, q.head_stride)) == S
@@ -152,10 +153,34 @@ def test_python_checks():
         wino.make_rope(torch.zeros(32), rot_dim=64)
     with pytest.raises(wino.WinoError):
         wino.make_rope(torch.zeros(31, dtype=torch.float64), rot_dim=64)
+    with pytest.raises(wino.WinoError):
+        wino.make_rope(None, rot_dim=64)
     q = torch.zeros((4, 4, 64), dtype=torch.bfloat16)
     for bad in (q[:3], q[:, :3], q[..., :32], q.half(), q.transpose(0, 1)[..., ::2]):
         with pytest.raises(wino.WinoError):
             _abi._heads(bad, b, b.q_shape, "test")
+
+
+def test_rope_on_another_device_is_refused(monkeypatch):
+    """The frequencies as wino_rope_frequencies returns them, on the host, for a batch on a device; nothing is launched."""
+    freq, _ = wino.wino_rope_frequencies(64, 1e4)
+    launched = []
+    stub = SimpleNamespace(wino_status_string=wino.lib().wino_status_string,
+                           wino_rope_append=lambda *a: launched.append(a) or wino.WINO_OK)
+    monkeypatch.setattr(_abi, "lib", lambda: stub)
+    monkeypatch.setattr(_abi, "_current_device", lambda: 0)
+    k, i, t = torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), torch.zeros((2, 3), dtype=torch.int32)
+    b = wino.make_kv_batch(k, k, t, i, i, i, i, n_rows=4, n_q_heads=4, mask=0)
+    b.device, b.devices = 0, {0}  # as over a cache on device 0
+    ws = torch.zeros(256, dtype=torch.uint8)
+    for rope in (wino.make_rope(freq, rot_dim=64),
+                 wino.make_rope(None, rot_dim=0, positions=torch.zeros(4, dtype=torch.int32))):
+        with pytest.raises(wino.WinoError) as e:
+            wino.wino_rope_append(None, None, None, b, rope, ws)
+        assert e.value.status == wino.WINO_ERR_ARG
+    with pytest.raises(wino.WinoError) as e:
+        wino.wino_rope_append(None, None, None, b, wino.make_rope(None, rot_dim=0), ws[:255])
+    assert e.value.status == wino.WINO_ERR_WORKSPACE and not launched
 
 
 @pytest.mark.parametrize("name,mirror", [("wino_kv_batch", "WinoKvBatch"), ("wino_rope", "WinoRope"), ("wino_heads", "WinoHeads")])
