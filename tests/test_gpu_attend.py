@@ -371,3 +371,25 @@ def test_failure_is_reported_once_and_cleared():
     assert (words[64:64 + 160 * 64] == 0).all() and words[0] == 0 and words[2] == 0
     c.extra["whole"].fill_(77.0)
     run(c, ws=ws)
+
+
+def test_two_graphs_share_a_workspace():
+    """Graphs of other shapes on one workspace, replayed one behind the other without a pause: as the calls by themselves."""
+    a = add_rows(make_kv(CAUSAL, [(300, 5000, 4700)], heads=8, kv_heads=2, dim=128))
+    b = add_rows(make_kv(SHADOW, [(16, 4000, 3990), (2, 31, 30)], heads=8, kv_heads=2, dim=64))
+    ws = wino.attend_workspace(a.batch)
+    want = []
+    for c in (a, b):
+        run(c, ws=ws)
+        want.append(c.out.clone())
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g, c in zip(graphs, (a, b)):
+        with torch.cuda.graph(g):
+            attend(c, ws=ws)
+        c.extra["whole"].fill_(77.0)
+    for _ in range(20):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
