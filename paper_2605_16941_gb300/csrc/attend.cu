@@ -59,6 +59,7 @@ constexpr int kTaskCost = 3;            // what a task costs beside its slot til
 constexpr int kSnap = 2;                // a cut this near to a task's border (in slot tiles) is moved there
 constexpr float kRescaleLog2 = 8.f;
 constexpr uint32_t kTmemAll = 512;
+constexpr uint32_t kSharedBytes = 3 * 1024;  // for struct Shared, behind the tiles
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 // Where slot row r, dims 64 h .. 64 h + 63 of a K or V tile lie: (r / 8) group + h half + (r % 8) 128 bytes.  With 128 dims
 // one copy brings both halves of a page's rows, interleaved by groups of 8 rows, if the cache's strides let one
@@ -173,7 +174,7 @@ struct Config {
     static constexpr int kSlotsK = DP == 128 ? 2 : 5, kSlotsV = DP == 128 ? 3 : 7;
     static constexpr int kSlots = kSlotsK + kSlotsV;
     static constexpr uint32_t kRing = kSlots * kTileBytes;
-    static constexpr uint32_t kShared = 3072;
+    static constexpr uint32_t kShared = kSharedBytes;
     // Tensor memory columns of warpgroup g: S at kTmemS + g 128, P at kTmemP + g kStrideP, O at kTmemO + g DP.  With 64 dims
     // P has columns of its own, and the scores of the next tile are computed as soon as S is in registers; with 128
     // they are taken by O, P overwrites S, and the next scores wait for P V.
@@ -197,7 +198,7 @@ struct alignas(16) Shared {
     int32_t abort;
     float2 ml[2][kTileM];
 };
-static_assert(sizeof(Shared) <= 3072, "shared block must fit its reserve");
+static_assert(sizeof(Shared) <= kSharedBytes, "shared block must fit its reserve");
 
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
