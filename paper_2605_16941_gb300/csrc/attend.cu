@@ -116,20 +116,27 @@ template <typename U>
 struct Cut {
     U total, per;
     int32_t n, more;  // total = n per + more
-    float inv_n;
+    float inv_n, runs_per_unit;
     // Up to as many tasks as CTAs: a multiple of the tasks, so that tasks of one length are cut alike, unless that makes the
-    // runs longer by more than joining a part costs.
-    __device__ __forceinline__ Cut(U units, U tasks, int32_t ctas, U min_units) : total(units)
+    // runs longer by more than joining a part costs.  Quotients of integers below 2^11 are taken in fp32, half a unit off the
+    // border: exact, and shorter than an integer division.
+    __device__ __forceinline__ Cut(U units, U tasks, int32_t ctas, int32_t min_units) : total(units)
     {
-        n = (int32_t)min((U)ctas, max((U)1, total / min_units));
+        n = ctas;
+        if (total < (U)(ctas * min_units))
+            n = max(1, (int32_t)__fdividef((float)(int32_t)total + 0.5f, (float)min_units));
+        inv_n = __fdividef(1.f, (float)n);
         if (tasks > 0 && tasks <= (U)n) {
-            const int32_t whole = n - n % (int32_t)tasks;
-            if (total / (U)whole - total / (U)n < min_units)
+            const int32_t whole = (int32_t)tasks * (int32_t)__fdividef((float)n + 0.5f, (float)(int32_t)tasks);
+            const float inv_whole = __fdividef(1.f, (float)whole);
+            if ((float)total * (inv_whole - inv_n) < (float)min_units) {
                 n = whole;
+                inv_n = inv_whole;
+            }
         }
+        runs_per_unit = __fdividef((float)n, (float)total);
         per = total / (U)n;
         more = (int32_t)(total - per * (U)n);
-        inv_n = 1.f / (float)n;
     }
     // c more < 2^15 and n <= 160: the quotient's distance from an integer, at least 1 / (2 n), is far above its rounding
     __device__ __forceinline__ U start(int32_t c) const
@@ -139,7 +146,7 @@ struct Cut {
     // The run that holds a unit: off by one at most from the quotient in fp32.
     __device__ __forceinline__ int32_t run_of(U unit) const
     {
-        int32_t c = min(n - 1, (int32_t)((float)unit * ((float)n / (float)total)));
+        int32_t c = min(n - 1, (int32_t)((float)unit * runs_per_unit));
         while (start(c) > unit)
             --c;
         while (c + 1 < n && start(c + 1) <= unit)
@@ -233,6 +240,15 @@ __device__ __forceinline__ U warp_sum(U x, int width)  // over groups of `width`
 }
 
 template <typename U>
+__device__ __forceinline__ U warp_total(U x)
+{
+    if constexpr (sizeof(U) == 4)
+        return __reduce_add_sync(0xffffffffu, x);
+    else
+        return warp_sum(x, 32);
+}
+
+template <typename U>
 __device__ __forceinline__ U warp_scan(U x, int lane)  // inclusive
 {
 #pragma unroll
@@ -255,7 +271,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         width >>= 1;
     const int per_round = 32 / width, sub = lane & (width - 1);
     SeqRows q;
-    U mine = 0;             // units of this lane's sequence, of one kv head
+    U share = 0, mine = 0;  // units of this lane's tasks, and of its sequence, of one kv head
     int32_t n_tasks = 0;    // and its tasks
     int32_t row_tiles = 2;  // of a task
     auto load_round = [&](int32_t s0) {
@@ -267,12 +283,12 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         ok = ok && q.ok;
     };
     auto count = [&]() {
-        U u = 0;
+        share = 0;
         n_tasks = q.n > 0 ? tasks_of(a, q, row_tiles) : 0;
 #pragma unroll 1
         for (int32_t x = sub; x < n_tasks; x += width)
-            u += (U)(tiles_of(task_slots(a, q, row_tiles, x)) + kTaskCost);
-        mine = warp_sum(u, width);
+            share += (U)(tiles_of(task_slots(a, q, row_tiles, x)) + kTaskCost);
+        mine = warp_sum(share, width);
     };
     U total, tasks;
 #pragma unroll 1
@@ -283,8 +299,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             if (row_tiles == 2 || n_seq > per_round)
                 load_round(s0);
             count();
-            total += warp_sum(sub == 0 ? mine : (U)0, 32);
-            tasks += warp_sum(sub == 0 ? (U)n_tasks : (U)0, 32);
+            total += warp_total(share);
+            tasks += warp_total(sub == 0 ? (U)n_tasks : (U)0);
         }
         // Few and short tasks: one row tile each gives twice as many, for twice the copies of K and V, and fewer parts to
         // join.  256 rows of each of 32 heads behind 1025 / 4097 / 16385 slots (runs of 3 / 8 / 28 units): 17.9 / 28.7 / 99.9 us
@@ -295,7 +311,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
         row_tiles = 1;
     }
     total *= (U)n_kv;
-    const Cut<U> cut(total, tasks * (U)n_kv, (int32_t)gridDim.x, (U)a.min_units);
+    const Cut<U> cut(total, tasks * (U)n_kv, (int32_t)gridDim.x, a.min_units);
     const int32_t c = (int32_t)blockIdx.x;
     U at = cut.start(c);  // the next unit to hand out
     const U end = c < cut.n && total > 0 ? cut.start(c + 1) : at;
@@ -329,7 +345,12 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             before += __shfl_sync(0xffffffffu, pre, 31);
         }
         // its kv head, and by the sum over 32 tasks at a time the task
-        kv_head = (int32_t)((at - task) / mine);
+        const U behind = at - task;
+        kv_head = (int32_t)__fdividef((float)behind, (float)mine);  // off by one at most
+        while ((U)kv_head * mine > behind)
+            --kv_head;
+        while ((U)(kv_head + 1) * mine <= behind)
+            ++kv_head;
         task += (U)kv_head * mine;
 #pragma unroll 1
         for (int32_t p0 = 0; p0 < n_tasks && n_tasks > 1; p0 += 32) {
@@ -362,6 +383,10 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             part.kv_end = slots;
             part.i0 = index * row_tiles * a.positions;
             const bool to_end = stop == next;
+            // the part's first pages, which the copying warps read next, on their way to the L1 cache
+            const int32_t entry = page_entry(a, part.j0 * kTileN) + lane;
+            if (part.n > 0 && slots > 0 && entry <= page_entry(a, slots - 1))
+                ptx::touch(a.b.page_table + (int64_t)seq * a.b.table_width + entry);
             part.flags = (row_tiles == 2 && q.n - part.i0 > a.positions ? kTwo : 0) |
                          (to_end && (slots & (kTileN - 1)) != 0 ? kTail : 0) | (to_end && part.j0 == 0 ? kWhole : 0);
             if ((part.flags & kWhole) == 0 && part.n > 0) {

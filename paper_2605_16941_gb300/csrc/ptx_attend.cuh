@@ -20,6 +20,12 @@ __device__ __forceinline__ void regs_dec()
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
+// A load that brings the line to the L1 cache; the value is dropped.
+__device__ __forceinline__ void touch(const int32_t *p)
+{
+    asm volatile("{\n\t.reg .b32 x;\n\tld.global.ca.b32 x, [%0];\n\t}" ::"l"(p));
+}
+
 // 3-D to 5-D forms without a cache hint, innermost coordinate first.
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int32_t c0, int32_t c1,
                                             int32_t c2)
