@@ -24,11 +24,12 @@
 //     clocks, so K and V have a warp each and a page's halves one box.
 //   many rows, 128 dims: each warpgroup's chain of scores (512 clocks), softmax (1400) and P V (512, half of it behind the
 //     second half of the weights); two warpgroups overlap to 2500 to 2700 clocks per pair of tiles, against 2048 of MMAs.
-//     Four prompts of up to 8192 tokens, 32 heads: 378 (floor 313), 1.57 PFLOP/s of products that the mask keeps.
+//     Four prompts of up to 8192 tokens, 32 heads: 376 (floor 313), 1.58 PFLOP/s of products that the mask keeps; 411 where
+//     calls follow one another for long and the power cap lowers the clock.
 //   many rows, 64 dims: the softmax, 2100 to 2400 clocks per pair of tiles, 1024 of them exponentials (32 a clock and SM)
 //     and the rest mostly latencies of loads, votes and barriers, which two warps per scheduler do not hide.  Two threads
 //     per row (16 softmax warps of 104 registers) take the same time, at 128 dims too: each repeats the latencies.
-//   short calls: 1.4 of launch, 1.7 of plan, then one latency after the other; 32 heads over 300 slots 9.5.
+//   short calls: 1.4 of launch, 1.5 of plan, then one latency after the other; 32 heads over 300 slots 9.5.
 //
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
 // 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  m follows
