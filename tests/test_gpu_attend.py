@@ -393,3 +393,11 @@ def test_two_graphs_share_a_workspace():
     torch.cuda.synchronize()
     assert wino.wino_read_device_status(ws) == wino.WINO_OK
     assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+
+
+@pytest.mark.parametrize("heads,kv_heads,rows", [(80, 80, 260), (80, 40, 140)])
+@pytest.mark.parametrize("mask", [CAUSAL, SHADOW], ids=["causal", "shadow"])
+def test_more_tasks_than_ctas(mask, heads, kv_heads, rows):
+    """Several tasks of each of many kv heads, some sequences between them without any: the order by row position."""
+    seqs = [(rows, rows + 20, 30), (0, 100, 0), (rows + 30, rows - 60, 40), (2, 500, 490), (0, 0, 0)]
+    run(add_rows(make_kv(mask, seqs, heads=heads, kv_heads=kv_heads, dim=16, gap=1)))
