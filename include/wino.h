@@ -468,7 +468,8 @@ WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
 /*
  * out[r, h] = sum_j p_j V_j over the slots j that row r sees, p = softmax of
  * scale * <q[r, h], K_j>.  Products and sums in fp32 (the weights p rounded to
- * the element type for the product with V), one rounding to the element type
+ * the element type for the product with V; with WINO_FP16 those below 2^-23.9 of
+ * a row's largest to steps of 2^-33.9 of it), one rounding to the element type
  * at the end.  Rows of no sequence are left as they are.
  *   q, out  [n_rows, n_q_heads, head_dim]; out shares no element with q or the
  *           cache
