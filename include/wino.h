@@ -16,7 +16,7 @@
  * Conventions shared by every entry point
  *   - Every array argument is a DEVICE pointer owned by the caller unless
  *     marked host; the library never allocates, frees or synchronises
- *     (except wino_read_device_status, which reads back one word, and
+ *     (except wino_read_device_status, which reads the status words back, and
  *     wino_decode, whose loop reads each step's counts back).
  *   - bf16 data are passed as uint16_t bit patterns (IEEE binary32 top half).
  *   - Alignment: H and W 16 bytes, workspaces 256 bytes, int32 and float
@@ -490,9 +490,12 @@ WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale
  * (published by its last kernel): WINO_OK, WINO_ERR_DEVICE_TIMEOUT (a bounded
  * wait expired), WINO_ERR_ARG (an active-sequence list entry out of range, or
  * what a batch's device arrays must not hold, see wino_kv_batch) or
- * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).
+ * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).  Of wino_attend
+ * calls, of which a step makes one per layer on one workspace, it returns the
+ * first failure since the status of `ws` was last read, and clears it: one read
+ * per step tells of all its layers.
  */
-WINO_API int wino_read_device_status(const void *ws, void *stream, int *device_status);
+WINO_API int wino_read_device_status(void *ws, void *stream, int *device_status);
 
 /*
  * Launch timing of the fused score kernel (for benchmarks).  Between

@@ -480,6 +480,8 @@ def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, s
 
 
 def wino_read_device_status(ws, stream=None) -> int:
+    """The status of a workspace's last call; of its paged-cache calls the first failure since this was last read, which is
+    cleared."""
     out = C.c_int(0)
     _check(lib().wino_read_device_status(_ptr(ws), _stream(stream), C.byref(out)), "wino_read_device_status")
     return out.value

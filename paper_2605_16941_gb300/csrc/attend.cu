@@ -1161,7 +1161,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (atomicAdd(&a.status->finished, 1u) + 1u == gridDim.x) {
             __threadfence();
             failed = atomicExch(&a.status->current, (int32_t)WINO_OK);
-            a.status->last = failed;
+            if (failed && a.status->first == WINO_OK)
+                a.status->first = failed;
             a.status->finished = 0;
         }
     }

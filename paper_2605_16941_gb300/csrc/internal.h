@@ -127,14 +127,17 @@ constexpr int kMaxRecordsPerRow = 256;
 // Status words at the start of every workspace.  `current` collects the
 // errors of the call in flight: score-kernel CTAs record theirs only after
 // griddepcontrol.wait (so after the previous call's finish kernel has cleared
-// the word).  The finish kernel publishes the outcome as `last` (what
-// wino_read_device_status returns); only after a failure does it clear
-// `current` for the next call, by the last of its CTAs, which `finished` counts
-// (zero between calls).  A workspace starts zeroed.
+// the word).  The finish kernel publishes the outcome as `last`; only after a
+// failure does it clear `current` for the next call, by the last of its CTAs,
+// which `finished` counts (zero between calls).  A workspace starts zeroed.
+// wino_attend publishes failures only, as `first`, which stays until
+// wino_read_device_status has returned it: a step's layers share a workspace,
+// and the ones behind a failed one must not hide it.
 struct StatusWords {
     int32_t current;
     int32_t last;
     uint32_t finished;
+    int32_t first;
 };
 
 // Optional per-CTA timeline of the score kernel (diagnostics, off by default):

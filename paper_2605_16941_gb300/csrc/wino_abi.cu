@@ -561,7 +561,7 @@ int wino_profile_end(double *score_ms_total, int *score_launches)
     return rc;
 }
 
-int wino_read_device_status(const void *ws, void *stream, int *device_status)
+int wino_read_device_status(void *ws, void *stream, int *device_status)
 {
     if (!ws || !device_status)
         return WINO_ERR_ARG;
@@ -572,7 +572,10 @@ int wino_read_device_status(const void *ws, void *stream, int *device_status)
     if (cudaMemcpy(&w, ws, sizeof w, cudaMemcpyDeviceToHost) != cudaSuccess)
         return WINO_ERR_CUDA;
     // `current` outlives a call only where no later kernel of it publishes: wino_rope_append's errors
-    *device_status = w.current ? w.current : w.last;
+    *device_status = w.first ? w.first : (w.current ? w.current : w.last);
+    if (w.first && (cudaMemsetAsync(&static_cast<StatusWords *>(ws)->first, 0, sizeof w.first, s) != cudaSuccess ||
+                    cudaStreamSynchronize(s) != cudaSuccess))
+        return WINO_ERR_CUDA;
     return WINO_OK;
 }
 

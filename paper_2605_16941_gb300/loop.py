@@ -218,8 +218,10 @@ class BlockCache:
     ``step(blk_start)`` describes the rows of a step as ``wino_step`` wants their hidden states, [s][kind][l] (with
     ``no_shadow`` [s][l]): block rows see the context and the block, shadow rows these and the shadow block but for the
     position that they verify (Sec. 4.2.2).  Within a layer, ``append`` rotates q (in place) and stores k and v, then
-    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws`` (of
-    which ``wino_read_device_status`` reads what the device found wrong), so a decode keeps to one stream.
+    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws``, so a
+    decode keeps to one stream.  What the device finds wrong (a wait that ran out, a bad page) is not raised here: the rows
+    concerned are undefined, and ``wino_read_device_status(ws)`` returns the first failure of any layer since it was last read,
+    so once per step, or per decode, is enough.  The decode loops do not know the cache and do not ask.
     """
 
     def __init__(self, n_layers: int, n_seq: int, seq_len: int, blk_len: int, n_q_heads: int, n_kv_heads: int,
