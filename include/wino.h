@@ -449,8 +449,9 @@ WINO_API int wino_rope_frequencies(int32_t rot_dim, double base, int32_t scaling
  *   k, v      [n_rows, n_kv_heads, head_dim]; both NULL: only q is rotated
  *   ws        workspace of which the first 256 bytes (status words) are used:
  *             wino_attend's, or 256 bytes of its own, zero-filled before its
- *             first use.  An error found on the device stays there until a
- *             wino_attend with the same workspace has reported it.
+ *             first use.  An error found on the device is reported by
+ *             wino_read_device_status once, and by the next wino_attend with
+ *             the same workspace, whose cache lacks the rows.
  * Two rows of a call that are stored in one slot race.
  */
 WINO_API int wino_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
@@ -490,10 +491,10 @@ WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale
  * (published by its last kernel): WINO_OK, WINO_ERR_DEVICE_TIMEOUT (a bounded
  * wait expired), WINO_ERR_ARG (an active-sequence list entry out of range, or
  * what a batch's device arrays must not hold, see wino_kv_batch) or
- * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).  Of wino_attend
- * calls, of which a step makes one per layer on one workspace, it returns the
- * first failure since the status of `ws` was last read, and clears it: one read
- * per step tells of all its layers.
+ * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).  Of wino_rope_append
+ * and wino_attend calls, of which a step makes some per layer on one workspace,
+ * it returns the first failure since the status of `ws` was last read, and
+ * clears it: one read per step tells of all its layers.
  */
 WINO_API int wino_read_device_status(void *ws, void *stream, int *device_status);
 

@@ -1160,7 +1160,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         __threadfence();
         if (atomicAdd(&a.status->finished, 1u) + 1u == gridDim.x) {
             __threadfence();
-            failed = atomicExch(&a.status->current, (int32_t)WINO_OK);
+            failed = -abs(atomicExch(&a.status->current, (int32_t)WINO_OK));  // positive: an append's, already read
             if (failed && a.status->first == WINO_OK)
                 a.status->first = failed;
             a.status->finished = 0;

@@ -132,7 +132,10 @@ constexpr int kMaxRecordsPerRow = 256;
 // which `finished` counts (zero between calls).  A workspace starts zeroed.
 // wino_attend publishes failures only, as `first`, which stays until
 // wino_read_device_status has returned it: a step's layers share a workspace,
-// and the ones behind a failed one must not hide it.
+// and the ones behind a failed one must not hide it.  wino_rope_append leaves its
+// errors in `current`, for the wino_attend that reads the cache; once
+// wino_read_device_status has returned such a one it makes it positive there, and
+// only that wino_attend still reports it.
 struct StatusWords {
     int32_t current;
     int32_t last;

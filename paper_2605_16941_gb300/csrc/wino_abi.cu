@@ -6,6 +6,7 @@
 // wino_read_device_status, which reads the status words back.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <mutex>
 
@@ -572,10 +573,14 @@ int wino_read_device_status(void *ws, void *stream, int *device_status)
     if (cudaMemcpy(&w, ws, sizeof w, cudaMemcpyDeviceToHost) != cudaSuccess)
         return WINO_ERR_CUDA;
     // `current` outlives a call only where no later kernel of it publishes: wino_rope_append's errors
-    *device_status = w.first ? w.first : (w.current ? w.current : w.last);
-    if (w.first && (cudaMemsetAsync(&static_cast<StatusWords *>(ws)->first, 0, sizeof w.first, s) != cudaSuccess ||
-                    cudaStreamSynchronize(s) != cudaSuccess))
-        return WINO_ERR_CUDA;
+    *device_status = w.first ? w.first : (w.current < 0 ? w.current : w.last);
+    if (w.first || w.current < 0) {
+        w.first = WINO_OK;
+        w.current = std::abs(w.current);
+        if (cudaMemcpyAsync(ws, &w, sizeof w, cudaMemcpyHostToDevice, s) != cudaSuccess ||
+            cudaStreamSynchronize(s) != cudaSuccess)
+            return WINO_ERR_CUDA;
+    }
     return WINO_OK;
 }
 
