@@ -236,6 +236,29 @@ struct PartReader {
     __device__ __forceinline__ int slot() const { return (int)(count % kParts); }
 };
 
+// The parity of the last copy into slot s of a ring of `slots`, after `issued` > s copies that took the slots in turn.
+__host__ __device__ constexpr uint32_t last_parity(uint32_t issued, uint32_t s, uint32_t slots) { return ((issued - 1 - s) / slots) & 1u; }
+
+// Walks the ring as the copying warps do, slot by slot with the phase turned over at its end.
+constexpr bool last_parity_holds()
+{
+    for (uint32_t slots = 1; slots <= 8; ++slots) {
+        uint32_t last[8] = {}, slot = 0, phase = 0;
+        for (uint32_t issued = 1; issued <= 40; ++issued) {
+            last[slot] = phase;
+            if (++slot == slots) {
+                slot = 0;
+                phase ^= 1u;
+            }
+            for (uint32_t s = 0; s < slots && s < issued; ++s)
+                if (last_parity(issued, s, slots) != last[s])
+                    return false;
+        }
+    }
+    return true;
+}
+static_assert(last_parity_holds(), "drained parities");
+
 template <typename U>
 __device__ __forceinline__ U warp_sum(U x, int width)  // over groups of `width` lanes
 {
@@ -1017,12 +1040,14 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                     }
                 }
             }
-            if (aborted && lane == 0) {  // copies already issued land before the shared memory goes away
+            // All copies issued land before the shared memory goes away.  In a call that went well their readers waited for
+            // them, and each wait is one try.  Where any role gave up, this one may already be behind its last part.
+            if (lane == 0) {
                 if (parts > 0)
                     wait_drain(q_full, (parts - 1) & 1u);
                 const uint32_t slots = (uint32_t)(slot1 - slot0);
                 for (uint32_t s = 0; s < slots && s < issued; ++s)
-                    wait_drain(full(slot0 + (int)s), ((issued - 1 - s) / slots) & 1u);
+                    wait_drain(full(slot0 + (int)s), last_parity(issued, s, slots));
             }
             __syncwarp();
         } else if (warp == kWarpMma) {
