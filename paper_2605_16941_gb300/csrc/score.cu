@@ -271,8 +271,9 @@ __global__ void __launch_bounds__(kScoreThreads, 1)
                     }
                 }
             }
-            if (aborted && leader) {
-                // Let every copy already issued (by either CTA) land before the pair's shared memory goes away.
+            if (leader) {
+                // Every copy issued (by either CTA) lands before the pair's shared memory goes away.  In a launch that went
+                // well the MMAs waited for them, and each wait is one try; where another role gave up, this one may be done.
                 for (int s = 0; s < S && s < issued; ++s)
                     wait_drain(full(s), (uint32_t)((issued - 1 - s) / S) & 1u);
             }
