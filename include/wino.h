@@ -412,8 +412,8 @@ typedef struct {
 
 /* Rotary positions.  Pair j < rot_dim / 2 of a head's first rot_dim dims is (j, j + rot_dim / 2), or with
    `interleaved` (2j, 2j + 1); it is turned by position * freq[j] radians and multiplied by `factor`.  The other dims
-   are copied.  rot_dim = 0 rotates nothing.  Turns are formed in 64-bit fixed point, so far positions keep their
-   angles to 2^-31 turns. */
+   are copied.  rot_dim = 0 rotates nothing.  Turns are formed in 64-bit fixed point from freq / (2 pi) to 2^-63, so any
+   position keeps its angle to 2^-32 turns at any |freq| below 2^42. */
 typedef struct {
     int32_t rot_dim;     /* even, 0..head_dim */
     int32_t interleaved; /* 0: halves, 1: neighbouring pairs */

@@ -3,7 +3,8 @@
 // Pair (a, b) of a head at position x, turned by t = x f:  a' = m (a cos t - b sin t),  b' = m (b cos t + a sin t).
 // Angles: t / 2 pi modulo 1 is what matters, and x f in 32 bits loses it for far positions (x = 10^6, f = 1: 0.06
 // radians).  f / 2 pi is taken to a 64-bit fixed-point fraction of a turn once per CTA and pair; its product with the
-// position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.
+// position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.  The quotient is formed in two
+// doubles, since one alone is off by 2^-54 of itself or more, which positions from 2^24 and frequencies above 1 make visible.
 //
 // Bound by HBM: every element is read and written once, 16 bytes at a time (8 where head_dim or rot_dim is no multiple of
 // 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in
@@ -60,11 +61,15 @@ __device__ __forceinline__ uint16_t from_f<__half>(float x)
     return __half_as_ushort(__float2half_rn(x));
 }
 
-// The fraction of a turn per position, in units of 2^-64.
+// The fraction of a turn per position, in units of 2^-64, off by one at most for |radians| < 2^42: the product with 1 / (2 pi) as a
+// sum of two doubles, hi + lo, its remainder by fma.
 __device__ __forceinline__ uint64_t turn_fraction(double radians)
 {
-    const double x = radians * 0.15915494309189533577;  // 1 / (2 pi)
-    return (uint64_t)((x - floor(x)) * 18446744073709551616.0);
+    constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;  // 1 / (2 pi) = kHigh + kLow to 2^-110
+    const double hi = radians * kHigh;
+    const double lo = fma(radians, kLow, fma(radians, kHigh, -hi));
+    const int64_t turns = __double2ll_rn((hi - rint(hi)) * 18446744073709551616.0);  // the difference is exact
+    return (uint64_t)turns + (uint64_t)__double2ll_rn(lo * 18446744073709551616.0);
 }
 
 template <typename T>
