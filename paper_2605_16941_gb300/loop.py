@@ -217,7 +217,13 @@ class BlockCache:
     each other and everything before them: the prompt, or a block that is done, taken into the cache once.
     ``step(blk_start)`` describes the rows of a step as ``wino_step`` wants their hidden states, [s][kind][l] (with
     ``no_shadow`` [s][l]): block rows see the context and the block, shadow rows these and the shadow block but for the
-    position that they verify (Sec. 4.2.2).  Within a layer, ``append`` rotates q (in place) and stores k and v, then
+    position that they verify (Sec. 4.2.2).
+    Both leave out what lies to the right, the blocks that are still masked, which the rows of the paper see too
+    ([Y_left, Y_cur, Y_right, Y_shad]).  ``seen`` takes it in: the rows see the positions [0, seen), of which ``context`` must have stored
+    the ones behind the block.  The shadow block is stored in the ``blk_len`` slots from ``seen`` on, so a decode whose right side is
+    in the cache passes ``seen=seq_len`` to every step.  What is in the cache stays as its last pass made it, until ``context``
+    is called on it again; the paper's pass over everything is the rows left of the block, right of it and the step's, all with
+    ``seen=seq_len``, each layer storing all of them before any attends.  Within a layer, ``append`` rotates q (in place) and stores k and v, then
     ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws``, so a
     decode keeps to one stream.  What the device finds wrong (a wait that ran out, a bad page) is not raised here: the rows
     concerned are undefined, and ``wino_read_device_status(ws)`` returns the first failure of any layer since it was last read,
@@ -248,20 +254,27 @@ class BlockCache:
                               n_rows=self.n_seq * rows, n_q_heads=self.n_q_heads, mask=mask)
                 for i in range(self.n_layers)]
 
-    def context(self, start: int, end: int) -> list[WinoKvBatch]:
-        """Per layer, the batch of positions [start, end)."""
+    def _seen(self, end: int, seen: int | None) -> int:
+        seen = end if seen is None else seen
+        if not end <= seen <= self.seq_len:
+            raise ValueError(f"rows up to {end} that see {seen} of {self.seq_len} positions")
+        return seen
+
+    def context(self, start: int, end: int, *, seen: int | None = None) -> list[WinoKvBatch]:
+        """Per layer, the batch of positions [start, end), which see [0, seen) (default: up to ``end``)."""
         if not 0 <= start < end <= self.seq_len:
             raise ValueError(f"positions [{start}, {end}) of {self.seq_len}")
-        return self._batches(end - start, end, start, WINO_MASK_FULL)
+        return self._batches(end - start, self._seen(end, seen), start, WINO_MASK_FULL)
 
-    def step(self, blk_start: int) -> list[WinoKvBatch]:
-        """Per layer, the batch of a step on the block at ``blk_start``."""
+    def step(self, blk_start: int, *, seen: int | None = None) -> list[WinoKvBatch]:
+        """Per layer, the batch of a step on the block at ``blk_start``, whose rows see [0, seen) (default: up to the block's end)."""
         end = blk_start + self.blk_len
         if not 0 <= blk_start or end > self.seq_len:
             raise ValueError(f"block [{blk_start}, {end}) of {self.seq_len}")
+        seen = self._seen(end, seen)
         if self.no_shadow:
-            return self._batches(self.blk_len, end, blk_start, WINO_MASK_FULL)
-        return self._batches(2 * self.blk_len, end, blk_start, WINO_MASK_SHADOW)
+            return self._batches(self.blk_len, seen, blk_start, WINO_MASK_FULL)
+        return self._batches(2 * self.blk_len, seen, blk_start, WINO_MASK_SHADOW)
 
     def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope) -> None:
         wino_rope_append(q, k, v, batch, rope, self.ws)
