@@ -431,7 +431,12 @@ typedef struct {
  *                     r = trained_len * freq / (2 pi) turns in the trained
  *                     context, frequencies with r > 32 are kept, with r < 1
  *                     divided by scale, in between mixed linearly in r; and
- *                     *factor = 0.1 ln(scale) + 1
+ *                     *factor = 0.1 ln(scale) + 1.  That is the paper's ramp.
+ *                     Checkpoints whose configuration gives bounds other
+ *                     than 32 and 1, a factor of its own, or a ramp that is
+ *                     linear in the pair's index j between rounded ends
+ *                     were trained with other angles: pass their own
+ *                     frequencies and factor in wino_rope instead
  * *factor is 1 for the others.  Pure host code.  WINO_ERR_SHAPE for an odd or
  * negative rot_dim or one above 128, WINO_ERR_ARG for null pointers, base <= 1, scale < 1,
  * trained_len < 1 (PARTS), or values that are not finite.

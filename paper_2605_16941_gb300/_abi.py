@@ -409,7 +409,9 @@ def make_rope(freq, *, rot_dim: int, factor: float = 1.0, interleaved: bool = Fa
 
 def wino_rope_frequencies(rot_dim: int, base: float, *, scaling: str = "none", factor: float = 1.0,
                           trained_len: int = 1):
-    """(frequencies as a host float64 [rot_dim / 2] tensor, factor on the rotated values) for ``make_rope``."""
+    """(frequencies as a host float64 [rot_dim / 2] tensor, factor on the rotated values) for ``make_rope``.  ``scaling``: "none",
+    "linear", or "parts" as in arXiv 2309.00071, with a ramp in turns from 1 to 32; for a checkpoint trained with another ramp
+    or other bounds give ``make_rope`` frequencies and factor of its own."""
     import torch
     freq = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64)
     out = C.c_float(0)
