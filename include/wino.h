@@ -479,7 +479,7 @@ WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
  * at the end.  Rows of no sequence are left as they are.
  *   q, out  [n_rows, n_q_heads, head_dim]; out shares no element with q or the
  *           cache
- *   scale   > 0, < 2^127 (commonly head_dim^-1/2); scores and scale times scores
+ *   scale   >= 2^-126, < 2^127 (commonly head_dim^-1/2); scores and scale times scores
  *           have to be finite in fp32
  *   ws      256-byte aligned, zero-filled before its first use, used by
  *           wino_attend and wino_rope_append only; calls that may overlap on

@@ -134,7 +134,8 @@ int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const w
                 size_t ws_bytes, void *stream)
 {
     const Range range("wino_attend");
-    if (!ws || !aligned(ws, kStatusBytes) || !(scale > 0.f) || !(scale < 0x1p127f))
+    // scale * log2(e) is a normal number: a subnormal counts as zero in the kernel, and zero times a masked -inf is NaN
+    if (!ws || !aligned(ws, kStatusBytes) || !(scale >= 0x1p-126f) || !(scale < 0x1p127f))
         return WINO_ERR_ARG;
     int rc = check_batch(b);
     if (rc != WINO_OK)

@@ -80,6 +80,17 @@ def test_attend_refusals():
     assert call(n=100) == W
 
 
+def test_attend_refuses_subnormal_scales():
+    L = wino.lib()
+
+    def call(scale):  # a workspace too small for it is found behind the scale
+        return L.wino_attend(heads(), heads(FAKE * 2), scale, batch(), FAKE, 100, None)
+    for scale in (1e-45, 1e-42, 2.0 ** -127):
+        assert call(scale) == wino.WINO_ERR_ARG, scale
+    for scale in (2.0 ** -126, 1e-30):
+        assert call(scale) == wino.WINO_ERR_WORKSPACE, scale
+
+
 def test_append_refusals():
     L = wino.lib()
 
