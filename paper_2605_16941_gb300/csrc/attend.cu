@@ -20,21 +20,26 @@
 //
 // What bounds it (us; floors from 6.7 TB/s and 1.9 PFLOP/s):
 //   few rows per slot: the K and V stream from HBM.  64 tokens over 500 to 32767 slots, 32 heads over 8 kv heads of 128:
-//     2.05 GB in 304 to 308 = 6.7 TB/s (floor 306).  With one warp for all copies 407: a warp issues a 2 KB box in 68 to 130
+//     2.05 GB in 303 to 308 = 6.7 TB/s (floor 306).  With one warp for all copies 407: a warp issues a 2 KB box in 68 to 130
 //     clocks, so K and V have a warp each and a page's halves one box.
 //   many rows, 128 dims: each warpgroup's chain of scores (512 clocks), softmax (1400) and P V (512, half of it behind the
 //     second half of the weights); two warpgroups overlap to 2500 to 2700 clocks per pair of tiles, against 2048 of MMAs.
-//     Four prompts of up to 8192 tokens, 32 heads: 376 (floor 313), 1.58 PFLOP/s of products that the mask keeps; 411 where
+//     Four prompts of up to 8192 tokens, 32 heads: 379 (floor 313), 1.57 PFLOP/s of products that the mask keeps; 413 where
 //     calls follow one another for long and the power cap lowers the clock.
 //   many rows, 64 dims: the softmax, 2100 to 2400 clocks per pair of tiles, 1024 of them exponentials (32 a clock and SM)
 //     and the rest mostly latencies of loads, votes and barriers, which two warps per scheduler do not hide.  Two threads
 //     per row (16 softmax warps of 104 registers) take the same time, at 128 dims too: each repeats the latencies.
-//   short calls: 1.4 of launch, 1.5 of plan, then one latency after the other; 32 heads over 300 slots 9.5.
+//   short calls: 1.4 of launch, 1.5 of plan, then one latency after the other; 32 heads over 300 slots 9.6.
+//   many short sequences: every CTA's plan loads all lengths, 32 sequences a round and twice where there are more, and each task
+//     pays its own chain of latencies.  Single tokens over 61 slots, 8 heads of 64 over 2: 10 for 32 sequences, 28 for 256, 88
+//     for 1024, 353 for 4096, 1560 for 16384 (floor 81).
 //
+// Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one box.
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
-// 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  m follows
-// the row's maximum only when that has grown by more than some bits (kRescaleBits), so that O is rarely rescaled; the quotient
-// O / l does not depend on m.  fp16 has 40 bits of range, subnormals included, and many small weights may add up to the result:
+// 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  Against 64 bits out
+// is 1.2 to 1.4 times as far off as with fp32 weights.  In the online softmax (arXiv 1805.02867) any m serves that keeps the
+// exponentials in range: here it follows the row's maximum only when that has grown by more than some bits (kRescaleBits), so
+// that O is rarely rescaled; the quotient O / l does not depend on m.  fp16 has 40 bits of range, subnormals included, and many small weights may add up to the result:
 // there P, l and O carry a factor 2^kTopBits that the quotient drops.  P ends at 2^15.9 < 65504, a weight keeps all its bits down to
 // 2^-23.9 of the row's largest, and what is lost below is 2^-34.9 each.  More bits above leave fewer to grow and rescale O more
 // often: with 4 / 5 / 6 / 8 to grow, four prompts in fp16 take 430 / 399 / 393 / 389 us, the chunks of 64 dims 76.7 / 75.6 / 74.7 / 72.8.
@@ -331,8 +336,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
             tasks += warp_total(sub == 0 ? (U)n_tasks : (U)0);
         }
         // Few and short tasks: one row tile each gives twice as many, for twice the copies of K and V, and fewer parts to
-        // join.  256 rows of each of 32 heads behind 1025 / 4097 / 16385 slots (runs of 3 / 8 / 28 units): 17.9 / 28.7 / 99.9 us
-        // with one row tile, 23.3 / 33.5 / 68.3 with two; 64 rows of 4 heads to each of 8 behind 8193 (14): 40.4 and 42.5.
+        // join.  256 rows of each of 32 heads behind 1025 / 4097 / 16385 slots (runs of 3 / 8 / 28 units): 16.8 / 28.1 / 97.4 us
+        // with one row tile, 22.5 / 32.7 / 66.8 with two; 64 rows of 4 heads to each of 8 behind 8193 (14): 28.7 and 35.8.
         if (row_tiles == 1 || a.b.n_rows <= a.positions || tasks * (U)n_kv * 2 > (U)gridDim.x ||
             total * (U)n_kv > (U)gridDim.x * 16)
             break;
@@ -346,7 +351,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, Shared &sh, int lane)
     // The current task: `index` among its kv head's.  A sequence's tasks come by kv head and index while there are no more
     // than CTAs: neighbours of nearly one length are then cut alike.  More of them come by index and kv head, so that
     // CTAs some way apart read one head's K and V at the same time and one of them finds it in the L2 cache.  4 x 512 rows of 32
-    // heads (256 tasks) 82.7 and 79.4 us; 256 rows of 32 heads behind 1025 slots (64 tasks) 16.8 and 23.6.
+    // heads (256 tasks) 82.1 and 79.7 us; 256 rows of 32 heads behind 1025 slots (64 tasks) 16.8 and 23.5.
     const bool by_index = tasks * (U)n_kv > (U)cut.n;
     int32_t seq = 0, kv_head = 0, index = 0;
     U task = 0;  // the unit at which the current task starts
@@ -1178,8 +1183,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         ptx::tmem_dealloc(tmem, kTmemAll);
     if (threadIdx.x == 0 && sh.abort)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_DEVICE_TIMEOUT);
-    // The last CTA publishes the outcome and clears it for the next call, and after a failure the nodes too, which parts
-    // that never came may have left.
+    // The last CTA publishes a failure and clears it for the next call, and with it the nodes, which parts that never came
+    // may have left.
     int32_t failed = 0;
     if (threadIdx.x == 0) {
         __threadfence();
@@ -1310,9 +1315,9 @@ int launch_attend(const wino_heads &q, const wino_heads &out, float scale, const
         a.magic[i] = (uint32_t)(((uint64_t(1) << 32) + w - 1) / w);
     }
     // A part that is left for another CTA to join is written and read in 2 to 3 us where all warps have rows, and in less
-    // than 1 us for a few rows, so that runs are longer there.  Runs of 6 / 8 / 12 at least: 18.4 / 17.0 / 17.0 us for a
-    // block of 128 + 128 rows behind 1025 slots (32 heads), 26.7 / 25.8 / 28.7 for 16 of 32 + 32; a few rows, one token over
-    // 300 slots, runs of 3 / 8: 9.7 / 14.9.
+    // than 1 us for a few rows, so that runs are longer there.  Runs of 6 / 8 / 12 at least: 18.3 / 16.8 / 16.9 us for a
+    // block of 128 + 128 rows behind 1025 slots (32 heads), 26.4 / 26.1 / 29.1 for 16 of 32 + 32; a few rows, one token over
+    // 300 / 4097 / 16385 slots, runs of 3: 9.7 / 22.3 / 28.7, of 8: 13.4 / 20.2 / 27.4.
     a.min_units = L.piece * L.quarters >= 256 ? 8 : 3;
     a.wide = attend_units(b) >= 2147483648.0;
     a.page_shift = -1;

@@ -9,9 +9,11 @@
 // Bound by HBM: every element is read and written once, 16 bytes at a time (8 where head_dim or rot_dim is no multiple of
 // 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in
 // registers, and walks the heads with the loads of two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of
-// 128 (100 MB) 16.3; 20027 rows of 32 + 2 x 8 heads, half of each rotated (492 MB), 84 = 5.9 TB/s.  Four heads in flight take
-// registers for one CTA per SM less: 19.8 and 96; one in flight 29 and 100; more CTAs than 4 of 256 threads per SM 19 to 26
-// and 85 to 101.
+// 128 (100 MB) 21.3 with inputs that change from call to call, 16.6 replayed from a CUDA graph on one input, which the L2 cache
+// holds in part; 20027 rows of 32 + 2 x 8 heads, half of each rotated (492 MB), 84 = 5.9 TB/s either way.  Replayed: four heads
+// in flight 19.2 and 98, one 18.9 and 96; at most 3 / 5 / 6 CTAs of 256 threads per SM instead of 4: 22.1 / 18.9 / 26.3 and
+// 88.8 / 83.2 / 96.4.  Rotations that are no multiple of 8 dims go pair by pair in 2-byte accesses: 20 dims of heads of 80 take 323
+// where 40 take 74.  A CTA looks for its rows among all sequences: 16384 sequences of one row 97.
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -304,7 +306,9 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     a.rope = rope;
     a.status = status;
     // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads
-    // (4 against 8 rows: 2048 rows 16.3 and 23.4 us, 20027 rows 89 and 84).
+    // (replayed, 32 + 2 x 32 heads of 128: 1 against 2 rows: 600 rows 7.0 and 7.7 us, 900 10.6 and 9.2; 2 against 4: 900 9.2 and 11.6,
+    // 1200 9.7 and 11.0, 2048 19.1 and 16.5; 4 against 8: 2048 16.5 and 23.1, 4096 33.6 and 32.0, 9000 73.1 and 71.8; and 20027 rows of
+    // 32 + 2 x 8 heads 90.5 and 83.6).
     a.rows_per_cta = b.n_rows >= 8192 ? 8 : (b.n_rows >= 1024 ? 4 : (b.n_rows >= 512 ? 2 : 1));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
