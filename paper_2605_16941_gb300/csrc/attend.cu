@@ -35,15 +35,18 @@
 //     for 1024, 353 for 4096, 1560 for 16384 (floor 81).
 //
 // Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one box.
+//
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
 // 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  Against 64 bits out
 // is 1.2 to 1.4 times as far off as with fp32 weights.  In the online softmax (arXiv 1805.02867) any m serves that keeps the
 // exponentials in range: here it follows the row's maximum only when that has grown by more than some bits (kRescaleBits), so
-// that O is rarely rescaled; the quotient O / l does not depend on m.  fp16 has 40 bits of range, subnormals included, and many small weights may add up to the result:
-// there P, l and O carry a factor 2^kTopBits that the quotient drops.  P ends at 2^15.9 < 65504, a weight keeps all its bits down to
-// 2^-23.9 of the row's largest, and what is lost below is 2^-34.9 each.  More bits above leave fewer to grow and rescale O more
-// often: with 4 / 5 / 6 / 8 to grow, four prompts in fp16 take 430 / 399 / 393 / 389 us, the chunks of 64 dims 76.7 / 75.6 / 74.7 / 72.8.
+// that O is rarely rescaled; the quotient O / l does not depend on m.  fp16 has 40 bits of range, subnormals included, and many
+// small weights may add up to the result: there P, l and O carry a factor 2^kTopBits that the quotient drops.  P ends at
+// 2^15.9 < 65504, a weight keeps all its bits down to 2^-23.9 of the row's largest, and what is lost below is 2^-34.9 each.
+// Scores may lie anywhere in fp32: only their differences count, and far from zero these are formed before they are scaled.
+// More bits above leave fewer to grow and rescale O more often: with 4 / 5 / 6 / 8 to grow, four prompts in fp16 take 430 / 399 / 393 / 389 us, the chunks of 64 dims 76.7 / 75.6 / 74.7 / 72.8.
 #include <algorithm>
+#include <cfloat>
 #include <cstring>
 #include <mutex>
 
@@ -68,6 +71,7 @@ constexpr int kTaskCost = 3;            // what a task costs beside its slot til
 constexpr int kSnap = 2;                // a cut this near to a task's border (in slot tiles) is moved there
 constexpr float kRescaleBits[2] = {6.f, 8.f};  // fp16, bf16
 constexpr float kTopBits[2] = {9.9f, 0.f};     // the P of a score of m is 2^this
+constexpr float kFarBits = 65536.f;            // up to here m sl2 is rounded by 2^-8 at most: P stays below 65504
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kSharedBytes = 3 * 1024;  // for struct Shared, behind the tiles
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
@@ -666,7 +670,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const uint32_t t_p = lanes + C::kTmemP + (uint32_t)g * C::kStrideP;
         const int pos_in_tile = r / a.group;
         const float sl2 = a.scale_log2;
-        const float rescale = kRescaleBits[kBf16] / sl2;
+        constexpr float kTop = kTopBits[kBf16];
+        const float rescale = fminf(kRescaleBits[kBf16] / sl2, FLT_MAX);  // the growth that m does not follow, in units of S
         uint32_t done = 0;   // slot tiles of this warpgroup so far
         uint32_t joins = 0;  // joined parts so far
         uint32_t leads = 0;  // parts with both row tiles so far
@@ -684,6 +689,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             }
             const bool any = __any_sync(0xffffffffu, valid);
             float m = -INFINITY, l = 0.f;  // m in units of S
+            bool far = false;              // of any of the warp's rows
             const int32_t step = two ? 1 : 2, first = two ? 0 : g;
             lim -= (part.j0 + first) * kTileN;
             hole -= (part.j0 + first) * kTileN;
@@ -736,28 +742,45 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
                         y[k] = fmaxf(y[k], x[3][k + 24]);
                     }
                     const float mx = ptx::max3(ptx::max3(y[0], y[1], y[2]), ptx::max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
-                    const bool grow = mx > m + (m == -INFINITY ? 0.f : rescale);
-                    if (t != first && __any_sync(0xffffffffu, grow && m != -INFINITY)) {
-                        // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
-                        if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
-                            break;
-                        ptx::tc_fence_after();
-                        const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
-                        l *= f;
+                    const bool grow = mx - m > rescale;  // the difference is exact where it is close
+                    if (__any_sync(0xffffffffu, grow)) {
+                        if (t != first) {
+                            // the O of earlier tiles is scaled to the new maximum; P V of the tile before is done first
+                            if (!(good = warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort)))
+                                break;
+                            ptx::tc_fence_after();
+                            const float f = (grow && m != -INFINITY) ? ptx::ex2((m - mx) * sl2) : 1.f;
+                            l *= f;
 #pragma unroll 1
-                        for (int c = 0; c < DP; c += 16) {
-                            uint32_t o[16];
-                            ptx::tmem_ld_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
-                            ptx::tmem_ld_wait();
+                            for (int c = 0; c < DP; c += 16) {
+                                uint32_t o[16];
+                                ptx::tmem_ld_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
+                                ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int k = 0; k < 16; ++k)
-                                o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            ptx::tmem_st_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
+                                for (int k = 0; k < 16; ++k)
+                                    o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                                ptx::tmem_st_32x32b_x16(lanes + C::kTmemO + (uint32_t)(g * DP + c), o);
+                            }
                         }
+                        if (grow)
+                            m = mx;
+                        far = __any_sync(0xffffffffu, m != -INFINITY && fabsf(m * sl2) >= kFarBits);
                     }
-                    if (grow)
-                        m = mx;
-                    const float neg = m == -INFINITY ? 0.f : fmaf(-m, sl2, kTopBits[kBf16]);
+                    // Where some row's m sl2 is far from zero its rounding would show in P, all of it from 2^24 on: the differences
+                    // are formed first there, which are exact near the maximum.
+                    float neg = m == -INFINITY ? 0.f : fmaf(-m, sl2, kTop);
+                    if (__builtin_expect(far, 0)) {
+                        const float base = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) {
+                                const float2 d = ptx::add2(make_float2(x[c][k], x[c][k + 1]), make_float2(base, base));
+                                x[c][k] = d.x;
+                                x[c][k + 1] = d.y;
+                            }
+                        neg = kTop;
+                    }
                     const float2 s2 = make_float2(sl2, sl2), n2 = make_float2(neg, neg);
                     float2 l0 = make_float2(0.f, 0.f), l1 = l0;
 #pragma unroll
