@@ -24,17 +24,17 @@
 //     clocks, so K and V have a warp each and a page's halves one box.
 //   many rows, 128 dims: each warpgroup's chain of scores (512 clocks), softmax (1400) and P V (512, half of it behind the
 //     second half of the weights); two warpgroups overlap to 2500 to 2700 clocks per pair of tiles, against 2048 of MMAs.
-//     Four prompts of up to 8192 tokens, 32 heads: 379 (floor 313), 1.57 PFLOP/s of products that the mask keeps; 413 where
+//     Four prompts of up to 8192 tokens, 32 heads: 380 (floor 313), 1.56 PFLOP/s of products that the mask keeps; 416 where
 //     calls follow one another for long and the power cap lowers the clock.
 //   many rows, 64 dims: the softmax, 2100 to 2400 clocks per pair of tiles, 1024 of them exponentials (32 a clock and SM)
 //     and the rest mostly latencies of loads, votes and barriers, which two warps per scheduler do not hide.  Two threads
 //     per row (16 softmax warps of 104 registers) take the same time, at 128 dims too: each repeats the latencies.
-//   short calls: 1.4 of launch, 1.5 of plan, then one latency after the other; 32 heads over 300 slots 9.6.
+//   short calls: 1.4 of launch, 1.5 of plan, then one latency after the other; 32 heads over 300 slots 9.7.
 //   many short sequences: every CTA's plan loads all lengths, 32 sequences a round and twice where there are more, and each task
-//     pays its own chain of latencies.  Single tokens over 61 slots, 8 heads of 64 over 2: 10 for 32 sequences, 28 for 256, 88
-//     for 1024, 353 for 4096, 1560 for 16384 (floor 81).
+//     pays its own chain of latencies.  Single tokens over 61 slots, 8 heads of 64 over 2: 10 for 32 sequences, 29 for 256, 92
+//     for 1024, 371 for 4096, 1620 for 16384 (floor 81).
 //
-// Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one box.
+// Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one device.
 //
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside
 // 16-bit values (half a step per weight, as much as the result's own rounding); l sums the unrounded weights.  Against 64 bits out
@@ -44,7 +44,8 @@
 // small weights may add up to the result: there P, l and O carry a factor 2^kTopBits that the quotient drops.  P ends at
 // 2^15.9 < 65504, a weight keeps all its bits down to 2^-23.9 of the row's largest, and what is lost below is 2^-34.9 each.
 // Scores may lie anywhere in fp32: only their differences count, and far from zero these are formed before they are scaled.
-// More bits above leave fewer to grow and rescale O more often: with 4 / 5 / 6 / 8 to grow, four prompts in fp16 take 430 / 399 / 393 / 389 us, the chunks of 64 dims 76.7 / 75.6 / 74.7 / 72.8.
+// More bits above leave fewer to grow and rescale O more often: with 4 / 5 / 6 / 8 to grow, four prompts in fp16 take 430 / 399 /
+// 393 / 389 us, the chunks of 64 dims 76.7 / 75.6 / 74.7 / 72.8.
 #include <algorithm>
 #include <cfloat>
 #include <cstring>
