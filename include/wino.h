@@ -282,7 +282,8 @@ WINO_API int wino_step_static_scratch(const uint16_t *H, const uint16_t *W, int6
  * at position p->blk_start + b * p->blk_len; each block is stepped with
  * wino_step until none of its positions is MASK in any sequence.  The
  * hidden states of every step come from the caller, who runs the transformer's
- * layers (wino_rope_append and wino_attend are their attention):
+ * layers (wino_rope_append and wino_attend are their attention, or wino_norm_rope_append
+ * and wino_attend_scaled):
  *   hidden(user, k, blk_start) returns the device bf16 rows of global step k
  *   for the block at blk_start, laid out as wino_step's H, and must stay
  *   valid until the next call of `hidden` or the return of wino_decode;
@@ -375,7 +376,8 @@ WINO_API int wino_decode(const uint16_t *W, int64_t d, int64_t V, int32_t *token
  */
 typedef enum {
     WINO_BF16 = 0, /* elements of q, k, v, out and the cache; all the same type */
-    WINO_FP16 = 1
+    WINO_FP16 = 1,
+    WINO_CACHE_E4M3 = 16 /* added to one of these: the cache holds 8-bit values, see wino_kv_scales */
 } wino_dtype;
 
 typedef enum {
@@ -406,8 +408,8 @@ typedef struct {
     int32_t table_width; /* entries of page_table per sequence; table_width * page_size <= 2^30 */
     const int32_t *q_start, *q_len, *kv_len, *new_slot; /* [n_seq] each */
     const int32_t *page_table; /* [n_seq, table_width]; entries that hold no slot of the sequence are not read */
-    uint16_t *k_cache, *v_cache; /* 16-byte aligned; written by wino_rope_append only */
-    int64_t page_stride, slot_stride, head_stride; /* of both, in elements: multiples of 8 */
+    uint16_t *k_cache, *v_cache; /* 16-byte aligned; written by wino_rope_append and wino_norm_rope_append only */
+    int64_t page_stride, slot_stride, head_stride; /* of both, in elements: multiples of 8 (of 16 with WINO_CACHE_E4M3) */
 } wino_kv_batch;
 
 /* Rotary positions.  Pair j < rot_dim / 2 of a head's first rot_dim dims is (j, j + rot_dim / 2), or with
@@ -490,6 +492,87 @@ WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
  */
 WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b, void *ws,
                          size_t ws_bytes, void *stream);
+
+/*
+ * The cache in 8 bits.  A batch whose dtype has WINO_CACHE_E4M3 added describes
+ * a cache of bytes (k_cache and v_cache point to them; head_dim and the strides
+ * are multiples of 16): the K and the V of a slot and head are head_dim e4m3
+ * codes c (1 sign, 4 exponent, 3 mantissa bits, largest 448) and one scale byte
+ * s, which stand for the values c 2^(s - 127).  A row z is written as
+ *     e = the least integer in [e_min, 7] with max |z| <= 448 2^e (7 where none is),
+ *         e_min = -110 for WINO_BF16, -14 for WINO_FP16
+ *     c = z 2^-e rounded to the nearest code, ties to even; s = e + 127
+ * so that a value keeps 4 significant bits unless it is below 2^-13.8 of its row's
+ * largest or below 2^(e_min - 6), values beyond +-57344 are held as that, and every
+ * value read is exact in the element type.  A row with an infinity or NaN is
+ * held as s = 255 and reads as NaN throughout.  The codes 0x7f and 0xff and the
+ * scales from 135 to 254 are not written, and must not be in slots that some
+ * row sees.
+ * wino_norm_rope_append writes such a cache, wino_cache_read takes rows out of
+ * it, wino_attend_scaled attends over it; wino_rope_append and wino_attend
+ * refuse it with WINO_ERR_ARG.
+ */
+typedef struct {
+    uint8_t *k_scale, *v_scale; /* device [n_pages, n_kv_heads, page_size], 16-byte aligned */
+} wino_kv_scales;
+
+/* Norms of queries and keys: each head x of a row becomes x (offset + weight) / sqrt(mean(x^2) + eps), in fp32 and not
+   rounded before the rotation. */
+typedef struct {
+    const uint16_t *q_weight, *k_weight; /* device, element type, 16-byte aligned, [head_dim] per head; NULL: q (or k) is not normalised */
+    int64_t q_head_stride, k_head_stride; /* elements from one head's weights to the next: 0 (all heads share them) or a
+                                             multiple of 8 that is at least head_dim */
+    float eps;    /* 2^-60 .. 2^60 */
+    float offset; /* finite: 0, or 1 where the weights are kept as differences from 1 */
+} wino_head_norm;
+
+/* Rotary positions of several axes (time, height, width of images and video): pair j is turned by
+   positions[axis[j] * axis_stride + row] * freq[j]. */
+typedef struct {
+    int32_t n_axes;           /* 1..4 */
+    const uint8_t *axis;      /* device [rot_dim / 2], below n_axes */
+    const int32_t *positions; /* device [n_axes, n_rows], 4-byte aligned */
+    int64_t axis_stride;      /* at least n_rows where there is more than one axis */
+} wino_rope_axes;
+
+/*
+ * wino_rope_append for layers that normalise queries and keys per head, whose
+ * positions have several axes, or whose cache is in 8 bits: per row the norm, the
+ * rotation, both in fp32, and one rounding: of q and of an element-type cache's
+ * K to the element type, of an 8-bit cache's K and V to codes.
+ *   axes    NULL: one position per row as in wino_rope; else rope->positions
+ *           must be NULL.  An entry of `axis` that is n_axes or more ends in
+ *           WINO_ERR_ARG from wino_read_device_status, its pairs undefined
+ *   norm    NULL: no norms
+ *   scales  the 8-bit cache's scales; NULL for a cache of the element type
+ * Everything else as for wino_rope_append, whose results it gives where the
+ * three are NULL.
+ */
+WINO_API int wino_norm_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k,
+                                   const wino_heads *v, const wino_kv_batch *b, const wino_rope *rope,
+                                   const wino_rope_axes *axes, const wino_head_norm *norm, const wino_kv_scales *scales,
+                                   void *ws, void *stream);
+
+/*
+ * The append's inverse: K and V of every row of every sequence, from the slots
+ * at which the mask stores them into k and v [n_rows, n_kv_heads, head_dim] of
+ * the element type (either may be NULL), from a cache of the element type
+ * (scales NULL) or of 8 bits: to hand a prompt's rows to another cache, say.
+ * No rotation is undone.  Rows of no sequence and rows with a negative slot are
+ * left as they are.  k and v share no element with each other or the cache.
+ * ws and errors found on the device as for wino_rope_append.
+ */
+WINO_API int wino_cache_read(const wino_heads *k, const wino_heads *v, const wino_kv_batch *b,
+                             const wino_kv_scales *scales, void *ws, void *stream);
+
+/*
+ * wino_attend over an 8-bit cache: the same rows, masks, arguments, workspace
+ * and errors, K and V the values that codes and scales stand for.  The result is
+ * that of wino_attend over a cache of the element type that holds these values.
+ * Codes and scales in slots that no row of the sequence sees have no effect.
+ */
+WINO_API int wino_attend_scaled(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b,
+                                const wino_kv_scales *scales, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Waits for `stream`, then reads the outcome of the last call that used `ws`

@@ -16,6 +16,8 @@ from ._abi import (EXPORTS, WINO_STATIC_SCRATCH_BYTES, FLAG_DRAFT, FLAG_DRAFT_FA
                    make_params, wino_draft_verify, wino_profile_begin, wino_profile_end, wino_read_device_status, wino_score_rows, wino_status_string, wino_step_static_scratch, wino_selftest_wait_timeout,
                    wino_step, wino_version, wino_workspace_size, workspace, wino_decode, WinoBlockStats,
                    make_kv_batch, make_rope, wino_rope_frequencies, wino_rope_append, wino_attend_workspace_size, attend_workspace, append_workspace, wino_attend,
+                   make_rope_axes, make_head_norm, wino_norm_rope_append, wino_cache_read, wino_attend_scaled,
+                   WinoKvScales, WinoHeadNorm, WinoRopeAxes, WINO_CACHE_E4M3,
                    WinoHeads, WinoKvBatch, WinoRope, WINO_BF16, WINO_FP16, WINO_MASK_FULL, WINO_MASK_CAUSAL, WINO_MASK_SHADOW)
 
 __all__ = [
@@ -26,5 +28,7 @@ __all__ = [
     "make_params", "wino_draft_verify", "wino_profile_begin", "wino_profile_end", "wino_read_device_status", "wino_score_rows", "wino_status_string", "wino_step_static_scratch", "wino_selftest_wait_timeout",
     "wino_step", "wino_version", "wino_workspace_size", "workspace", "wino_decode", "WinoBlockStats",
     "make_kv_batch", "make_rope", "wino_rope_frequencies", "wino_rope_append", "wino_attend_workspace_size", "attend_workspace", "append_workspace", "wino_attend",
+    "make_rope_axes", "make_head_norm", "wino_norm_rope_append", "wino_cache_read", "wino_attend_scaled",
+    "WinoKvScales", "WinoHeadNorm", "WinoRopeAxes", "WINO_CACHE_E4M3",
     "WinoHeads", "WinoKvBatch", "WinoRope", "WINO_BF16", "WINO_FP16", "WINO_MASK_FULL", "WINO_MASK_CAUSAL", "WINO_MASK_SHADOW",
 ]

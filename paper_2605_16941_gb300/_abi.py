@@ -36,10 +36,12 @@ EXPORTS = ("wino_workspace_size", "wino_workspace_size_step", "wino_score_rows",
            "wino_step_static_scratch", "wino_read_device_status", "wino_profile_begin", "wino_profile_end",
            "wino_selftest_wait_timeout", "wino_status_string", "wino_version", "wino_decode", "wino_timeline_begin",
            "wino_timeline_end", "wino_score_plan", "wino_score_plan_host", "wino_score_launch", "wino_lm_head_panels",
-           "wino_rope_frequencies", "wino_rope_append", "wino_attend_workspace_size", "wino_attend")
+           "wino_rope_frequencies", "wino_rope_append", "wino_attend_workspace_size", "wino_attend",
+           "wino_norm_rope_append", "wino_cache_read", "wino_attend_scaled")
 
 # wino_kv_batch.dtype, wino_kv_batch.mask, scalings of wino_rope_frequencies
 WINO_BF16, WINO_FP16 = 0, 1
+WINO_CACHE_E4M3 = 16
 WINO_MASK_FULL, WINO_MASK_CAUSAL, WINO_MASK_SHADOW = 0, 1, 2
 ROPE_SCALINGS = {"none": 0, "linear": 1, "parts": 2}
 
@@ -92,6 +94,22 @@ class WinoRope(C.Structure):
                 ("positions", C.c_void_p)]
 
 
+class WinoKvScales(C.Structure):
+    """wino_kv_scales; ``make_kv_batch`` makes one beside the batch of an 8-bit cache."""
+    _fields_ = [("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class WinoHeadNorm(C.Structure):
+    """wino_head_norm; ``make_head_norm`` makes one and keeps its tensors alive."""
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_head_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("eps", C.c_float), ("offset", C.c_float)]
+
+
+class WinoRopeAxes(C.Structure):
+    """wino_rope_axes; ``make_rope_axes`` makes one and keeps its tensors alive."""
+    _fields_ = [("n_axes", C.c_int32), ("axis", C.c_void_p), ("positions", C.c_void_p), ("axis_stride", C.c_int64)]
+
+
 # const uint16_t *(*)(void *user, int32_t step, int32_t blk_start)
 HIDDEN_FN = C.CFUNCTYPE(C.c_void_p, C.c_void_p, C.c_int32, C.c_int32)
 
@@ -128,6 +146,14 @@ def lib() -> C.CDLL:
         L.wino_attend_workspace_size.argtypes = [batch, C.POINTER(sz)]
         L.wino_attend.restype = C.c_int
         L.wino_attend.argtypes = [heads, heads, C.c_float, batch, vp, sz, vp]
+        scales = C.POINTER(WinoKvScales)
+        L.wino_norm_rope_append.restype = C.c_int
+        L.wino_norm_rope_append.argtypes = [heads, heads, heads, heads, batch, C.POINTER(WinoRope),
+                                            C.POINTER(WinoRopeAxes), C.POINTER(WinoHeadNorm), scales, vp, vp]
+        L.wino_cache_read.restype = C.c_int
+        L.wino_cache_read.argtypes = [heads, heads, batch, scales, vp, vp]
+        L.wino_attend_scaled.restype = C.c_int
+        L.wino_attend_scaled.argtypes = [heads, heads, C.c_float, batch, scales, vp, sz, vp]
         L.wino_lm_head_panels.restype = C.c_int
         L.wino_lm_head_panels.argtypes = [vp, i64, i64, vp, vp]
         L.wino_step_static_scratch.restype = C.c_int
@@ -361,16 +387,19 @@ def _require(ok: bool, where: str, status: int = WINO_ERR_ARG) -> None:
 
 
 def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot, *, n_rows: int, n_q_heads: int,
-                  mask: int) -> WinoKvBatch:
+                  mask: int, k_scale=None, v_scale=None, dtype=None) -> WinoKvBatch:
     """wino_kv_batch over a paged cache.  ``k_cache`` and ``v_cache`` are [n_pages, page_size, n_kv_heads, head_dim]
     views of one layout (a [pages, heads, slots, dim] cache is given as ``cache.transpose(1, 2)``), bfloat16, float16
     or 16-bit integers that hold bfloat16; ``page_table`` [n_seq, width] and the four length and slot arrays [n_seq]
-    are contiguous int32 on the same device.  The batch keeps the tensors alive."""
+    are contiguous int32 on the same device.  An 8-bit cache is float8_e4m3fn (or uint8 that holds such codes), with
+    ``k_scale`` and ``v_scale`` contiguous uint8 [n_pages, n_kv_heads, page_size] and ``dtype`` the rows' element type
+    (bfloat16 by default).  The batch keeps the tensors alive."""
     import torch
     where = "make_kv_batch"
     ints = (page_table, q_start, q_len, kv_len, new_slot)
+    scaled = k_scale is not None or v_scale is not None
     _require(k_cache.dim() == 4 and v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and
-             k_cache.element_size() == 2 and page_table.dim() == 2, where, WINO_ERR_SHAPE)
+             k_cache.element_size() == (1 if scaled else 2) and page_table.dim() == 2, where, WINO_ERR_SHAPE)
     n_pages, page_size, n_kv_heads, head_dim = k_cache.shape
     live = [i for i in range(4) if k_cache.shape[i] > 1]  # strides of single entries say nothing
     _require(all(k_cache.stride(i) == v_cache.stride(i) for i in live) and k_cache.stride(3) == 1, where,
@@ -379,14 +408,26 @@ def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot
              v_cache.device == k_cache.device, where)
     n_seq = page_table.size(0)
     _require(all(t.numel() == n_seq for t in ints[1:]), where, WINO_ERR_SHAPE)
+    elements, scales = k_cache.dtype, None
+    if scaled:
+        elements = torch.bfloat16 if dtype is None else dtype
+        _require(k_cache.dtype in (torch.float8_e4m3fn, torch.uint8) and elements in (torch.bfloat16, torch.float16) and
+                 all(t is not None and t.dtype == torch.uint8 and t.is_contiguous() and t.device == k_cache.device
+                     for t in (k_scale, v_scale)), where)
+        _require(k_scale.shape == v_scale.shape == (n_pages, n_kv_heads, page_size), where, WINO_ERR_SHAPE)
+        scales = WinoKvScales(_ptr(k_scale), _ptr(v_scale))
+        scales.tensors = (k_scale, v_scale)
+    else:
+        _require(dtype is None or dtype == elements, where)
     b = WinoKvBatch(n_seq, n_rows, n_q_heads, n_kv_heads, head_dim,
-                    WINO_FP16 if k_cache.dtype == torch.float16 else WINO_BF16, mask, page_size, n_pages,
-                    page_table.size(1), _ptr(q_start), _ptr(q_len), _ptr(kv_len), _ptr(new_slot), _ptr(page_table),
-                    _ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
+                    (WINO_FP16 if elements == torch.float16 else WINO_BF16) | (WINO_CACHE_E4M3 if scaled else 0), mask,
+                    page_size, n_pages, page_table.size(1), _ptr(q_start), _ptr(q_len), _ptr(kv_len), _ptr(new_slot),
+                    _ptr(page_table), _ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
     b.tensors = (k_cache, v_cache, *ints)
+    b.scales = scales
     # plain attributes: what the calls compare with, cheaper than the struct's fields
     b.q_shape, b.kv_shape = (n_rows, n_q_heads, head_dim), (n_rows, n_kv_heads, head_dim)
-    b.elements, b.device = k_cache.dtype, k_cache.get_device()
+    b.elements, b.device = elements, k_cache.get_device()
     b.devices = {b.device}
     return b
 
@@ -405,6 +446,38 @@ def make_rope(freq, *, rot_dim: int, factor: float = 1.0, interleaved: bool = Fa
     r.devices = {t.get_device() for t in r.tensors if t is not None}
     r.n_positions = None if positions is None else positions.numel()
     return r
+
+
+def make_rope_axes(axis, positions) -> WinoRopeAxes:
+    """wino_rope_axes: ``axis`` device uint8 [rot_dim / 2], the axis of each pair; ``positions`` device int32
+    [n_axes, n_rows] (rows of a wider array will do)."""
+    import torch
+    where = "make_rope_axes"
+    _require(positions.dim() == 2 and axis.dim() == 1, where, WINO_ERR_SHAPE)
+    _require(axis.dtype == torch.uint8 and axis.is_contiguous() and positions.dtype == torch.int32 and
+             (positions.size(1) == 1 or positions.stride(1) == 1) and axis.device == positions.device, where)
+    a = WinoRopeAxes(positions.size(0), _ptr(axis), _ptr(positions), positions.stride(0))
+    a.tensors = (axis, positions)
+    a.device = positions.get_device()
+    a.n_pairs, a.n_positions = axis.numel(), positions.size(1)
+    return a
+
+
+def make_head_norm(q_weight, k_weight, *, eps: float = 1e-6, offset: float = 0.0) -> WinoHeadNorm:
+    """wino_head_norm: device weights of the element type, [head_dim] for all heads or [heads, head_dim], None for what is not
+    normalised; ``offset`` 1 for weights that are kept as differences from 1."""
+    where = "make_head_norm"
+    given = [w for w in (q_weight, k_weight) if w is not None]
+    _require(all(w.dim() in (1, 2) for w in given), where, WINO_ERR_SHAPE)
+    _require(all(w.stride(-1) == 1 and w.element_size() == 2 for w in given) and
+             len({(w.device, w.dtype) for w in given}) < 2, where)
+    n = WinoHeadNorm(_ptr(q_weight), _ptr(k_weight), *(w.stride(0) if w is not None and w.dim() == 2 and w.size(0) > 1 else 0
+                                                       for w in (q_weight, k_weight)), eps, offset)
+    n.tensors = (q_weight, k_weight)
+    n.devices = {w.get_device() for w in given}
+    n.elements = given[0].dtype if given else None
+    n.shapes = tuple(None if w is None else tuple(w.shape) for w in (q_weight, k_weight))
+    return n
 
 
 def wino_rope_frequencies(rot_dim: int, base: float, *, scaling: str = "none", factor: float = 1.0,
@@ -431,10 +504,8 @@ def _heads(t, b: WinoKvBatch, shape, where: str) -> WinoHeads:
     return WinoHeads(t.data_ptr(), row, head)
 
 
-def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=None, stream=None) -> None:
-    """Rotate the rows' queries (into ``q_out``, or in place) and write their rotated keys and their values into the
-    batch's cache.  ``q`` None: the cache alone; ``k`` and ``v`` None: the queries alone."""
-    where = "wino_rope_append"
+def _append_args(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, q_out, where: str):
+    """The heads of an append, checked together with what is common to both appends."""
     qh = qo = kh = vh = None
     if q is not None:
         qh = _heads(q, batch, batch.q_shape, where)
@@ -450,7 +521,48 @@ def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=N
     # the kernels run on the current device; wino_rope_frequencies' values are on the host
     if not rope.devices <= batch.devices or batch.device != _current_device() or ws.get_device() != batch.device:
         raise WinoError(WINO_ERR_ARG, where)
-    _check(lib().wino_rope_append(qh, qo, kh, vh, batch, rope, _ptr(ws), _stream(stream)), where)
+    return qh, qo, kh, vh
+
+
+def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=None, stream=None) -> None:
+    """Rotate the rows' queries (into ``q_out``, or in place) and write their rotated keys and their values into the
+    batch's cache.  ``q`` None: the cache alone; ``k`` and ``v`` None: the queries alone."""
+    where = "wino_rope_append"
+    heads = _append_args(q, k, v, batch, rope, ws, q_out, where)
+    _check(lib().wino_rope_append(*heads, batch, rope, _ptr(ws), _stream(stream)), where)
+
+
+def wino_norm_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, norm: WinoHeadNorm | None = None,
+                          axes: WinoRopeAxes | None = None, q_out=None, stream=None) -> None:
+    """``wino_rope_append`` with per-head norms of queries and keys (``norm``), positions of several axes (``axes``, with a
+    ``rope`` without positions), and into an 8-bit cache where ``batch`` has one."""
+    where = "wino_norm_rope_append"
+    heads = _append_args(q, k, v, batch, rope, ws, q_out, where)
+    if axes is not None:
+        if axes.n_positions != batch.q_shape[0] or axes.n_pairs != rope.rot_dim // 2:
+            raise WinoError(WINO_ERR_SHAPE, where)
+        if axes.device != batch.device:
+            raise WinoError(WINO_ERR_ARG, where)
+    if norm is not None:
+        for shape, want in zip(norm.shapes, (batch.q_shape, batch.kv_shape)):
+            if shape is not None and shape != want[2:] and shape != want[1:]:
+                raise WinoError(WINO_ERR_SHAPE, where)
+        if not norm.devices <= batch.devices or norm.elements not in (None, batch.elements):
+            raise WinoError(WINO_ERR_ARG, where)
+    _check(lib().wino_norm_rope_append(*heads, batch, rope, axes, norm, batch.scales, _ptr(ws), _stream(stream)), where)
+
+
+def wino_cache_read(k, v, batch: WinoKvBatch, ws, *, stream=None) -> None:
+    """The batch's rows out of its cache, from the slots at which an append with the same batch stores them, into ``k`` and ``v``
+    [n_rows, n_kv_heads, head_dim] (either may be None)."""
+    where = "wino_cache_read"
+    kh = None if k is None else _heads(k, batch, batch.kv_shape, where)
+    vh = None if v is None else _heads(v, batch, batch.kv_shape, where)
+    if _nbytes(ws) < STATUS_BYTES:
+        raise WinoError(WINO_ERR_WORKSPACE, where)
+    if batch.device != _current_device() or ws.get_device() != batch.device:
+        raise WinoError(WINO_ERR_ARG, where)
+    _check(lib().wino_cache_read(kh, vh, batch, batch.scales, _ptr(ws), _stream(stream)), where)
 
 
 def wino_attend_workspace_size(batch: WinoKvBatch) -> int:
@@ -471,14 +583,25 @@ def append_workspace(device=None):
     return torch.zeros(STATUS_BYTES, dtype=torch.uint8, device=device or "cuda")
 
 
-def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
-    """Attention of the batch's rows over its cache, into ``out``; ``scale`` defaults to head_dim^-1/2."""
-    where = "wino_attend"
+def _attend_args(q, out, batch: WinoKvBatch, ws, scale, where: str):
     qh, oh = _heads(q, batch, batch.q_shape, where), _heads(out, batch, batch.q_shape, where)
     if batch.device != _current_device() or ws.get_device() != batch.device:  # the kernels run on the current device
         raise WinoError(WINO_ERR_ARG, where)
-    _check(lib().wino_attend(qh, oh, batch.q_shape[2] ** -0.5 if scale is None else scale, batch, _ptr(ws), _nbytes(ws),
-                             _stream(stream)), where)
+    return qh, oh, batch.q_shape[2] ** -0.5 if scale is None else scale
+
+
+def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
+    """Attention of the batch's rows over its cache, into ``out``; ``scale`` defaults to head_dim^-1/2."""
+    where = "wino_attend"
+    qh, oh, scale = _attend_args(q, out, batch, ws, scale, where)
+    _check(lib().wino_attend(qh, oh, scale, batch, _ptr(ws), _nbytes(ws), _stream(stream)), where)
+
+
+def wino_attend_scaled(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
+    """``wino_attend`` over an 8-bit cache."""
+    where = "wino_attend_scaled"
+    qh, oh, scale = _attend_args(q, out, batch, ws, scale, where)
+    _check(lib().wino_attend_scaled(qh, oh, scale, batch, batch.scales, _ptr(ws), _nbytes(ws), _stream(stream)), where)
 
 
 def wino_read_device_status(ws, stream=None) -> int:

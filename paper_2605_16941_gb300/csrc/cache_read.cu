@@ -1,0 +1,84 @@
+// cache_read.cu -- wino_cache_read: K and V of the batch's rows out of the cache's pages, codes as the values they stand for.
+//
+// Bound by HBM: each element is read and written once; a thread moves 8 elements of a head (16 bytes, from 8 codes or 16 bytes).
+#include "e4m3.cuh"
+#include "ptx.cuh"
+#include "rope_rows.cuh"
+
+namespace wino {
+namespace {
+
+constexpr int kThreads = kRopeThreads;
+
+struct ReadArgs {
+    wino_heads k, v;
+    wino_kv_batch b;
+    wino_kv_scales scales;
+    StatusWords *status;
+    int32_t rows_per_cta;
+};
+
+template <bool kScaled, bool kBf16>
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ ReadArgs a)
+{
+    __shared__ Rows<1> sh;
+    const wino_kv_batch &b = a.b;
+    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
+    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
+    ptx::grid_dep_launch_dependents();
+    ptx::grid_dep_wait();
+    find_rows(b, wino_rope{}, nullptr, true, a.status, sh, row0, n_rows);
+    const int chunks = b.head_dim / 8, units = 2 * b.n_kv_heads * chunks;
+    for (int x = (int)threadIdx.x; x < n_rows * units; x += kThreads) {
+        const int r = x / units, y = x - r * units, h = y / chunks, c = y - h * chunks;
+        const bool is_v = h >= b.n_kv_heads;
+        const int hk = is_v ? h - b.n_kv_heads : h;
+        const wino_heads &to = is_v ? a.v : a.k;
+        if (sh.seq[r] < 0 || sh.page[r] < 0 || !to.data)
+            continue;
+        const int64_t at = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride + hk * b.head_stride + 8 * c;
+        const uint16_t *const cache = is_v ? b.v_cache : b.k_cache;
+        uint4 out;
+        if (kScaled) {
+            const uint2 codes = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(cache) + at);
+            const uint32_t f = read_factor<kBf16>((is_v ? a.scales.v_scale : a.scales.k_scale)[scale_at(b, sh.page[r], sh.in_page[r], hk)]);
+            decode4<kBf16>(codes.x, f, out.x, out.y);
+            decode4<kBf16>(codes.y, f, out.z, out.w);
+        } else {
+            out = *reinterpret_cast<const uint4 *>(cache + at);
+        }
+        *reinterpret_cast<uint4 *>(to.data + (int64_t)(row0 + r) * to.row_stride + hk * to.head_stride + 8 * c) = out;
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_cache_read(const wino_heads *k, const wino_heads *v, const wino_kv_batch &b, const wino_kv_scales *scales,
+                              StatusWords *status, cudaStream_t stream)
+{
+    ReadArgs a{};
+    if (k)
+        a.k = *k;
+    if (v)
+        a.v = *v;
+    a.b = b;
+    if (scales)
+        a.scales = *scales;
+    a.status = status;
+    a.rows_per_cta = rope_rows_per_cta(b.n_rows);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (!scales)
+        return cudaLaunchKernelEx(&cfg, cache_read_kernel<false, true>, a);
+    return (b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16 ? cudaLaunchKernelEx(&cfg, cache_read_kernel<true, true>, a)
+                                                     : cudaLaunchKernelEx(&cfg, cache_read_kernel<true, false>, a);
+}
+
+}  // namespace wino

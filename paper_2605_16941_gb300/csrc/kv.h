@@ -23,6 +23,20 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
                                const wino_kv_batch &b, const wino_rope &rope, StatusWords *status,
                                cudaStream_t stream);
 
+// wino_norm_rope_append: as above with norms, axes and an 8-bit cache, each of which may be NULL (norm_rope.cu).
+cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
+                                    const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes,
+                                    const wino_head_norm *norm, const wino_kv_scales *scales, StatusWords *status,
+                                    cudaStream_t stream);
+
+// wino_cache_read (cache_read.cu).
+cudaError_t launch_cache_read(const wino_heads *k, const wino_heads *v, const wino_kv_batch &b, const wino_kv_scales *scales,
+                              StatusWords *status, cudaStream_t stream);
+
+// wino_attend_scaled (attend_scaled.cu).
+int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b,
+                         const wino_kv_scales &scales, StatusWords *status, cudaStream_t stream);
+
 // wino_attend (attend.cu): the bytes behind the status words that its kernel uses, the most work units that a batch may
 // have (below 2^62), and its launch.
 size_t attend_scratch_bytes(const wino_kv_batch &b);

@@ -1,11 +1,6 @@
 // rope.cu -- wino_rope_append: the new rows' queries and keys rotated, keys and values written into the cache's pages.
 //
 // Pair (a, b) of a head at position x, turned by t = x f:  a' = m (a cos t - b sin t),  b' = m (b cos t + a sin t).
-// Angles: t / 2 pi modulo 1 is what matters, and x f in 32 bits loses it for far positions (x = 10^6, f = 1: 0.06
-// radians).  f / 2 pi is taken to a 64-bit fixed-point fraction of a turn once per CTA and pair; its product with the
-// position, modulo 2^64, is then the fraction of the turn to 2^-63 |x|, by integer arithmetic.  The quotient is formed in two
-// doubles, since one alone is off by 2^-54 of itself or more, which positions from 2^24 and frequencies above 1 make visible.
-//
 // Bound by HBM: every element is read and written once, 16 bytes at a time (8 where head_dim or rot_dim is no multiple of
 // 16).  A thread has one row and two such chunks of a head that hold 8 (4) whole pairs, keeps their cosines and sines in
 // registers, and walks the heads with the loads of two of them in flight.  Measured (us): 2048 rows of 32 + 2 x 32 heads of
@@ -16,18 +11,13 @@
 // where 40 take 74.  A CTA looks for its rows among all sequences: 16384 sequences of one row 97.
 #include <algorithm>
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "kv_batch.cuh"
 #include "ptx.cuh"
+#include "rope_rows.cuh"
 
 namespace wino {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMaxRowsPerCta = 8;
-constexpr int kMaxPairs = 64;  // head_dim / 2
+constexpr int kThreads = kRopeThreads;
 constexpr int kAhead = 2;  // heads of which a thread has loads in flight
 
 struct RopeArgs {
@@ -37,115 +27,6 @@ struct RopeArgs {
     StatusWords *status;
     int32_t rows_per_cta;
 };
-
-template <typename T>
-__device__ __forceinline__ float to_f(uint16_t x);
-template <>
-__device__ __forceinline__ float to_f<__nv_bfloat16>(uint16_t x)
-{
-    return __uint_as_float((uint32_t)x << 16);
-}
-template <>
-__device__ __forceinline__ float to_f<__half>(uint16_t x)
-{
-    return __half2float(__ushort_as_half(x));
-}
-template <typename T>
-__device__ __forceinline__ uint16_t from_f(float x);
-template <>
-__device__ __forceinline__ uint16_t from_f<__nv_bfloat16>(float x)
-{
-    return __bfloat16_as_ushort(__float2bfloat16_rn(x));
-}
-template <>
-__device__ __forceinline__ uint16_t from_f<__half>(float x)
-{
-    return __half_as_ushort(__float2half_rn(x));
-}
-
-// The fraction of a turn per position, in units of 2^-64, off by one at most for |radians| < 2^42: the product with 1 / (2 pi) as a
-// sum of two doubles, hi + lo, its remainder by fma.
-__device__ __forceinline__ uint64_t turn_fraction(double radians)
-{
-    constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;  // 1 / (2 pi) = kHigh + kLow to 2^-110
-    const double hi = radians * kHigh;
-    const double lo = fma(radians, kLow, fma(radians, kHigh, -hi));
-    const int64_t turns = __double2ll_rn((hi - rint(hi)) * 18446744073709551616.0);  // the difference is exact
-    return (uint64_t)turns + (uint64_t)__double2ll_rn(lo * 18446744073709551616.0);
-}
-
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    return (uint32_t)from_f<T>(lo) | (uint32_t)from_f<T>(hi) << 16;
-}
-
-// a' and b' of one pair.
-__device__ __forceinline__ float2 turn(float a, float b, float2 c)
-{
-    return make_float2(a * c.x - b * c.y, b * c.x + a * c.y);
-}
-
-// What a CTA knows of its rows.
-struct Rows {
-    float2 cs[kMaxRowsPerCta][kMaxPairs];
-    uint64_t turns[kMaxPairs];
-    SeqRows q[kMaxRowsPerCta];
-    int32_t seq[kMaxRowsPerCta];   // -1: a row of no sequence
-    int32_t page[kMaxRowsPerCta];  // -1: not stored
-    int32_t in_page[kMaxRowsPerCta], pos[kMaxRowsPerCta];
-};
-
-__device__ __forceinline__ void find_rows(const RopeArgs &a, Rows &sh, int32_t row0, int32_t n_rows)
-{
-    const wino_kv_batch &b = a.b;
-    const int tid = (int)threadIdx.x, n_pairs = a.rope.rot_dim >> 1;
-    if (tid < kMaxRowsPerCta)
-        sh.seq[tid] = -1;
-    __syncthreads();
-    bool ok = true;
-    for (int32_t s = tid; s < b.n_seq; s += kThreads) {
-        const SeqRows q = load_seq(b, s);
-        ok = ok && q.ok;
-        const int32_t r1 = min(n_rows, q.start + q.n - row0);
-        if (q.n > 0)
-            for (int32_t r = max(0, q.start - row0); r < r1; ++r) {
-                sh.seq[r] = s;
-                sh.q[r] = q;
-            }
-    }
-    for (int j = tid; j < n_pairs; j += kThreads)
-        sh.turns[j] = turn_fraction(a.rope.freq[j]);
-    __syncthreads();
-    if (tid < n_rows && sh.seq[tid] >= 0) {
-        const SeqRows q = sh.q[tid];
-        const int32_t i = row0 + tid - q.start, slot = row_slot(b, q, i), cap = b.table_width * b.page_size;
-        int32_t page = -1;
-        if (a.k.data && slot >= 0) {
-            if (slot < cap)
-                page = load_page(b, sh.seq[tid], slot / b.page_size, ok);
-            else
-                ok = false;
-        }
-        sh.page[tid] = page;
-        sh.in_page[tid] = page >= 0 ? slot % b.page_size : 0;
-        sh.pos[tid] = a.rope.positions ? a.rope.positions[row0 + tid]
-                                       : q.base + (b.mask == WINO_MASK_SHADOW && i >= (q.n >> 1) ? i - (q.n >> 1) : i);
-    }
-    if (!ok)
-        atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
-    __syncthreads();
-    for (int x = tid; x < n_rows * n_pairs; x += kThreads) {
-        const int r = x / n_pairs, j = x - r * n_pairs;
-        if (sh.seq[r] < 0)
-            continue;
-        const uint64_t t = sh.turns[j] * (uint64_t)(int64_t)sh.pos[r];
-        float sn, cn;
-        sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &sn, &cn);  // half-turns in [-1, 1)
-        sh.cs[r][j] = make_float2(cn * a.rope.factor, sn * a.rope.factor);
-    }
-    __syncthreads();
-}
 
 // Chunks of kWords 32-bit words; head_dim and rot_dim multiples of two chunks: two chunks of a head per thread and turn, which
 // hold whole pairs, or plain dims.
@@ -163,13 +44,13 @@ struct Chunk<2> {
 template <typename T, int kWords>
 __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs a)
 {
-    __shared__ Rows sh;
+    __shared__ Rows<1> sh;
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
     ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();
-    find_rows(a, sh, row0, n_rows);
+    find_rows(a.b, a.rope, nullptr, a.k.data != nullptr, a.status, sh, row0, n_rows);
     using V = typename Chunk<kWords>::type;
     constexpr int kDims = 4 * kWords;  // of two chunks
     const int items = b.head_dim / kDims, turned = a.rope.rot_dim / kDims;  // of a head
@@ -240,13 +121,13 @@ __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_append_any_kernel(const RopeArgs a)
 {
-    __shared__ Rows sh;
+    __shared__ Rows<1> sh;
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
     ptx::grid_dep_launch_dependents();
     ptx::grid_dep_wait();
-    find_rows(a, sh, row0, n_rows);
+    find_rows(a.b, a.rope, nullptr, a.k.data != nullptr, a.status, sh, row0, n_rows);
     const int n_pairs = a.rope.rot_dim >> 1, nq = a.q.data ? b.n_q_heads : 0;
     const int heads = nq + (a.k.data ? 2 * b.n_kv_heads : 0);
     const int units = b.head_dim - n_pairs;  // pairs, then the plain dims
@@ -305,11 +186,7 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
     a.b = b;
     a.rope = rope;
     a.status = status;
-    // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads
-    // (replayed, 32 + 2 x 32 heads of 128: 1 against 2 rows: 600 rows 7.0 and 7.7 us, 900 10.6 and 9.2; 2 against 4: 900 9.2 and 11.6,
-    // 1200 9.7 and 11.0, 2048 19.1 and 16.5; 4 against 8: 2048 16.5 and 23.1, 4096 33.6 and 32.0, 9000 73.1 and 71.8; and 20027 rows of
-    // 32 + 2 x 8 heads 90.5 and 83.6).
-    a.rows_per_cta = b.n_rows >= 8192 ? 8 : (b.n_rows >= 1024 ? 4 : (b.n_rows >= 512 ? 2 : 1));
+    a.rows_per_cta = rope_rows_per_cta(b.n_rows);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
     cfg.blockDim = dim3(kThreads);
