@@ -60,9 +60,10 @@ template <bool kBf16>
 __device__ __forceinline__ void decode4(uint32_t codes, uint32_t factor, uint32_t &lo, uint32_t &hi)
 {
     if (kBf16) {
-        // s eeee mmm into the places of a bf16's sign, low exponent bits and high mantissa bits
-        const uint32_t a = __byte_perm(codes, 0u, 0x1404), b = __byte_perm(codes, 0u, 0x3424);
-        const uint32_t x = (a >> 4 & 0x07f007f0u) | (a & 0x80008000u), y = (b >> 4 & 0x07f007f0u) | (b & 0x80008000u);
+        // s eeee mmm into the places of a bf16's sign, low exponent bits and high mantissa bits: 16 times the byte, and the sign
+        // bit 2^11 moved on to 2^15
+        const uint32_t a = __byte_perm(codes, 0u, 0x4140), b = __byte_perm(codes, 0u, 0x4342);
+        const uint32_t x = a * 16u + (a & 0x00800080u) * 240u, y = b * 16u + (b & 0x00800080u) * 240u;
         asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(x), "r"(factor));
         asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(hi) : "r"(y), "r"(factor));
     } else {

@@ -35,7 +35,7 @@ cudaError_t launch_cache_read(const wino_heads *k, const wino_heads *v, const wi
 
 // wino_attend_scaled (attend_scaled.cu).
 int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b,
-                         const wino_kv_scales &scales, StatusWords *status, cudaStream_t stream);
+                         const wino_kv_scales &scales, uint8_t *scratch, StatusWords *status, int sm_count, cudaStream_t stream);
 
 // wino_attend (attend.cu): the bytes behind the status words that its kernel uses, the most work units that a batch may
 // have (below 2^62), and its launch.

@@ -251,7 +251,8 @@ int wino_attend_scaled(const wino_heads *q, const wino_heads *out, float scale, 
     DeviceInfo info;
     if ((rc = device_info(&info)) != WINO_OK)
         return rc;
-    return launch_attend_scaled(*q, *out, scale, *b, *scales, static_cast<StatusWords *>(ws), static_cast<cudaStream_t>(stream));
+    return launch_attend_scaled(*q, *out, scale, *b, *scales, static_cast<uint8_t *>(ws) + kStatusBytes,
+                                static_cast<StatusWords *>(ws), info.sm_count, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

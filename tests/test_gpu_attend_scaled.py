@@ -188,3 +188,18 @@ def test_an_append_error_reaches_the_attention():
     assert wino.wino_read_device_status(ws) == wino.WINO_ERR_ARG
     attend8(c, ws=ws)
     assert wino.wino_read_device_status(ws) == wino.WINO_OK
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("name", ["one_token", "empty_and_absent", "tile_edges_128", "shadow_32", "shadow_large", "shadow_large_128", "causal_prompt",
+                                  "causal_ragged_128", "group_5_dim_80", "dim_32", "long", "long_rows", "long_rows_64"])
+def test_bit_for_bit_the_attention_over_the_values(name, dtype):
+    """Codes become tiles of the element type without rounding, and everything behind them is the same."""
+    mask, seqs, kw = CASES[name]
+    c = add_rows(make_kv8(mask, seqs, dtype=dtype, poison=False, **kw))
+    attend8(c)
+    first = c.out.clone()
+    c.out.fill_(77.0)
+    plain = wino.make_kv_batch(c.k_cache, c.v_cache, c.table_dev, *c.ints, n_rows=c.n_rows, n_q_heads=c.heads, mask=mask)
+    wino.wino_attend(c.q, c.out, plain, wino.attend_workspace(plain))
+    assert torch.equal(c.out, first)
