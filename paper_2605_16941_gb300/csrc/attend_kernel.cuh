@@ -67,9 +67,9 @@ namespace attend {
 
 constexpr int kTileM = 128, kTileN = 128;  // rows and slots of a tile
 constexpr int kSoftmaxThreads = 256;
-constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11, kWarpDecode = 12;  // the last: the first of eight
+constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11, kWarpDecode = 12;  // the last: the first of four
 template <bool kScaled>
-constexpr int kAttendThreads = kSoftmaxThreads + (kScaled ? 384 : 128);
+constexpr int kAttendThreads = kSoftmaxThreads + (kScaled ? 256 : 128);
 constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kLevels = 8;              // of the tree over the parts of a task: 2^8 >= kMaxCtas
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
     if (threadIdx.x == 0) {
         for (int s = 0; s < kParts; ++s) {
             ptx::mbar_init(part_full(s), 1);
-            ptx::mbar_init(part_empty(s), kScaled ? 19 : 11);  // 8 softmax warps, 2 for the copies, MMAs, 8 for codes
+            ptx::mbar_init(part_empty(s), kScaled ? 15 : 11);  // 8 softmax warps, 2 for the copies, MMAs, 4 for codes
         }
         ptx::mbar_init(q_full, 1);
         ptx::mbar_init(q_empty, 1);
@@ -685,11 +685,11 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
         ptx::mbar_arrive(part_empty(reader.slot()));
     };
 
-    // A softmax thread holds its row of S: the launch's 384 x 168 registers are split 208 / 88, its 640 x 96 with codes
-    // 168 / 48 / 48.
+    // A softmax thread holds its row of S: the launch's 384 x 168 registers are split 208 / 88, its 512 x 128 with codes
+    // 184 / 72 / 72.
     if (warp < 8) {
         // ------------------------------------------------------------ softmax: one thread per row
-        ptx::regs_inc<kScaled ? 168 : 208>();
+        ptx::regs_inc<kScaled ? 184 : 208>();
         const int g = warp >> 2;               // warpgroup
         const int r = (warp & 3) * 32 + lane;  // row of the tile, its TMEM lane
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -984,7 +984,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
             }
         }
     } else if (!kScaled || warp < kWarpDecode) {
-        ptx::regs_dec<kScaled ? 48 : 88>();
+        ptx::regs_dec<kScaled ? 72 : 88>();
         if (warp == kWarpPlan) {
             if (a.wide)
                 plan<uint64_t>(a, sh, lane);
@@ -1287,55 +1287,54 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
         }
     }
     if (kScaled && warp >= kWarpDecode) {
-        // ------------------------------------------------------------ codes to values: four warps for K, four for V
-        ptx::regs_dec<48>();
+        // ------------------------------------------------------------ codes to values
+        ptx::regs_dec<72>();
         constexpr int kChunks = DP / 16, kAtOnce = 32 / kChunks;  // chunks of 16 codes per slot, slots per turn of a warp
         constexpr int kTurns = 16 / kAtOnce;                      // a warp's 16 slots of a stage
-        const bool is_v = warp >= kWarpDecode + 4;
         const int of_warp = (warp & 3) * 16 + lane / kChunks, chunk = lane % kChunks;
         const bool swap = chunk >= 4;  // which 8 of 16 values are written first: no two of 8 lanes meet in a bank
-        const int stage0 = is_v ? C::kStages : 0;
-        int stage = 0;           // the next of K's or V's, and its phase
-        uint32_t stage_phase = 0;
-        uint32_t tiles = 0;      // ring slots that earlier parts have taken
+        int tile = 0, stage_k = 0, stage_v = 0;  // the next of each ring, and their phases
+        uint32_t phase = 0, phase_k = 0, phase_v = 0;
         while (__all_sync(0xffffffffu, next_part())) {
             const Part &part = sh.parts[reader.slot()];
             // Tiles in the order in which the MMAs take them: the first scores' K, then K and V in turn, then the last V.
-            const int32_t n = part.n, lead = min(n, (part.flags & kTwo) != 0 ? 1 : 2), pairs = n - lead;
-            int32_t left = part.kv_end - part.j0 * kTileN;  // slots from the current stage's first on
+            const int32_t n = part.n, lead = min(n, (part.flags & kTwo) != 0 ? 1 : 2);
+            const int32_t slots = part.kv_end - part.j0 * kTileN;  // from the part's first on
             __syncwarp();
             if (lane == 0)
                 done_with();
             ++reader.count;
             bool good = true;
-            for (int32_t t = 0; good && t < n; ++t) {
-                const int32_t order = is_v ? (t < pairs ? lead + 2 * t + (C::kEarly ? 1 : 0) : n + t)
-                                           : (t < lead ? t : lead + 2 * (t - lead) + (C::kEarly ? 0 : 1));
-                const uint32_t place = tiles + (uint32_t)order;
-                const int tile = (int)(place % C::kSlots);
-                if (!(good = warp_wait(empty(tile), (place / C::kSlots & 1u) ^ 1u, &sh.abort)))
+            int32_t next_k = 0, next_v = 0;
+            while (good && next_v < n) {
+                const bool is_v = next_k == n || (C::kEarly ? next_k - next_v > lead : next_k - next_v >= lead);
+                int32_t left = slots - (is_v ? next_v : next_k) * kTileN;
+                ++(is_v ? next_v : next_k);
+                if (!(good = warp_wait(empty(tile), phase ^ 1u, &sh.abort)))
                     break;
                 // A tile as TMA would write it: swizzled blocks of 64 dims, in which 16 bytes of row r lie at the place of
                 // their number xor r % 8.
                 uint8_t *const to = smem_raw + (slot_addr(tile) - raw) + (chunk >> 2) * kHalfBytes;
+#pragma unroll 1
                 for (int half = 0; half < 2; ++half, left -= kStageN) {
                     uint4 c[kTurns];
                     uint32_t f[kTurns];
+                    int used = -1;
                     if (left > 0) {
-                        if (!(good = warp_wait(stage_full(stage0 + stage), stage_phase, &sh.abort)))
+                        const int stage = is_v ? C::kStages + stage_v : stage_k;
+                        if (!(good = warp_wait(stage_full(stage), is_v ? phase_v : phase_k, &sh.abort)))
                             break;
-                        const uint8_t *const codes = smem_raw + kStage0 + (uint32_t)(stage0 + stage) * C::kStageBytes;
+                        const uint8_t *const codes = smem_raw + kStage0 + (uint32_t)stage * C::kStageBytes;
 #pragma unroll
                         for (int k = 0; k < kTurns; ++k) {
                             c[k] = *reinterpret_cast<const uint4 *>(codes + (of_warp + k * kAtOnce) * DP + chunk * 16);
-                            f[k] = sh.scale[stage0 + stage][of_warp + k * kAtOnce];
+                            f[k] = sh.scale[stage][of_warp + k * kAtOnce];
                         }
-                        __syncwarp();
-                        if (lane == 0)
-                            ptx::mbar_arrive(stage_free(stage0 + stage));
-                        if (++stage == C::kStages) {
-                            stage = 0;
-                            stage_phase ^= 1u;
+                        used = stage;
+                        int &s = is_v ? stage_v : stage_k;
+                        if (++s == C::kStages) {
+                            s = 0;
+                            (is_v ? phase_v : phase_k) ^= 1u;
                         }
                     }
                     if (left < kStageN) {  // behind the last slot: zeros, which V needs
@@ -1359,6 +1358,11 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at ^ 1 : at) * 16) = swap ? hi : lo;
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at : at ^ 1) * 16) = swap ? lo : hi;
                     }
+                    // Given back once its values have been used, not once they have been asked for: a copy was seen to overtake
+                    // reads that were still on their way.
+                    __syncwarp();
+                    if (lane == 0 && used >= 0)
+                        ptx::mbar_arrive(stage_free(used));
                 }
                 if (!good)
                     break;
@@ -1366,10 +1370,13 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 __syncwarp();
                 if (lane == 0)
                     ptx::mbar_arrive(full(tile));
+                if (++tile == C::kSlots) {
+                    tile = 0;
+                    phase ^= 1u;
+                }
             }
             if (!good)
                 break;
-            tiles += 2u * (uint32_t)n;
         }
     }
     if (!ok)

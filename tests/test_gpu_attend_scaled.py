@@ -203,3 +203,17 @@ def test_bit_for_bit_the_attention_over_the_values(name, dtype):
     plain = wino.make_kv_batch(c.k_cache, c.v_cache, c.table_dev, *c.ints, n_rows=c.n_rows, n_q_heads=c.heads, mask=mask)
     wino.wino_attend(c.q, c.out, plain, wino.attend_workspace(plain))
     assert torch.equal(c.out, first)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_every_call_gives_the_same(dim, dtype):
+    """A thousand calls behind one another: codes that a copy overwrites while they are read would show."""
+    c = add_rows(make_kv8(CAUSAL, [(700, 2100, 1400), (1, 1500, 1499), (300, 300, 0)], heads=8, kv_heads=2, dim=dim, page=32, dtype=dtype))
+    ws = attend8(c)
+    first, off = c.out.clone(), torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(1000):
+        c.out.fill_(77.0)
+        attend8(c, ws=ws)
+        off += (c.out != first).sum()
+    assert off.item() == 0 and wino.wino_read_device_status(ws) == wino.WINO_OK
