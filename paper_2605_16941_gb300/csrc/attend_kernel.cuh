@@ -1285,8 +1285,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
             }
             __syncwarp();
         }
-    }
-    if (kScaled && warp >= kWarpDecode) {
+    } else if constexpr (kScaled) {
         // ------------------------------------------------------------ codes to values
         ptx::regs_dec<72>();
         constexpr int kChunks = DP / 16, kAtOnce = 32 / kChunks;  // chunks of 16 codes per slot, slots per turn of a warp
