@@ -791,7 +791,8 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                         }
                         if (grow)
                             m = mx;
-                        far = __any_sync(0xffffffffu, m != -INFINITY && fabsf(m * sl2) >= kFarBits);
+                        // a row that no head uses has whatever lay in shared memory for its query
+                        far = __any_sync(0xffffffffu, valid && m != -INFINITY && fabsf(m * sl2) >= kFarBits);
                     }
                     // Where some row's m sl2 is far from zero its rounding would show in P, all of it from 2^24 on: the differences
                     // are formed first there, which are exact near the maximum.
