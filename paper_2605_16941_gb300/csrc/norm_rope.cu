@@ -24,17 +24,20 @@ struct NormRopeArgs {
     wino_kv_scales scales;
     StatusWords *status;
     int32_t rows_per_cta;
+    int32_t lanes;  // per head: the smallest power of two that is no less than head_dim / 16
 };
 
-// The values x[0 .. n) of a head that `lanes` neighbouring lanes hold (others zero) become x / sqrt(mean(x^2) + eps).
+// 1 / sqrt(mean(x^2) + eps) of a head whose values `lanes` neighbouring lanes hold (others zero), by all lanes of the warp; x is
+// scaled by 2^-100 first, here and in the result, where its squares come too close to fp32's limits.
 template <int kN>
-__device__ __forceinline__ void normalise(float (&x)[kN], int lanes, float dim, float eps)
+__device__ __forceinline__ float inverse_rms(float2 (&x)[kN], int lanes, float inv_dim, float eps)
 {
     auto squares = [&]() {
-        float s = 0.f;
+        float2 p = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < kN; ++k)
-            s = fmaf(x[k], x[k], s);
+            p = ptx::fma2(x[k], x[k], p);
+        float s = p.x + p.y;
         for (int i = lanes >> 1; i; i >>= 1)
             s += __shfl_xor_sync(0xffffffffu, s, i);
         return s;
@@ -45,7 +48,7 @@ __device__ __forceinline__ void normalise(float (&x)[kN], int lanes, float dim, 
         if (large) {
 #pragma unroll
             for (int k = 0; k < kN; ++k)
-                x[k] *= 0x1p-100f;
+                x[k] = make_float2(x[k].x * 0x1p-100f, x[k].y * 0x1p-100f);
         }
         const float again = squares();
         if (large) {
@@ -53,10 +56,173 @@ __device__ __forceinline__ void normalise(float (&x)[kN], int lanes, float dim, 
             eps = 0.f;  // times 2^-200
         }
     }
-    const float r = rsqrtf(s / dim + eps);
+    return rsqrtf(s * inv_dim + eps);
+}
+
+enum class Kind { kQ, kK, kV };
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
+{
+    uint32_t r;
+    if (__is_same(T, __nv_bfloat16))
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Head dims and rotations that are multiples of 16: a thread has two chunks of 8 dims of a head that hold whole pairs, and
+// the smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A warp
+// has one row and a unit of neighbouring heads of one kind at a time, so that it never branches apart.
+template <typename T, bool kScaled, int kAxes>
+__global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_constant__ NormRopeArgs a)
+{
+    constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+    __shared__ Rows<kAxes> sh;
+    const wino_kv_batch &b = a.b;
+    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
+    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
+    __shared__ __align__(16) float shared_weight[2][128];  // offset + weight where all heads share it; zeros behind the last dim
+    ptx::grid_dep_launch_dependents();
+    ptx::grid_dep_wait();
+    {
+        const int k = (int)threadIdx.x >> 7, c = (int)threadIdx.x & 127;
+        const uint16_t *const w = k ? a.norm.k_weight : a.norm.q_weight;
+        shared_weight[k][c] = w && c < b.head_dim ? a.norm.offset + to_f<T>(w[c]) : 0.f;
+    }
+    find_rows(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows);
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int r = warp % a.rows_per_cta;
+    if (r >= n_rows || sh.seq[r] < 0)
+        return;
+    const int turned = a.rope.rot_dim / 16, lanes = a.lanes, j = lane & (lanes - 1), of_unit = 32 / lanes, sub = lane / lanes;
+    const bool live = j < b.head_dim / 16, turns = j < turned;
+    // the item's chunks: halves j and j + turned, or neighbours
+    const int c0 = turns && !a.rope.interleaved ? j : 2 * j, c1 = turns && !a.rope.interleaved ? j + turned : 2 * j + 1;
+    float2 cs[8];
 #pragma unroll
-    for (int k = 0; k < kN; ++k)
-        x[k] *= r;
+    for (int k = 0; k < 8; ++k)
+        cs[k] = turns ? sh.cs[r][8 * j + k] : make_float2(1.f, 0.f);
+    const float inv_dim = 1.f / (float)b.head_dim;
+    const int64_t row = row0 + r, slot = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride;
+    auto unpack = [&](const uint4 &v, float2 *to) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            to[k] = make_float2(to_f<T>((uint16_t)w[k]), to_f<T>((uint16_t)(w[k] >> 16)));
+    };
+    auto unit = [&](auto kind, int head, int heads, uint4 x, uint4 y) {
+        constexpr bool kQ = decltype(kind)::value == Kind::kQ, kV = decltype(kind)::value == Kind::kV;
+        const bool mine = live && head < heads;
+        float2 z[8];  // the first chunk's pairs of neighbours, then the second's
+        unpack(x, z);
+        unpack(y, z + 4);
+        const uint16_t *const weight = kQ ? a.norm.q_weight : a.norm.k_weight;
+        if (!kV && weight) {
+            const float by = inverse_rms(z, lanes, inv_dim, a.norm.eps);
+            const int64_t stride = kQ ? a.norm.q_head_stride : a.norm.k_head_stride;
+            float2 w[8];
+            if (stride == 0) {
+                const float4 *const f = reinterpret_cast<const float4 *>(shared_weight[kQ ? 0 : 1]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float4 p = f[2 * c0 + k], q = f[2 * c1 + k];
+                    w[2 * k] = make_float2(p.x, p.y);
+                    w[2 * k + 1] = make_float2(p.z, p.w);
+                    w[4 + 2 * k] = make_float2(q.x, q.y);
+                    w[4 + 2 * k + 1] = make_float2(q.z, q.w);
+                }
+            } else {
+                const uint4 *const p = reinterpret_cast<const uint4 *>(weight + min(head, heads - 1) * stride);
+                unpack(p[live ? c0 : 0], w);
+                unpack(p[live ? c1 : 0], w + 4);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    w[k] = ptx::add2(w[k], make_float2(a.norm.offset, a.norm.offset));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                z[k] = ptx::mul2(ptx::mul2(z[k], make_float2(by, by)), w[k]);
+        }
+        if (!kV && turns) {
+            if (a.rope.interleaved) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    z[k] = turn(z[k].x, z[k].y, cs[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 p = turn(z[k].x, z[4 + k].x, cs[2 * k]), q = turn(z[k].y, z[4 + k].y, cs[2 * k + 1]);
+                    z[k] = make_float2(p.x, q.x);
+                    z[4 + k] = make_float2(p.y, q.y);
+                }
+            }
+        }
+        if (kQ || !kScaled) {
+            uint16_t *const dst = kQ ? a.q_out.data + row * a.q_out.row_stride + head * a.q_out.head_stride
+                                     : (kV ? b.v_cache : b.k_cache) + slot + head * b.head_stride;
+            auto pack = [&](const float2 *v) {
+                return make_uint4(pack_pair<T>(v[0].x, v[0].y), pack_pair<T>(v[1].x, v[1].y), pack_pair<T>(v[2].x, v[2].y),
+                                  pack_pair<T>(v[3].x, v[3].y));
+            };
+            if (mine) {
+                reinterpret_cast<uint4 *>(dst)[c0] = pack(z);
+                reinterpret_cast<uint4 *>(dst)[c1] = pack(z + 4);
+            }
+        } else {
+            uint32_t most = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                most = max(most, max(__float_as_uint(z[k].x) & 0x7fffffffu, __float_as_uint(z[k].y) & 0x7fffffffu));
+            for (int i = lanes >> 1; i; i >>= 1)
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, i));
+            const uint32_t s = scale_byte<kBf16>(most);
+            const float f = code_factor(s);
+            auto codes = [&](const float2 *v) {
+                if (s == kScaleNan)
+                    return make_uint2(0, 0);
+                return make_uint2(codes2(v[0].x * f, v[0].y * f) | codes2(v[1].x * f, v[1].y * f) << 16,
+                                  codes2(v[2].x * f, v[2].y * f) | codes2(v[3].x * f, v[3].y * f) << 16);
+            };
+            if (mine) {
+                uint2 *const dst = reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(kV ? b.v_cache : b.k_cache) + slot +
+                                                             head * b.head_stride);
+                dst[c0] = codes(z);
+                dst[c1] = codes(z + 4);
+                if (j == 0)
+                    (kV ? a.scales.v_scale : a.scales.k_scale)[scale_at(b, sh.page[r], sh.in_page[r], head)] = (uint8_t)s;
+            }
+        }
+    };
+    const int nq = a.q.data ? b.n_q_heads : 0, nk = a.k.data && sh.page[r] >= 0 ? b.n_kv_heads : 0;
+    const int q_units = (nq + of_unit - 1) / of_unit, k_units = (nk + of_unit - 1) / of_unit;
+    const int units = q_units + 2 * k_units, step = kWarps / a.rows_per_cta;
+    auto fetch = [&](int u, uint4 &x, uint4 &y) {
+        x = y = make_uint4(0, 0, 0, 0);
+        if (u >= units)
+            return;
+        const bool is_q = u < q_units, is_v = u >= q_units + k_units;
+        const wino_heads &from = is_q ? a.q : (is_v ? a.v : a.k);
+        const int head = (is_q ? u : (is_v ? u - q_units - k_units : u - q_units)) * of_unit + sub;
+        if (live && head < (is_q ? nq : nk)) {
+            const uint4 *const p = reinterpret_cast<const uint4 *>(from.data + row * from.row_stride + head * from.head_stride);
+            x = p[c0];
+            y = p[c1];
+        }
+    };
+    uint4 nx, ny;
+    fetch(warp / a.rows_per_cta, nx, ny);
+    for (int u = warp / a.rows_per_cta; u < units; u += step) {
+        const uint4 x = nx, y = ny;
+        fetch(u + step, nx, ny);
+        if (u < q_units)
+            unit(std::integral_constant<Kind, Kind::kQ>(), u * of_unit + sub, nq, x, y);
+        else if (u < q_units + k_units)
+            unit(std::integral_constant<Kind, Kind::kK>(), (u - q_units) * of_unit + sub, nk, x, y);
+        else
+            unit(std::integral_constant<Kind, Kind::kV>(), (u - q_units - k_units) * of_unit + sub, nk, x, y);
+    }
 }
 
 // Any dims: a warp per head, whose lane l has the dims l, l + 32, l + 64 and l + 96.
@@ -83,18 +249,17 @@ __global__ void __launch_bounds__(kThreads) norm_append_any_kernel(const __grid_
         const int hk = is_q ? h : (is_v ? h - nq - b.n_kv_heads : h - nq);
         const wino_heads &from = is_q ? a.q : (is_v ? a.v : a.k);
         const uint16_t *const src = from.data + (int64_t)(row0 + r) * from.row_stride + hk * from.head_stride;
-        float x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            x[k] = lane + 32 * k < D ? to_f<T>(src[lane + 32 * k]) : 0.f;
+        auto dim = [&](int k) { return lane + 32 * k < D ? to_f<T>(src[lane + 32 * k]) : 0.f; };
+        float2 pairs[2] = {make_float2(dim(0), dim(1)), make_float2(dim(2), dim(3))};
         const uint16_t *const weight = is_q ? a.norm.q_weight : a.norm.k_weight;
+        const float by = !is_v && weight ? inverse_rms(pairs, 32, 1.f / (float)D, a.norm.eps) : 1.f;
+        float x[4] = {pairs[0].x, pairs[0].y, pairs[1].x, pairs[1].y};
         if (!is_v && weight) {
-            normalise(x, 32, (float)D, a.norm.eps);
             const uint16_t *const w = weight + hk * (is_q ? a.norm.q_head_stride : a.norm.k_head_stride);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (lane + 32 * k < D)
-                    x[k] *= a.norm.offset + to_f<T>(w[lane + 32 * k]);
+                    x[k] = x[k] * by * (a.norm.offset + to_f<T>(w[lane + 32 * k]));
         }
         if (!is_v && n_pairs) {
 #pragma unroll
@@ -169,6 +334,9 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
         a.scales = *scales;
     a.status = status;
     a.rows_per_cta = rope_rows_per_cta(b.n_rows);
+    a.lanes = 1;
+    while (a.lanes < b.head_dim / 16)
+        a.lanes *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
     cfg.blockDim = dim3(kThreads);
@@ -182,6 +350,8 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
     auto of_type = [&](auto type, auto scaled) {
         using T = decltype(type);
         constexpr bool kScaled = decltype(scaled)::value;
+        if (b.head_dim % 16 == 0 && rope.rot_dim % 16 == 0)
+            return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes>) : launch(norm_append_kernel<T, kScaled, 1>);
         return axes ? launch(norm_append_any_kernel<T, kScaled, kMaxAxes>) : launch(norm_append_any_kernel<T, kScaled, 1>);
     };
     if ((b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16)

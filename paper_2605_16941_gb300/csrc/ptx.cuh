@@ -404,7 +404,7 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Two fp32 operations per instruction, each rounded as the scalar one: a * b + c and a + b.
+// Two fp32 operations per instruction, each rounded as the scalar one: a * b + c, a + b and a * b.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
     union { float2 f; uint64_t u; } x{a}, y{b}, z{c}, d;
@@ -416,6 +416,13 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
     union { float2 f; uint64_t u; } x{a}, y{b}, d;
     asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d.u) : "l"(x.u), "l"(y.u));
+    return d.f;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    union { float2 f; uint64_t u; } x{a}, y{b}, d;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d.u) : "l"(x.u), "l"(y.u));
     return d.f;
 }
 
