@@ -312,8 +312,8 @@ __device__ __forceinline__ U warp_scan(U x, int lane)  // inclusive
     return x;
 }
 
-// The planning warp: cuts the work and hands this CTA's run out part by part.  U is unsigned.
-template <typename U, typename S>
+// The planning warp: cuts the work and hands this CTA's run out part by part.  U is unsigned.  kMostTiles: row tiles of a task.
+template <typename U, typename S, int kMostTiles = 2>
 __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
 {
     const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads;
@@ -325,7 +325,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
     SeqRows q;
     U share = 0, mine = 0;  // units of this lane's tasks, and of its sequence, of one kv head
     int32_t n_tasks = 0;    // and its tasks
-    int32_t row_tiles = 2;  // of a task
+    int32_t row_tiles = kMostTiles;  // of a task
     auto load_round = [&](int32_t s0) {
         const int32_t s = s0 + lane / width;
         q.n = 0;
@@ -348,7 +348,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
         total = tasks = 0;
 #pragma unroll 1
         for (int32_t s0 = 0; s0 < n_seq; s0 += per_round) {
-            if (row_tiles == 2 || n_seq > per_round)
+            if (row_tiles == kMostTiles || n_seq > per_round)
                 load_round(s0);
             count();
             total += warp_total(share);
@@ -592,6 +592,26 @@ __device__ __forceinline__ bool join_parts(const AttendArgs &a, const Part &part
         m = big;
     }
     return true;
+}
+
+// By all threads of a CTA at its end, after its failures are recorded: the last CTA publishes a failure and clears it for
+// the next call, and with it the nodes, which parts that never came may have left.
+__device__ __forceinline__ void publish(const AttendArgs &a, int threads)
+{
+    int32_t failed = 0;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&a.status->finished, 1u) + 1u == gridDim.x) {
+            __threadfence();
+            failed = -abs(atomicExch(&a.status->current, (int32_t)WINO_OK));  // positive: an append's, already read
+            if (failed && a.status->first == WINO_OK)
+                a.status->first = failed;
+            a.status->finished = 0;
+        }
+    }
+    if (__syncthreads_or(failed))
+        for (int x = (int)threadIdx.x; x < kMaxCtas * kLevels * 8; x += threads)
+            a.nodes[x] = 0;
 }
 
 template <int DP, bool kBf16, bool kScaled>
@@ -1388,22 +1408,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
         ptx::tmem_dealloc(tmem, kTmemAll);
     if (threadIdx.x == 0 && sh.abort)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_DEVICE_TIMEOUT);
-    // The last CTA publishes a failure and clears it for the next call, and with it the nodes, which parts that never came
-    // may have left.
-    int32_t failed = 0;
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(&a.status->finished, 1u) + 1u == gridDim.x) {
-            __threadfence();
-            failed = -abs(atomicExch(&a.status->current, (int32_t)WINO_OK));  // positive: an append's, already read
-            if (failed && a.status->first == WINO_OK)
-                a.status->first = failed;
-            a.status->finished = 0;
-        }
-    }
-    if (__syncthreads_or(failed))
-        for (int x = (int)threadIdx.x; x < kMaxCtas * kLevels * 8; x += kAttendThreads<kScaled>)
-            a.nodes[x] = 0;
+    publish(a, kAttendThreads<kScaled>);
 }
 
 template <int DP, bool kBf16, bool kScaled>
@@ -1443,6 +1448,11 @@ int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, 
 // What both calls give the kernel (attend.cu): the arguments but for the cache's layout, and the map of Q.
 int attend_args(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
                 StatusWords *status, AttendArgs *a, CUtensorMap *tq);
+
+// Few rows per sequence over an 8-bit cache (attend_few.cu): whether a batch is of that kind, and its launch with the arguments
+// of attend_args and the scales.
+bool few_rows(const wino_kv_batch &b);
+int launch_few(AttendArgs a, int ctas, cudaStream_t stream);
 
 }  // namespace attend
 }  // namespace wino

@@ -34,13 +34,15 @@ int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale
     if (rc != WINO_OK)
         return rc;
     a.scales = scales;
+    const int ctas = std::min(sm_count, kMaxCtas);
+    if (few_rows(b))
+        return launch_few(a, ctas, stream);
     a.end = b.n_pages;
     a.tile = TileLayout{1024u, kHalfBytes};
     const int32_t width = b.head_dim <= 64 ? 64 : 128, box_rows = std::min(a.box_rows, kStageN);
     if ((rc = encode_codes(&tk, b.k_cache, b, width, box_rows)) != WINO_OK ||
         (rc = encode_codes(&tv, b.v_cache, b, width, box_rows)) != WINO_OK)
         return rc;
-    const int ctas = std::min(sm_count, kMaxCtas);
     const bool bf16 = (b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16;
     if (width == 64)
         return bf16 ? launch<64, true, true>(tq, tk, tv, a, ctas, stream) : launch<64, false, true>(tq, tk, tv, a, ctas, stream);
