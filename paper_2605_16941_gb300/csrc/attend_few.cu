@@ -5,7 +5,7 @@
 // mma.m16n8k16: S^T = K Q^T and O^T = V^T P^T, with K and V as the A operand.  That is bound by the stream of codes: a token's
 // products would fill 8 of the 128 rows that tcgen05 takes, and its operands would have to go through shared memory twice more.
 //
-// A warp takes 32 slots at a time.  S^T: lane 4 g + t reads 16 codes of slots g and g + 8 at a time; which dims meet in a step of 16
+// A warp takes 32 slots at a time, whose codes copies bring to its ring in shared memory, swizzled so that no two of 8 lanes that read
 // does not matter as long as Q's do the same, so the four codes of a word are the four values that a step wants from a
 // lane.  O^T: lane 4 g + t reads 16 neighbouring dims of four slots, and a row of the product is any dim: two of the lane's dims per step,
 // whose codes of two slots are put side by side and converted.  Both ways 64 or 128 neighbouring bytes are read together, and
@@ -26,18 +26,26 @@ namespace {
 
 using namespace attend;
 
-constexpr int kWorkers = 11, kFewThreads = 32 * (kWorkers + 1);  // and the planning warp: 12 warps have 168 registers a thread
+constexpr int kWorkers = 15, kFewThreads = 32 * (kWorkers + 1);  // and the planning warp: 16 warps have 128 registers a thread
 constexpr int kFewRows = 8, kChunk = 32;  // rows of a tile, slots at a time of a warp
 constexpr float kWeightTop = 15.f;        // the largest weight is 2^this
+constexpr int kAlike = 6;                 // V's exponents this near to one another share a reference
+constexpr int kUnits = 3;                 // of a worker's ring: the codes of 32 slots' K, or V
+constexpr uint32_t kUnitBytes = kChunk * 128;
+constexpr uint32_t kWorkerBytes = kUnits * kUnitBytes, kRingBytes = kWorkers * kWorkerBytes;
+constexpr int kRowFloats = 128 + 4;       // of O in shared memory
+static_assert(kFewRows * kRowFloats * sizeof(float) <= kWorkerBytes, "O takes the ring's place at the end of a part");
 
 struct alignas(16) FewShared {
     Part parts[kParts];
     uint64_t part_full[kParts], part_empty[kParts];
+    uint64_t full[kWorkers][kUnits];
     int32_t abort, last;
     float m[kWorkers][kFewRows], c[kWorkers][kFewRows], l[kWorkers][kFewRows], f[kWorkers][kFewRows];  // f: factors of O
     float joined[3][kFewRows];  // m, c, l of all workers
-    alignas(16) float o[kWorkers][kFewRows][128 + 4];
 };
+constexpr uint32_t kFewSmem = kRingBytes + sizeof(FewShared);
+static_assert(kFewSmem <= kSmemLimit, "shared memory");
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -46,12 +54,10 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Two codes of the low or high half of a word as fp16.
-__device__ __forceinline__ uint32_t half2_of(uint32_t word, bool high)
+// Four codes of a word as pairs of fp16.
+__device__ __forceinline__ void halves_of(uint32_t word, uint32_t &lo, uint32_t &hi)
 {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)(high ? word >> 16 : word)));
-    return r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(word));
 }
 
 // An 8 x 8 matrix of 16-bit elements across the warp, turned over.
@@ -84,13 +90,14 @@ __device__ __forceinline__ float max_of_rows(float x)  // over the lanes of one 
 }
 
 template <int DP, typename T>
-__global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid_constant__ AttendArgs a)
+__global__ void __launch_bounds__(kFewThreads, 1)
+    attend_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a)
 {
-    constexpr int kLoadsK = DP / 64;      // 16 codes each, per slot
+    constexpr int kLoadsK = DP / 64;      // chunks of 16 codes that a lane has of a slot's K
     constexpr int kSteps = DP / 16;       // of 16 dims: K's words, and O's tiles
-    constexpr int kWordsV = DP / 32;      // codes of a slot that a lane has of V: DP / 8 dims
-    extern __shared__ __align__(16) uint8_t smem_few[];
-    FewShared &sh = *reinterpret_cast<FewShared *>(smem_few);
+    constexpr int kWordsV = DP / 32;      // words of a slot that a lane has of V: DP / 8 dims
+    extern __shared__ __align__(1024) uint8_t smem_few[];  // swizzle atoms
+    FewShared &sh = *reinterpret_cast<FewShared *>(smem_few + kRingBytes);
     const wino_kv_batch &b = a.b;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -98,8 +105,15 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
             ptx::mbar_init(ptx::smem_u32(&sh.part_full[s]), 1);
             ptx::mbar_init(ptx::smem_u32(&sh.part_empty[s]), kWorkers);
         }
+        for (int w = 0; w < kWorkers; ++w)
+            for (int u = 0; u < kUnits; ++u)
+                ptx::mbar_init(ptx::smem_u32(&sh.full[w][u]), 1);
         sh.abort = 0;
         ptx::fence_barrier_init();
+    }
+    if (warp == kWorkers && lane == 0) {
+        ptx::prefetch_tensormap(&tmK);
+        ptx::prefetch_tensormap(&tmV);
     }
     __syncthreads();
     ptx::grid_dep_launch_dependents();
@@ -114,10 +128,15 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
         const int g = lane >> 2, t4 = lane & 3;
         const float sl2 = a.scale_log2;
         PartReader reader;
+        uint32_t issued = 0, used = 0;  // units of the ring so far
+        bool good = true;
+        uint8_t *const ring = smem_few + warp * kWorkerBytes;
         while (true) {
             // Together: a worker that gave up alone would leave the others at their barriers.  Behind it the part before is out of
             // shared memory.
-            if (worker_any(!warp_wait(ptx::smem_u32(&sh.part_full[reader.slot()]), reader.parity(), &sh.abort)))
+            ptx::fence_proxy_async();  // O's stores to the ring, before the next copies into it
+            good = good && warp_wait(ptx::smem_u32(&sh.part_full[reader.slot()]), reader.parity(), &sh.abort);
+            if (worker_any(!good))
                 break;
             const Part part = sh.parts[reader.slot()];
             __syncwarp();
@@ -145,7 +164,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
                 };
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) {
-                    const int dim = 64 * (s / 4) + 16 * t4 + 4 * (s % 4);
+                    const int dim = kLoadsK * 16 * t4 + 4 * s;  // the lane's codes in their order
                     raw[s] = make_uint2(0, 0);
                     if (valid && dim < b.head_dim)
                         raw[s] = *reinterpret_cast<const uint2 *>(src + dim);
@@ -187,6 +206,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
                 }
             }
             all = __reduce_min_sync(0xffffffffu, all);
+            int e_most = -1000, e_least = 1000;  // of the exponents of V so far
             float o[kSteps][4];
 #pragma unroll
             for (int s = 0; s < kSteps; ++s)
@@ -194,187 +214,264 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
                 for (int k = 0; k < 4; ++k)
                     o[s][k] = 0.f;
 
-            // ---- the part's slots, 32 at a time; pages a turn ahead of the codes, codes a turn ahead of their use
+            // ---- the part's slots, 32 at a time; pages and scales a turn ahead of the codes, codes a turn ahead of their use
             const int32_t end = min(part.kv_end, (part.j0 + part.n) * kTileN);
             const int32_t *const table = b.page_table + (int64_t)part.seq * b.table_width;
             int32_t at = part.j0 * kTileN + warp * kChunk;
-            auto page_of = [&](int32_t slot) { return slot < end ? table[page_entry(a, slot)] : -1; };
-            int32_t pages[2] = {page_of(at), page_of(at + 16)};
-            uint4 k_codes[2][2][kLoadsK];         // [16 slots][slot g or g + 8]
-            uint32_t v_codes[2][4][kWordsV];      // [16 slots][slots 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9]
-            uint32_t k_scale[2][2], v_scale[2][2];  // of slots g and g + 8
-            // The base of 16 slots that lie in one page; null where nothing is read.
-            auto base_of = [&](int32_t slot, int32_t page, int64_t &codes, int64_t &scales) {
-                const int32_t in_page = slot - page_entry(a, slot) * b.page_size;
-                codes = (int64_t)page * b.page_stride + (int64_t)in_page * b.slot_stride + (int64_t)part.kv_head * b.head_stride;
-                scales = scale_at(b, page, in_page, part.kv_head);
-            };
-            auto fetch = [&](int32_t slot, auto is_v) {
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int32_t first = slot + 16 * x, left = end - first, page = pages[x];
-                    const bool there = left > 0 && (uint32_t)page < (uint32_t)b.n_pages;
-                    int64_t codes = 0, scales = 0;
-                    if (there)
-                        base_of(first, page, codes, scales);
-                    const uint8_t *const from = reinterpret_cast<const uint8_t *>(decltype(is_v)::value ? b.v_cache : b.k_cache) + codes;
-                    const uint8_t *const scale = (decltype(is_v)::value ? a.scales.v_scale : a.scales.k_scale) + scales;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        (decltype(is_v)::value ? v_scale : k_scale)[x][k] = there && g + 8 * k < left ? (uint32_t)scale[g + 8 * k] : 0u;
-                    if constexpr (decltype(is_v)::value) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int in = 2 * t4 + (k & 1) + 8 * (k >> 1);
-                            const bool some = there && in < left && g * (DP / 8) < b.head_dim;
-                            const uint8_t *const p = from + (int64_t)in * b.slot_stride + g * (DP / 8);
-                            if constexpr (DP == 128) {
-                                const uint4 w = some ? ptx::ld_stream(p) : make_uint4(0, 0, 0, 0);
-                                v_codes[x][k][0] = w.x;
-                                v_codes[x][k][1] = w.y;
-                                v_codes[x][k][2] = w.z;
-                                v_codes[x][k][3] = w.w;
-                            } else {
-                                const uint2 w = some ? ptx::ld_stream2(p) : make_uint2(0, 0);
-                                v_codes[x][k][0] = w.x;
-                                v_codes[x][k][1] = w.y;
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-#pragma unroll
-                            for (int n = 0; n < kLoadsK; ++n) {
-                                const int dim = 64 * n + 16 * t4;
-                                const bool some = there && g + 8 * k < left && dim < b.head_dim;
-                                k_codes[x][k][n] = some ? ptx::ld_stream(from + (int64_t)(g + 8 * k) * b.slot_stride + dim)
-                                                        : make_uint4(0, 0, 0, 0);
-                            }
-                    }
-                    ok = ok && (left <= 0 || there);
+            constexpr int32_t kStep = kWorkers * kChunk;
+            // of a slot behind the last one: the last one's, which nothing reads
+            auto page_of = [&](int32_t slot) { return table[page_entry(a, min(slot, end - 1))]; };
+            int32_t pages[2] = {-1, -1};
+            // The 32 slots from `slot` on, whose pages are at hand: a lane's box (its page, or n_pages for zeros), and its slot's scales.
+            int32_t box_page = 0, box_slot = 0, box_bytes = 0;
+            auto locate = [&](int32_t slot, uint32_t (&scales)[2]) {
+                const int32_t left = end - slot, boxes = min(kChunk / a.box_rows, (left + a.box_rows - 1) / a.box_rows);
+                const int x = lane >> 4;
+                const int32_t mine = slot + 16 * x, page = x ? pages[1] : pages[0];
+                const bool there = 16 * x < left && (uint32_t)page < (uint32_t)b.n_pages;
+                ok = ok && (16 * x >= left || there);
+                const int32_t in_page = mine - page_entry(a, mine) * b.page_size;
+                // lane 0 has the first box, lane 16 the second
+                box_page = there ? page : a.end;
+                box_slot = in_page;
+                box_bytes = (lane == 0 || (lane == 16 && boxes > 1)) ? a.box_rows * DP : 0;
+                scales[0] = scales[1] = 0;
+                if (there && lane < left) {
+                    const int64_t scale = scale_at(b, page, in_page + (lane & 15), part.kv_head);
+                    scales[0] = a.scales.k_scale[scale];
+                    scales[1] = a.scales.v_scale[scale];
                 }
             };
-            const std::false_type of_k{};
-            const std::true_type of_v{};
+            // K or V of the 32 slots that were located last into the next unit, swizzled by 128 (64) bytes.
+            auto copy = [&](const CUtensorMap *map) {
+                const uint32_t u = issued++ % kUnits, bar = ptx::smem_u32(&sh.full[warp][u]);
+                const uint32_t to = ptx::smem_u32(ring) + u * kUnitBytes;
+                const int32_t second = __shfl_sync(0xffffffffu, box_bytes, 16);
+                if (lane == 0)
+                    ptx::mbar_arrive_expect_tx(bar, (uint32_t)(box_bytes + second));
+                __syncwarp();
+                if (box_bytes)
+                    ptx::tma_load_4d(to + (uint32_t)(lane ? 16 * DP : 0), map, bar, 0, box_slot, part.kv_head, box_page);
+                __syncwarp();
+            };
+            auto next_unit = [&]() -> const uint8_t * {  // waits for it
+                const uint32_t u = used % kUnits;
+                good = warp_wait(ptx::smem_u32(&sh.full[warp][u]), used / kUnits & 1u, &sh.abort) && good;
+                ++used;
+                return ring + u * kUnitBytes;
+            };
+            uint32_t scales_now[2] = {0, 0}, scales_next[2] = {0, 0};  // of slot `lane`: K's and V's
             if (at < end) {
-                fetch(at, of_k);
-                fetch(at, of_v);
+                pages[0] = page_of(at);
+                pages[1] = page_of(at + 16);
+                locate(at, scales_now);
+                copy(&tmK);
+                copy(&tmV);
+                pages[0] = page_of(at + kStep);
+                pages[1] = page_of(at + kStep + 16);
+                if (at + kStep < end) {
+                    locate(at + kStep, scales_next);
+                    copy(&tmK);
+                }
             }
-            for (; at < end; at += kWorkers * kChunk) {
-                const int32_t next = at + kWorkers * kChunk;
-                const int32_t next_pages[2] = {page_of(next), page_of(next + 16)};
-                float s[2][4];  // scores of slots g (0, 1) and g + 8 (2, 3) with rows 2 t4 and 2 t4 + 1
+            for (; good && at < end; at += kStep) {
+                const int32_t next = at + kStep;
+                pages[0] = page_of(next + kStep);  // for the K copied at the end of this turn
+                pages[1] = page_of(next + kStep + 16);
+                const uint32_t k_scale = scales_now[0], v_scale = scales_now[1];
+                const uint8_t *const k_unit = next_unit();
+                float s[2][kLoadsK][4];  // scores of slots g (0, 1) and g + 8 (2, 3) with rows 2 t4 and 2 t4 + 1, in kLoadsK sums
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        s[x][k] = 0.f;
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int n = 0; n < kLoadsK; ++n) {
-                        const uint4 lo = k_codes[x][0][n], hi = k_codes[x][1][n];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            s[x][n][k] = 0.f;
+                        // 16 bytes of a row lie at the place of their number xor the row's (by 8, or by pairs by 4)
+                        const int c = kLoadsK * t4 + n, place = DP == 128 ? c ^ g : c ^ (g >> 1 & 3);
+                        const uint4 lo = *reinterpret_cast<const uint4 *>(k_unit + (16 * x + g) * DP + place * 16);
+                        const uint4 hi = *reinterpret_cast<const uint4 *>(k_unit + (16 * x + g + 8) * DP + place * 16);
                         const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-                        for (int w = 0; w < 4; ++w)
-                            mma_f16(s[x], half2_of(wl[w], false), half2_of(wh[w], false), half2_of(wl[w], true), half2_of(wh[w], true),
-                                    q[4 * n + w][0], q[4 * n + w][1]);
+                        for (int w = 0; w < 4; ++w) {
+                            uint32_t a0, a1, a2, a3;
+                            halves_of(wl[w], a0, a2);
+                            halves_of(wh[w], a1, a3);
+                            mma_f16(s[x][n], a0, a1, a2, a3, q[4 * n + w][0], q[4 * n + w][1]);
+                        }
                     }
+                if constexpr (kLoadsK == 2) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            s[x][0][k] += s[x][1][k];
                 }
-                float nan[2][2];  // NaN where a slot's K is held as that
+                // K's scales as factors.  A slot that is held as NaN counts as a score of 0 over zeros and makes l NaN.
+                const float k_factor = k_scale == kScaleNan ? 0.f : __uint_as_float(k_scale << 23);
+                float2 t[2][2];  // slots g and g + 8, the rows side by side
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const uint32_t e = k_scale[x][k];
-                        nan[x][k] = e == kScaleNan ? NAN : 0.f;
-                        const float f = e == kScaleNan ? 0.f : __uint_as_float(e << 23);
-                        s[x][2 * k] = s[x][2 * k] * f * inv_row[0];
-                        s[x][2 * k + 1] = s[x][2 * k + 1] * f * inv_row[1];
+                        const float f = __shfl_sync(0xffffffffu, k_factor, 16 * x + g + 8 * k);
+                        t[x][k] = ptx::mul2(ptx::mul2(make_float2(s[x][0][2 * k], s[x][0][2 * k + 1]), make_float2(f, f)),
+                                            make_float2(inv_row[0], inv_row[1]));
                     }
-                uint32_t v_exp[2][2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        v_exp[x][k] = v_scale[x][k];
+                __syncwarp();
+                if (good && next < end)  // the products above have used K's unit up
+                    copy(&tmV);
                 const int32_t here = at;
-                pages[0] = next_pages[0];
-                pages[1] = next_pages[1];
-                if (next < end)
-                    fetch(next, of_k);  // into the registers that the products above have read
                 if (here + kChunk > all) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int32_t slot = here + 16 * x + g + 8 * (k >> 1);
-                            if (slot >= lim[k & 1] || slot == hole[k & 1])
-                                s[x][k] = -INFINITY;
+                        for (int k = 0; k < 2; ++k) {
+                            const int32_t slot = here + 16 * x + g + 8 * k;
+                            if (slot >= lim[0] || slot == hole[0])
+                                t[x][k].x = -INFINITY;
+                            if (slot >= lim[1] || slot == hole[1])
+                                t[x][k].y = -INFINITY;
                         }
                 }
-                float fo[2];
-                uint32_t w[2][2];  // weights of slot g and g + 8, rows side by side
-                float p[2][4];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float mx = fmaxf(m[r], max_of_rows(fmaxf(fmaxf(s[0][r], s[0][2 + r]), fmaxf(s[1][r], s[1][2 + r]))));
-                    const float base = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: every t is -inf
-                    const float moved = m[r] == -INFINITY ? 0.f : (m[r] - base) * sl2;
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float &t = s[x][2 * k + r];
-                            t = (t - base) * sl2;
-                            const float e = v_exp[x][k] == kScaleNan ? 0.f : (float)((int)v_exp[x][k] - kScaleBias);
-                            p[x][2 * k + r] = t + e;
-                            top = fmaxf(top, t + e);
-                        }
-                    top = max_of_rows(top);
-                    const float before = c[r] + moved;  // -inf stays
-                    c[r] = fmaxf(before, top);
-                    fo[r] = before == -INFINITY ? 0.f : ptx::ex2(before - c[r]);
-                    l[r] *= ptx::ex2(moved);
-                    m[r] = mx;
-                    const float up = c[r] == -INFINITY ? 0.f : kWeightTop - c[r];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float t = s[x][2 * k + r];
-                            const bool seen = t != -INFINITY;
-                            l[r] += seen ? ptx::ex2(t) + nan[x][k] : 0.f;
-                            const float weight = ptx::ex2(p[x][2 * k + r] + up) + nan[x][k] + (v_exp[x][k] == kScaleNan ? NAN : 0.f);
-                            p[x][2 * k + r] = seen ? weight : 0.f;
-                        }
+                // t: how far each score is behind the running maximum, in powers of two; moved: how far that has moved
+                float2 moved, base;
+                {
+                    const float mx = fmaxf(m[0], max_of_rows(fmaxf(fmaxf(t[0][0].x, t[0][1].x), fmaxf(t[1][0].x, t[1][1].x))));
+                    const float my = fmaxf(m[1], max_of_rows(fmaxf(fmaxf(t[0][0].y, t[0][1].y), fmaxf(t[1][0].y, t[1][1].y))));
+                    base = make_float2(mx == -INFINITY ? 0.f : mx, my == -INFINITY ? 0.f : my);  // nothing seen yet: every t is -inf
+                    moved.x = m[0] == -INFINITY ? 0.f : (m[0] - base.x) * sl2;
+                    moved.y = m[1] == -INFINITY ? 0.f : (m[1] - base.y) * sl2;
+                    m[0] = mx;
+                    m[1] = my;
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
-                        w[x][k] = transposed(pack2<false>(p[x][2 * k], p[x][2 * k + 1]));
-                if (__any_sync(0xffffffffu, fo[0] != 1.f || fo[1] != 1.f)) {
+                        t[x][k] = ptx::mul2(ptx::add2(t[x][k], make_float2(-base.x, -base.y)), make_float2(sl2, sl2));
+                const uint8_t *const v_unit = next_unit();
+                const uint32_t nan = __ballot_sync(0xffffffffu, k_scale == kScaleNan || v_scale == kScaleNan);
+                const int exponent = v_scale == kScaleNan ? 0 : (int)v_scale - kScaleBias;
+                // Weights 2^(t + e - c + kWeightTop) of slots with V's exponent e, c no less than any t + e: the largest e so far where
+                // the slots' are alike, else the largest t + e itself, so that weights far below 1 do not leave fp16.
+                const int most = __reduce_max_sync(0xffffffffu, here + lane < end ? exponent : -1000);
+                const int least = __reduce_min_sync(0xffffffffu, here + lane < end ? exponent : 1000);
+                e_most = max(e_most, most);
+                e_least = min(e_least, least);
+                float2 p[2][2], weight[2][2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        p[x][k] = make_float2(ptx::ex2(t[x][k].x), ptx::ex2(t[x][k].y));
+                const float2 before = ptx::add2(make_float2(c[0], c[1]), moved);  // -inf stays
+                if (e_most - e_least <= kAlike) {
+                    c[0] = c[1] = (float)e_most;
+                    const float factor = __uint_as_float((uint32_t)max(exponent - e_most + (int)kWeightTop + 127, 0) << 23);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float f = __shfl_sync(0xffffffffu, factor, 16 * x + g + 8 * k);
+                            weight[x][k] = ptx::mul2(p[x][k], make_float2(f, f));
+                        }
+                } else {
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float e = __shfl_sync(0xffffffffu, (float)exponent, 16 * x + g + 8 * k);
+                            t[x][k] = ptx::add2(t[x][k], make_float2(e, e));
+                            top[0] = fmaxf(top[0], t[x][k].x);
+                            top[1] = fmaxf(top[1], t[x][k].y);
+                        }
+                    c[0] = fmaxf(before.x, max_of_rows(top[0]));
+                    c[1] = fmaxf(before.y, max_of_rows(top[1]));
+                    const float2 up = make_float2(c[0] == -INFINITY ? 0.f : kWeightTop - c[0], c[1] == -INFINITY ? 0.f : kWeightTop - c[1]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            weight[x][k] = make_float2(ptx::ex2(t[x][k].x + up.x), ptx::ex2(t[x][k].y + up.y));
+                }
+                const float2 fo = make_float2(before.x == -INFINITY ? 0.f : ptx::ex2(before.x - c[0]),
+                                              before.y == -INFINITY ? 0.f : ptx::ex2(before.y - c[1]));
+                const float2 sum = ptx::add2(ptx::add2(p[0][0], p[0][1]), ptx::add2(p[1][0], p[1][1]));
+                const float2 kept = ptx::fma2(make_float2(l[0], l[1]), make_float2(ptx::ex2(moved.x), ptx::ex2(moved.y)), sum);
+                l[0] = kept.x;
+                l[1] = kept.y;
+                if (__builtin_expect(nan != 0, 0)) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            if (nan >> (16 * x + g + 8 * k) & 1u) {
+                                if (p[x][k].x != 0.f || t[x][k].x != -INFINITY)
+                                    l[0] = NAN;
+                                if (p[x][k].y != 0.f || t[x][k].y != -INFINITY)
+                                    l[1] = NAN;
+                            }
+                }
+                uint32_t w[2][2];  // weights of slots g and g + 8, then of the lane's row and slots 2 t4 and 2 t4 + 1
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        w[x][k] = transposed(pack2<false>(weight[x][k].x, weight[x][k].y));
+                if (__any_sync(0xffffffffu, fo.x != 1.f || fo.y != 1.f)) {
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            o[i][k] *= fo[k & 1];
+                        for (int k = 0; k < 4; k += 2) {
+                            const float2 y = ptx::mul2(make_float2(o[i][k], o[i][k + 1]), fo);
+                            o[i][k] = y.x;
+                            o[i][k + 1] = y.y;
+                        }
                 }
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t v[4][kWordsV];  // slots 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = 16 * x + 2 * t4 + (k & 1) + 8 * (k >> 1);
+                        if constexpr (DP == 128)
+                            *reinterpret_cast<uint4 *>(v[k]) = *reinterpret_cast<const uint4 *>(v_unit + r * DP + (g ^ (r & 7)) * 16);
+                        else
+                            *reinterpret_cast<uint2 *>(v[k]) =
+                                *reinterpret_cast<const uint2 *>(v_unit + r * DP + ((g >> 1) ^ (r >> 1 & 3)) * 16 + (g & 1) * 8);
+                        if (here + kChunk > end && here + r >= end) {  // behind the last slot: whatever was there
+#pragma unroll
+                            for (int i = 0; i < kWordsV; ++i)
+                                v[k][i] = 0;
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) {
                         // dims 2 i and 2 i + 1 of the lane's: codes of two slots side by side, then the other two's
                         const uint32_t sel = (i & 1) ? 0x7362 : 0x5140;
-                        const uint32_t lo = __byte_perm(v_codes[x][0][i / 2], v_codes[x][1][i / 2], sel);
-                        const uint32_t hi = __byte_perm(v_codes[x][2][i / 2], v_codes[x][3][i / 2], sel);
-                        mma_f16(o[i], half2_of(lo, false), half2_of(lo, true), half2_of(hi, false), half2_of(hi, true), w[x][0], w[x][1]);
+                        const uint32_t lo = __byte_perm(v[0][i / 2], v[1][i / 2], sel);
+                        const uint32_t hi = __byte_perm(v[2][i / 2], v[3][i / 2], sel);
+                        uint32_t a0, a1, a2, a3;
+                        halves_of(lo, a0, a1);
+                        halves_of(hi, a2, a3);
+                        mma_f16(o[i], a0, a1, a2, a3, w[x][0], w[x][1]);
                     }
-                if (next < end)
-                    fetch(next, of_v);
+                }
+                __syncwarp();
+                scales_now[0] = scales_next[0];
+                scales_now[1] = scales_next[1];
+                if (good && next + kStep < end) {
+                    locate(next + kStep, scales_next);
+                    copy(&tmK);
+                }
             }
 
-            // ---- the warps' results become the part's
+            // ---- the warps' results become the part's; their O take the rings' places
+            auto o_of = [&](int worker) { return reinterpret_cast<float *>(smem_few + worker * kWorkerBytes); };
+            __syncwarp();
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -390,7 +487,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
                 }
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i)
-                    *reinterpret_cast<float2 *>(&sh.o[warp][row][g * (DP / 8) + 2 * i]) = make_float2(o[i][r], o[i][2 + r]);
+                    *reinterpret_cast<float2 *>(o_of(warp) + row * kRowFloats + g * (DP / 8) + 2 * i) = make_float2(o[i][r], o[i][2 + r]);
             }
             worker_barrier();
             // Joins `n` results (m, c, l, O): their maxima, the factors of each O, and the sum of l.
@@ -431,7 +528,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
 #pragma unroll
                 for (int i = 0; i < kWorkers; ++i) {
                     const float f = sh.f[i][row];
-                    const float4 z = *reinterpret_cast<const float4 *>(&sh.o[i][row][dim]);
+                    const float4 z = *reinterpret_cast<const float4 *>(o_of(i) + row * kRowFloats + dim);
                     if (f != 0.f) {
                         y.x = fmaf(f, z.x, y.x);
                         y.y = fmaf(f, z.y, y.y);
@@ -502,6 +599,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
                 }
             }
         }
+        // Copies in flight land before the shared memory goes away: none in a call that went well.
+        if (lane == 0)
+            for (uint32_t u = 0; u < kUnits && u < issued; ++u)
+                wait_drain(ptx::smem_u32(&sh.full[warp][u]), last_parity(issued, u, kUnits));
+        __syncwarp();
     }
     if (!ok)
         atomicExch(&a.status->current, (int32_t)WINO_ERR_ARG);
@@ -512,7 +614,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) attend_few_kernel(const __grid
 }
 
 template <int DP, typename T>
-int launch_few(const AttendArgs &a, int ctas, cudaStream_t stream)
+int launch_few(const CUtensorMap &tk, const CUtensorMap &tv, const AttendArgs &a, int ctas, cudaStream_t stream)
 {
     static std::mutex mu;
     static bool done[64];
@@ -523,7 +625,7 @@ int launch_few(const AttendArgs &a, int ctas, cudaStream_t stream)
         std::lock_guard<std::mutex> g(mu);
         if (!done[dev]) {
             if (cudaFuncSetAttribute(attend_few_kernel<DP, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)sizeof(FewShared)) != cudaSuccess)
+                                     (int)kFewSmem) != cudaSuccess)
                 return WINO_ERR_CUDA;
             done[dev] = true;
         }
@@ -531,14 +633,14 @@ int launch_few(const AttendArgs &a, int ctas, cudaStream_t stream)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kFewThreads);
-    cfg.dynamicSmemBytes = sizeof(FewShared);
+    cfg.dynamicSmemBytes = kFewSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_few_kernel<DP, T>, a) == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, attend_few_kernel<DP, T>, tk, tv, a) == cudaSuccess ? WINO_OK : WINO_ERR_CUDA;
 }
 
 }  // namespace
@@ -554,6 +656,14 @@ bool few_rows(const wino_kv_batch &b)
 int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
 {
     const wino_kv_batch &b = a.b;
+    a.end = b.n_pages;
+    a.box_rows = std::min(b.page_size, kChunk);
+    const int32_t width = b.head_dim <= 64 ? 64 : 128;
+    CUtensorMap tk, tv;
+    int rc;
+    if ((rc = encode_codes(&tk, b.k_cache, b, width, a.box_rows, true)) != WINO_OK ||
+        (rc = encode_codes(&tv, b.v_cache, b, width, a.box_rows, true)) != WINO_OK)
+        return rc;
     a.positions = kFewRows / a.group;
     for (int i = 0; i < 2; ++i) {
         const uint64_t w = (uint64_t)(i + 1) * a.positions;
@@ -563,9 +673,9 @@ int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
     a.wide = (double)b.n_seq * (b.n_rows / a.positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kTaskCost) >=
              2147483648.0;
     const bool bf16 = (b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16;
-    if (b.head_dim <= 64)
-        return bf16 ? wino::launch_few<64, __nv_bfloat16>(a, ctas, stream) : wino::launch_few<64, __half>(a, ctas, stream);
-    return bf16 ? wino::launch_few<128, __nv_bfloat16>(a, ctas, stream) : wino::launch_few<128, __half>(a, ctas, stream);
+    if (width == 64)
+        return bf16 ? wino::launch_few<64, __nv_bfloat16>(tk, tv, a, ctas, stream) : wino::launch_few<64, __half>(tk, tv, a, ctas, stream);
+    return bf16 ? wino::launch_few<128, __nv_bfloat16>(tk, tv, a, ctas, stream) : wino::launch_few<128, __half>(tk, tv, a, ctas, stream);
 }
 
 }  // namespace attend

@@ -1449,6 +1449,10 @@ int launch(const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, 
 int attend_args(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b, uint8_t *scratch,
                 StatusWords *status, AttendArgs *a, CUtensorMap *tq);
 
+// A tensor map over an 8-bit cache's codes (attend_scaled.cu): boxes of box_rows slots of one head and page, `width` (64 or 128)
+// bytes wide, as they are or swizzled by that width.
+int encode_codes(CUtensorMap *m, const void *cache, const wino_kv_batch &b, int32_t width, int32_t box_rows, bool swizzled);
+
 // Few rows per sequence over an 8-bit cache (attend_few.cu): whether a batch is of that kind, and its launch with the arguments
 // of attend_args and the scales.
 bool few_rows(const wino_kv_batch &b);

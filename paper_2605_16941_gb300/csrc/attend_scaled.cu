@@ -2,10 +2,9 @@
 #include "attend_kernel.cuh"
 
 namespace wino {
-namespace {
+namespace attend {
 
-// A tensor map over the codes, boxes of slots of one head and page.
-int encode_codes(CUtensorMap *m, const void *cache, const wino_kv_batch &b, int32_t width, int32_t box_rows)
+int encode_codes(CUtensorMap *m, const void *cache, const wino_kv_batch &b, int32_t width, int32_t box_rows, bool swizzled)
 {
     auto fn = encode_fn();
     if (!fn)
@@ -16,13 +15,15 @@ int encode_codes(CUtensorMap *m, const void *cache, const wino_kv_batch &b, int3
     for (int i = 0; i < 3; ++i)  // the stride of a single entry is never used; the encoder wants a legal one
         st[i] = (cuuint64_t)(dims[i + 1] > 1 ? strides[i] : 128);
     const cuuint32_t box[4] = {(cuuint32_t)width, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUtensorMapSwizzle swizzle = !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE
+                                                 : (width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(cache), dims, st, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
                ? WINO_OK
                : WINO_ERR_CUDA;
 }
 
-}  // namespace
+}  // namespace attend
 
 int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale, const wino_kv_batch &b,
                          const wino_kv_scales &scales, uint8_t *scratch, StatusWords *status, int sm_count, cudaStream_t stream)
@@ -40,8 +41,8 @@ int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale
     a.end = b.n_pages;
     a.tile = TileLayout{1024u, kHalfBytes};
     const int32_t width = b.head_dim <= 64 ? 64 : 128, box_rows = std::min(a.box_rows, kStageN);
-    if ((rc = encode_codes(&tk, b.k_cache, b, width, box_rows)) != WINO_OK ||
-        (rc = encode_codes(&tv, b.v_cache, b, width, box_rows)) != WINO_OK)
+    if ((rc = encode_codes(&tk, b.k_cache, b, width, box_rows, false)) != WINO_OK ||
+        (rc = encode_codes(&tv, b.v_cache, b, width, box_rows, false)) != WINO_OK)
         return rc;
     const bool bf16 = (b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16;
     if (width == 64)
