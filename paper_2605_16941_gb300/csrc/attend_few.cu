@@ -1,21 +1,30 @@
-// attend_few.cu -- wino_attend_scaled for sequences of few rows (single tokens): the codes go from global memory through registers
-// to the tensor cores.
+// attend_few.cu -- wino_attend_scaled for sequences of few rows (single tokens).
 //
-// out = softmax(scale Q K^T) V as in attend_kernel.cuh.  Up to 8 rows times heads of a kv head are a tile, the 8 columns of
-// mma.m16n8k16: S^T = K Q^T and O^T = V^T P^T, with K and V as the A operand.  That is bound by the stream of codes: a token's
-// products would fill 8 of the 128 rows that tcgen05 takes, and its operands would have to go through shared memory twice more.
+// out = softmax(scale Q K^T) V as in attend_kernel.cuh, whose planning warp cuts the work here too.  Up to 8 rows times heads of
+// a kv head are a tile, the 8 columns of mma.m16n8k16: S^T = K Q^T and O^T = V^T P^T, with K and V as the A operand.  The stream of
+// codes bounds this: a token's products would fill a few of the 128 rows that tcgen05 takes, and its operands would have to go
+// through shared memory as values of the element type (attend_kernel.cuh, 64 tokens: 330 us).
 //
-// A warp takes 32 slots at a time, whose codes copies bring to its ring in shared memory, swizzled so that no two of 8 lanes that read
-// does not matter as long as Q's do the same, so the four codes of a word are the four values that a step wants from a
-// lane.  O^T: lane 4 g + t reads 16 neighbouring dims of four slots, and a row of the product is any dim: two of the lane's dims per step,
-// whose codes of two slots are put side by side and converted.  Both ways 64 or 128 neighbouring bytes are read together, and
-// nothing passes through shared memory but the 11 warps' results at the end of a part.
+// A warp takes 32 slots at a time, whose codes copies bring to its own ring in shared memory, swizzled so that no two of the 8 lanes
+// that read at once meet in a bank.  S^T: lane 4 g + t reads 32 codes of slots g and g + 8; which dims meet in a step of 16 does
+// not matter as long as Q's do the same, so the four codes of a word are the four values that a step wants from a lane.  O^T: lane
+// 4 g + t reads 16 neighbouring dims of four slots, and a row of the product may be any dim: two of the lane's dims per
+// step, whose codes of two slots are put side by side and converted.  Weights turn from S^T's layout to O^T's by movmatrix.  At the
+// end of a part the 15 warps' results meet in shared memory, and a task's parts in the workspace, where the last to come
+// joins them in their order.
 //
 // Precision: codes are exact in fp16.  Q is brought to fp16 with a power of two per row that leaves its largest value in
-// [2^14, 2^15): all bits are kept down to 2^-28 of it.  K's scales multiply the scores in fp32.  V's scales are part of the weights:
-// w = 2^(t + e - c) with t the score behind the running maximum m, e the slot's exponent and c the running maximum of t + e; w is
-// rounded to fp16 (half a step; 2^-40 of the largest below its normal range), l sums the unrounded 2^t without e, and the result is
-// 2^c O / l.  Differences of scores are formed before they are scaled, so that scores may lie anywhere.
+// [2^14, 2^15): all bits are kept down to 2^-28 of it.  K's scales multiply the scores in fp32.  V's scales are part of the weights
+// (kAlike, below), which are rounded to fp16 (half a step; steps of 2^-33 of the largest below its normal range), l sums the
+// unrounded 2^t, and the result is 2^c O / l.  Differences of scores are formed before they are scaled, so that scores may
+// lie anywhere.
+//
+// Measured (us, replayed; floors from 6.7 TB/s): 64 tokens over 500 to 32767 slots, 32 heads over 8 kv heads of 128 (821 MB)
+// 166 (floor 122); one over 262144 slots (541 MB) 96 (80); one over 300 slots 9.1.  In the second a warp needs 4200 clocks for 32 slots
+// (29 bytes a clock and SM, 23 at the floor), 240 of them waiting for codes; in the first a part's start and end
+// take 6 us each of its 40.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads
+// ran at 13 bytes a clock and SM, whatever was in flight.  11 warps of 168 registers instead of 15 of 128: 210 and 140 against 223 and
+// 143 with cp.async.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,12 +38,13 @@ using namespace attend;
 constexpr int kWorkers = 15, kFewThreads = 32 * (kWorkers + 1);  // and the planning warp: 16 warps have 128 registers a thread
 constexpr int kFewRows = 8, kChunk = 32;  // rows of a tile, slots at a time of a warp
 constexpr float kWeightTop = 15.f;        // the largest weight is 2^this
-constexpr int kAlike = 6;                 // V's exponents this near to one another share a reference
+constexpr int kAlike = 6;                 // V's exponents within this of one another: see below
 constexpr int kUnits = 3;                 // of a worker's ring: the codes of 32 slots' K, or V
 constexpr uint32_t kUnitBytes = kChunk * 128;
 constexpr uint32_t kWorkerBytes = kUnits * kUnitBytes, kRingBytes = kWorkers * kWorkerBytes;
 constexpr int kRowFloats = 128 + 4;       // of O in shared memory
 static_assert(kFewRows * kRowFloats * sizeof(float) <= kWorkerBytes, "O takes the ring's place at the end of a part");
+static_assert(kMaxCtas * 4 * kFewRows * sizeof(float) <= kRingBytes, "and then the parts' m, c, l and factors");
 
 struct alignas(16) FewShared {
     Part parts[kParts];
@@ -42,7 +52,7 @@ struct alignas(16) FewShared {
     uint64_t full[kWorkers][kUnits];
     int32_t abort, last;
     float m[kWorkers][kFewRows], c[kWorkers][kFewRows], l[kWorkers][kFewRows], f[kWorkers][kFewRows];  // f: factors of O
-    float joined[3][kFewRows];  // m, c, l of all workers
+    float joined[kFewRows][3];  // m, c and l of a row, of all workers and then of all parts
 };
 constexpr uint32_t kFewSmem = kRingBytes + sizeof(FewShared);
 static_assert(kFewSmem <= kSmemLimit, "shared memory");
@@ -490,55 +500,59 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                     *reinterpret_cast<float2 *>(o_of(warp) + row * kRowFloats + g * (DP / 8) + 2 * i) = make_float2(o[i][r], o[i][2 + r]);
             }
             worker_barrier();
-            // Joins `n` results (m, c, l, O): their maxima, the factors of each O, and the sum of l.
-            auto factors = [&](int n, auto m_of, auto c_of, auto l_of, auto put, float &big, float &top, float &sum) {
-                big = -INFINITY;
-                for (int i = 0; i < n; ++i)
-                    big = fmaxf(big, m_of(i));
-                top = -INFINITY;
-                sum = 0.f;
-                for (int i = 0; i < n; ++i) {
-                    const float mi = m_of(i);
-                    if (mi == -INFINITY)
-                        continue;
-                    const float behind = (mi - big) * sl2;
-                    top = fmaxf(top, c_of(i) + behind);
-                    sum += l_of(i) * ptx::ex2(behind);
+            // Joins n results of a row, by a warp: their maxima, the factor of each O, and the sum of l.  of(i): result i's m, c and l.
+            auto factors = [&](int n, auto of, auto put, float *joined) {
+                float big = -INFINITY, top = -INFINITY, sum = 0.f;
+                for (int i = lane; i < n; i += 32)
+                    big = fmaxf(big, of(i).x);
+#pragma unroll
+                for (int i = 16; i; i >>= 1)
+                    big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, i));
+                for (int i = lane; i < n; i += 32) {
+                    const float3 y = of(i);
+                    if (y.x != -INFINITY) {
+                        const float behind = (y.x - big) * sl2;
+                        top = fmaxf(top, y.y + behind);
+                        sum += y.z * ptx::ex2(behind);
+                    }
                 }
-                for (int i = 0; i < n; ++i) {
-                    const float mi = m_of(i);
-                    put(i, mi == -INFINITY ? 0.f : ptx::ex2(c_of(i) + (mi - big) * sl2 - top));
+#pragma unroll
+                for (int i = 16; i; i >>= 1) {
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+                    sum += __shfl_xor_sync(0xffffffffu, sum, i);
+                }
+                for (int i = lane; i < n; i += 32) {
+                    const float3 y = of(i);
+                    put(i, y.x == -INFINITY ? 0.f : ptx::ex2(y.y + (y.x - big) * sl2 - top));
+                }
+                if (lane == 0) {
+                    joined[0] = big;
+                    joined[1] = top;
+                    joined[2] = sum;
                 }
             };
+            static_assert(kWorkers >= kFewRows, "a warp per row");
             const int tid = (int)threadIdx.x;
-            float big = -INFINITY, top = -INFINITY, sum = 0.f;
-            if (tid < kFewRows) {
-                factors(kWorkers, [&](int i) { return sh.m[i][tid]; }, [&](int i) { return sh.c[i][tid]; },
-                        [&](int i) { return sh.l[i][tid]; }, [&](int i, float x) { sh.f[i][tid] = x; }, big, top, sum);
-                sh.joined[0][tid] = big;
-                sh.joined[1][tid] = top;
-                sh.joined[2][tid] = sum;
-            }
+            if (warp < kFewRows)
+                factors(kWorkers, [&](int i) { return make_float3(sh.m[i][warp], sh.c[i][warp], sh.l[i][warp]); },
+                        [&](int i, float f) { sh.f[i][warp] = f; }, sh.joined[warp]);
             worker_barrier();
             // A thread has 4 neighbouring dims of a row.
             const int row = tid / (DP / 4), dim = tid % (DP / 4) * 4;
             const bool mine = row < kFewRows;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (mine) {
-#pragma unroll
-                for (int i = 0; i < kWorkers; ++i) {
-                    const float f = sh.f[i][row];
-                    const float4 z = *reinterpret_cast<const float4 *>(o_of(i) + row * kRowFloats + dim);
-                    if (f != 0.f) {
-                        y.x = fmaf(f, z.x, y.x);
-                        y.y = fmaf(f, z.y, y.y);
-                        y.z = fmaf(f, z.z, y.z);
-                        y.w = fmaf(f, z.w, y.w);
-                    }
+            auto add = [&](float f, const float4 &z) {  // f = 0: z may be anything
+                if (f != 0.f) {
+                    y.x = fmaf(f, z.x, y.x);
+                    y.y = fmaf(f, z.y, y.y);
+                    y.z = fmaf(f, z.z, y.z);
+                    y.w = fmaf(f, z.w, y.w);
                 }
-                big = sh.joined[0][row];
-                top = sh.joined[1][row];
-                sum = sh.joined[2][row];
+            };
+            if (mine) {
+#pragma unroll 5
+                for (int i = 0; i < kWorkers; ++i)
+                    add(sh.f[i][row], *reinterpret_cast<const float4 *>(o_of(i) + row * kRowFloats + dim));
             }
             bool whole = true;
             if ((part.flags & kWhole) == 0) {
@@ -548,44 +562,49 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                 float *const ml = reinterpret_cast<float *>(a.part_ml);
                 const int64_t of_ml = 2 * a.quarters * 64, of_o = (int64_t)2 * a.quarters * 32 * a.piece;
                 float *const po = reinterpret_cast<float *>(a.part_o);
-                if (mine) {
-                    const int64_t to = place((int)blockIdx.x);
-                    if (dim == 0) {
-                        ml[to * of_ml + row] = big;
-                        ml[to * of_ml + 8 + row] = top;
-                        ml[to * of_ml + 16 + row] = sum;
-                    }
+                const int64_t to = place((int)blockIdx.x);
+                if (mine)
                     *reinterpret_cast<float4 *>(&po[to * of_o + row * DP + dim]) = y;
-                }
+                if (tid < 3 * kFewRows)
+                    ml[to * of_ml + tid] = sh.joined[tid / 3][tid % 3];
                 __threadfence();
                 worker_barrier();
                 int32_t *const node = a.nodes + (int64_t)part.first * kLevels * 8;
                 if (tid == 0) {
-                    const int there = atomicAdd(node, 1);
-                    sh.last = there == n - 1;
-                    if (there == n - 1)
+                    const int before = atomicAdd(node, 1);
+                    sh.last = before == n - 1;
+                    if (before == n - 1)
                         *node = 0;  // for the next call
                 }
                 worker_barrier();
                 whole = sh.last != 0;
-                if (whole && mine) {
+                if (whole) {
                     __threadfence();
-                    auto value = [&](int i, int k) { return __ldcg(&ml[place(part.first + i) * of_ml + 8 * k + row]); };
+                    float *const all_ml = reinterpret_cast<float *>(smem_few);  // O is out of the rings
+                    for (int i = tid; i < n * 3 * kFewRows; i += kWorkers * 32) {
+                        const int of = i / (3 * kFewRows);
+                        all_ml[i] = __ldcg(&ml[place(part.first + of) * of_ml + i - of * 3 * kFewRows]);
+                    }
+                    worker_barrier();
+                    float *const all_f = all_ml + kMaxCtas * 3 * kFewRows;
+                    if (warp < kFewRows)
+                        factors(n,
+                                [&](int i) {
+                                    const float *const p = all_ml + (i * kFewRows + warp) * 3;
+                                    return make_float3(p[0], p[1], p[2]);
+                                },
+                                [&](int i, float f) { all_f[i * kFewRows + warp] = f; }, sh.joined[warp]);
+                    worker_barrier();
                     y = make_float4(0.f, 0.f, 0.f, 0.f);
-                    factors(n, [&](int i) { return value(i, 0); }, [&](int i) { return value(i, 1); },
-                            [&](int i) { return value(i, 2); },
-                            [&](int i, float f) {
-                                if (f != 0.f) {
-                                    const float4 z = __ldcg(reinterpret_cast<const float4 *>(&po[place(part.first + i) * of_o + row * DP + dim]));
-                                    y.x = fmaf(f, z.x, y.x);
-                                    y.y = fmaf(f, z.y, y.y);
-                                    y.z = fmaf(f, z.z, y.z);
-                                    y.w = fmaf(f, z.w, y.w);
-                                }
-                            },
-                            big, top, sum);
+                    if (mine) {
+#pragma unroll 4
+                        for (int i = 0; i < n; ++i)
+                            add(all_f[i * kFewRows + row],
+                                __ldcg(reinterpret_cast<const float4 *>(&po[place(part.first + i) * of_o + row * DP + dim])));
+                    }
                 }
             }
+            const float top = mine ? sh.joined[row][1] : 0.f, sum = mine ? sh.joined[row][2] : 0.f;
             if (whole && mine && dim < b.head_dim) {
                 const int pos = row / a.group, i = part.i0 + pos;
                 if (pos < a.positions && i < part.q.n) {
