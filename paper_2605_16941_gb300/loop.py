@@ -17,8 +17,9 @@ from __future__ import annotations
 from dataclasses import dataclass, field
 from typing import Callable
 
-from ._abi import (WINO_ERR_MAX_STEPS, WINO_MASK_FULL, WINO_MASK_SHADOW, WINO_OK, WinoError, WinoKvBatch, WinoRope,
-                   attend_workspace, make_kv_batch, make_params, wino_attend, wino_decode, wino_rope_append, wino_step,
+from ._abi import (WINO_ERR_MAX_STEPS, WINO_MASK_FULL, WINO_MASK_SHADOW, WINO_OK, WinoError, WinoHeadNorm, WinoKvBatch,
+                   WinoRope, WinoRopeAxes, attend_workspace, make_kv_batch, make_params, wino_attend, wino_attend_scaled,
+                   wino_cache_read, wino_decode, wino_norm_rope_append, wino_rope_append, wino_step,
                    wino_workspace_size_step)
 
 
@@ -224,21 +225,29 @@ class BlockCache:
     in the cache passes ``seen=seq_len`` to every step.  What is in the cache stays as its last pass made it, until ``context``
     is called on it again; the paper's pass over everything is the rows left of the block, right of it and the step's, all with
     ``seen=seq_len``, each layer storing all of them before any attends.  Within a layer, ``append`` rotates q (in place) and stores k and v, then
-    ``attend`` reads what the rows see.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws``, so a
+    ``attend`` reads what the rows see; ``read`` takes stored rows out again.  Layers that normalise queries and keys per head give
+    ``append`` their ``norm``, positions of several axes their ``axes``.  ``scaled``: the caches hold 8-bit codes and a power of two
+    per position and head (``k_scale``, ``v_scale``), half of the memory and of what attention reads; ``dtype`` is that of
+    the rows then.  Everything runs on PyTorch's current stream; the layers share the workspace ``ws``, so a
     decode keeps to one stream.  What the device finds wrong (a wait that ran out, a bad page) is not raised here: the rows
     concerned are undefined, and ``wino_read_device_status(ws)`` returns the first failure of any layer since it was last read,
     so once per step, or per decode, is enough.  The decode loops do not know the cache and do not ask.
     """
 
     def __init__(self, n_layers: int, n_seq: int, seq_len: int, blk_len: int, n_q_heads: int, n_kv_heads: int,
-                 head_dim: int, *, page_size: int = 64, dtype=None, device="cuda", no_shadow: bool = False):
+                 head_dim: int, *, page_size: int = 64, dtype=None, device="cuda", no_shadow: bool = False,
+                 scaled: bool = False):
         import torch
         self.n_layers, self.n_seq, self.seq_len, self.blk_len = n_layers, n_seq, seq_len, blk_len
         self.n_q_heads, self.no_shadow = n_q_heads, no_shadow
         width = -(-(seq_len + blk_len) // page_size)
         shape = (n_layers, n_seq * width, n_kv_heads, page_size, head_dim)
-        dtype = torch.bfloat16 if dtype is None else dtype
-        self.k, self.v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        self.dtype = dtype = torch.bfloat16 if dtype is None else dtype
+        self.scaled = scaled
+        self.k, self.v = (torch.zeros(shape, dtype=torch.uint8 if scaled else dtype, device=device) for _ in range(2))
+        if scaled:
+            self.k, self.v = self.k.view(torch.float8_e4m3fn), self.v.view(torch.float8_e4m3fn)
+            self.k_scale, self.v_scale = (torch.zeros(shape[:-1], dtype=torch.uint8, device=device) for _ in range(2))
         self.page_table = torch.arange(n_seq * width, dtype=torch.int32, device=device).view(n_seq, width)
         # one for the batches of any rows, never replaced: a captured call goes on using it
         most = self._batches(min(seq_len + blk_len, (1 << 24) // n_seq), 0, 0, WINO_MASK_FULL)
@@ -250,8 +259,11 @@ class BlockCache:
         torch.arange(0, self.n_seq * rows, rows, dtype=torch.int32, device=ints.device, out=ints[0])
         for i, x in enumerate((rows, kv_len, new_slot)):
             ints[i + 1].fill_(x)
+
+        def scales(i):
+            return dict(k_scale=self.k_scale[i], v_scale=self.v_scale[i], dtype=self.dtype) if self.scaled else {}
         return [make_kv_batch(self.k[i].transpose(1, 2), self.v[i].transpose(1, 2), self.page_table, *ints,
-                              n_rows=self.n_seq * rows, n_q_heads=self.n_q_heads, mask=mask)
+                              n_rows=self.n_seq * rows, n_q_heads=self.n_q_heads, mask=mask, **scales(i))
                 for i in range(self.n_layers)]
 
     def _seen(self, end: int, seen: int | None) -> int:
@@ -276,8 +288,16 @@ class BlockCache:
             return self._batches(self.blk_len, seen, blk_start, WINO_MASK_FULL)
         return self._batches(2 * self.blk_len, seen, blk_start, WINO_MASK_SHADOW)
 
-    def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope) -> None:
-        wino_rope_append(q, k, v, batch, rope, self.ws)
+    def append(self, q, k, v, batch: WinoKvBatch, rope: WinoRope, *, norm: WinoHeadNorm | None = None,
+               axes: WinoRopeAxes | None = None) -> None:
+        if self.scaled or norm is not None or axes is not None:
+            wino_norm_rope_append(q, k, v, batch, rope, self.ws, norm=norm, axes=axes)
+        else:
+            wino_rope_append(q, k, v, batch, rope, self.ws)
 
     def attend(self, q, out, batch: WinoKvBatch, *, scale: float | None = None) -> None:
-        wino_attend(q, out, batch, self.ws, scale=scale)
+        (wino_attend_scaled if self.scaled else wino_attend)(q, out, batch, self.ws, scale=scale)
+
+    def read(self, k, v, batch: WinoKvBatch) -> None:
+        """The keys (rotated, as stored) and values of the batch's rows into ``k`` and ``v`` (either may be None)."""
+        wino_cache_read(k, v, batch, self.ws)

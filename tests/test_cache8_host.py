@@ -235,3 +235,13 @@ def test_the_definition_itself():
         assert ((most <= 448 * 2.0 ** e) | (e == 7)).all() and ((most > 448 * 2.0 ** (e - 1)) | (e == e_min)).all()
         codes, s = quantise(torch.from_numpy(z)[None, :, None], dtype)
         assert np.array_equal(values_of(codes, s, dtype)[0, :, 0].double().numpy(), held_values(z, dtype))
+
+
+def test_block_cache_in_8_bits():
+    from paper_2605_16941_gb300 import loop
+    c = loop.BlockCache(2, 3, 50, 8, 4, 2, 64, page_size=16, device="cpu", scaled=True, dtype=FP)
+    assert c.k.dtype == torch.float8_e4m3fn and c.k_scale.shape == c.k.shape[:-1] and c.k_scale.dtype == torch.uint8
+    for b in (c.step(20)[1], c.context(0, 20)[1]):
+        assert b.dtype == E4M3 | wino.WINO_FP16 and b.k_cache == c.k[1].data_ptr() and b.scales.v_scale == c.v_scale[1].data_ptr()
+    with pytest.raises(wino.WinoError):
+        loop.BlockCache(1, 1, 50, 8, 4, 2, 24, page_size=16, device="cpu", scaled=True)
