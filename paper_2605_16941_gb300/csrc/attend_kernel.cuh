@@ -80,7 +80,7 @@ constexpr float kTopBits[2] = {9.9f, 0.f};     // the P of a score of m is 2^thi
 constexpr float kFarBits = 65536.f;            // up to here m sl2 is rounded by 2^-8 at most: P stays below 65504
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kSharedBytes = 3 * 1024;  // for struct Shared, behind the tiles
-constexpr int kStageN = 64;  // slots of a stage of codes
+constexpr int kStageN = kTileN;  // slots of a stage of codes
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 // Where slot row r, dims 64 h .. 64 h + 63 of a K or V tile lie: (r / 8) group + h half + (r % 8) 128 bytes.  With 128 dims
 // one copy brings both halves of a page's rows, interleaved by groups of 8 rows, if the cache's strides let one
@@ -203,7 +203,7 @@ struct Config {
     // values of both, in the order of their use, and behind it stages of codes, of K and as many of V.
     static constexpr int kSlotsK = kScaled ? 0 : (DP == 128 ? 2 : 5), kSlotsV = kScaled ? (DP == 128 ? 4 : 6) : (DP == 128 ? 3 : 7);
     static constexpr int kSlots = kSlotsK + kSlotsV;
-    static constexpr int kStages = kScaled ? (DP == 128 ? 2 : 4) : 0;
+    static constexpr int kStages = kScaled ? (DP == 128 ? 1 : 2) : 0;
     static constexpr uint32_t kStageBytes = kStageN * DP;
     static constexpr uint32_t kRing = kSlots * kTileBytes + 2 * kStages * kStageBytes;
     static constexpr uint32_t kShared = kSharedBytes + (kScaled && DP == 64 ? 1024 : 0);
@@ -1061,12 +1061,11 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                     ++parts;
                 }
                 if constexpr (kScaled) {
-                    // codes and scales, a box and an untiled copy per page and stage; no stage behind the last slot
-                    const int32_t stages = min(2 * n, (part.kv_end - part.j0 * kTileN + kStageN - 1) / kStageN);
-                    const int32_t box_rows = min(a.box_rows, kStageN), of_stage = kStageN / box_rows;
-                    for (int32_t x = 0; x < stages; ++x) {
+                    // codes and scales, a box and an untiled copy per page
+                    const int32_t box_rows = a.box_rows;
+                    for (int32_t x = 0; x < n; ++x) {
                         const int32_t first = part.j0 * kTileN + x * kStageN;
-                        const int32_t boxes = min(of_stage, (part.kv_end - first + box_rows - 1) / box_rows);
+                        const int32_t boxes = min(a.boxes, (part.kv_end - first + box_rows - 1) / box_rows);
                         const int32_t at = first + lane * box_rows;
                         const int32_t entry = page_entry(a, at);
                         if (page_entry(a, first + boxes * box_rows - 1) - window >= 32) {  // no stage straddles the border
@@ -1310,7 +1309,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
         // ------------------------------------------------------------ codes to values
         ptx::regs_dec<72>();
         constexpr int kChunks = DP / 16, kAtOnce = 32 / kChunks;  // chunks of 16 codes per slot, slots per turn of a warp
-        constexpr int kTurns = 16 / kAtOnce;                      // a warp's 16 slots of a stage
+        constexpr int kHalfN = kTileN / 2, kTurns = 16 / kAtOnce;  // a warp's 16 slots of half a tile
         const int of_warp = (warp & 3) * 16 + lane / kChunks, chunk = lane % kChunks;
         const bool swap = chunk >= 4;  // which 8 of 16 values are written first: no two of 8 lanes meet in a bank
         int tile = 0, stage_k = 0, stage_v = 0;  // the next of each ring, and their phases
@@ -1332,32 +1331,23 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 ++(is_v ? next_v : next_k);
                 if (!(good = warp_wait(empty(tile), phase ^ 1u, &sh.abort)))
                     break;
+                const int stage = is_v ? C::kStages + stage_v : stage_k;
+                if (!(good = warp_wait(stage_full(stage), is_v ? phase_v : phase_k, &sh.abort)))
+                    break;
                 // A tile as TMA would write it: swizzled blocks of 64 dims, in which 16 bytes of row r lie at the place of
                 // their number xor r % 8.
                 uint8_t *const to = smem_raw + (slot_addr(tile) - raw) + (chunk >> 2) * kHalfBytes;
+                const uint8_t *const codes = smem_raw + kStage0 + (uint32_t)stage * C::kStageBytes;
 #pragma unroll 1
-                for (int half = 0; half < 2; ++half, left -= kStageN) {
+                for (int half = 0; half < 2; ++half, left -= kHalfN) {
                     uint4 c[kTurns];
                     uint32_t f[kTurns];
-                    int used = -1;
-                    if (left > 0) {
-                        const int stage = is_v ? C::kStages + stage_v : stage_k;
-                        if (!(good = warp_wait(stage_full(stage), is_v ? phase_v : phase_k, &sh.abort)))
-                            break;
-                        const uint8_t *const codes = smem_raw + kStage0 + (uint32_t)stage * C::kStageBytes;
 #pragma unroll
-                        for (int k = 0; k < kTurns; ++k) {
-                            c[k] = *reinterpret_cast<const uint4 *>(codes + (of_warp + k * kAtOnce) * DP + chunk * 16);
-                            f[k] = sh.scale[stage][of_warp + k * kAtOnce];
-                        }
-                        used = stage;
-                        int &s = is_v ? stage_v : stage_k;
-                        if (++s == C::kStages) {
-                            s = 0;
-                            (is_v ? phase_v : phase_k) ^= 1u;
-                        }
+                    for (int k = 0; k < kTurns; ++k) {
+                        c[k] = *reinterpret_cast<const uint4 *>(codes + (half * kHalfN + of_warp + k * kAtOnce) * DP + chunk * 16);
+                        f[k] = sh.scale[stage][half * kHalfN + of_warp + k * kAtOnce];
                     }
-                    if (left < kStageN) {  // behind the last slot: zeros, which V needs
+                    if (left < kHalfN) {  // behind the last slot: zeros, which V needs
 #pragma unroll
                         for (int k = 0; k < kTurns; ++k)
                             if (of_warp + k * kAtOnce >= left) {
@@ -1367,7 +1357,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                     }
 #pragma unroll
                     for (int k = 0; k < kTurns; ++k) {
-                        const int r = half * kStageN + of_warp + k * kAtOnce;
+                        const int r = half * kHalfN + of_warp + k * kAtOnce;
                         const uint32_t factor = read_factor<kBf16>(f[k]);
                         uint4 lo, hi;
                         decode4<kBf16>(c[k].x, factor, lo.x, lo.y);
@@ -1378,21 +1368,23 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at ^ 1 : at) * 16) = swap ? hi : lo;
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at : at ^ 1) * 16) = swap ? lo : hi;
                     }
-                    // Given back once its values have been used, not once they have been asked for: a copy was seen to overtake
-                    // reads that were still on their way.
-                    __syncwarp();
-                    if (lane == 0 && used >= 0)
-                        ptx::mbar_arrive(stage_free(used));
                 }
-                if (!good)
-                    break;
                 ptx::fence_proxy_async();
                 __syncwarp();
-                if (lane == 0)
+                // The stage is given back once its values have been used, not once they have been asked for: a copy was seen to
+                // overtake reads that were still on their way.
+                if (lane == 0) {
                     ptx::mbar_arrive(full(tile));
+                    ptx::mbar_arrive(stage_free(stage));
+                }
                 if (++tile == C::kSlots) {
                     tile = 0;
                     phase ^= 1u;
+                }
+                int &s = is_v ? stage_v : stage_k;
+                if (++s == C::kStages) {
+                    s = 0;
+                    (is_v ? phase_v : phase_k) ^= 1u;
                 }
             }
             if (!good)

@@ -40,7 +40,7 @@ int launch_attend_scaled(const wino_heads &q, const wino_heads &out, float scale
         return launch_few(a, ctas, stream);
     a.end = b.n_pages;
     a.tile = TileLayout{1024u, kHalfBytes};
-    const int32_t width = b.head_dim <= 64 ? 64 : 128, box_rows = std::min(a.box_rows, kStageN);
+    const int32_t width = b.head_dim <= 64 ? 64 : 128, box_rows = a.box_rows;
     if ((rc = encode_codes(&tk, b.k_cache, b, width, box_rows, false)) != WINO_OK ||
         (rc = encode_codes(&tv, b.v_cache, b, width, box_rows, false)) != WINO_OK)
         return rc;

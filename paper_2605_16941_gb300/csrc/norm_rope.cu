@@ -56,7 +56,9 @@ __device__ __forceinline__ float inverse_rms(float2 (&x)[kN], int lanes, float i
             eps = 0.f;  // times 2^-200
         }
     }
-    return rsqrtf(s * inv_dim + eps);
+    // a Newton step: the root's own error, 2^-22, would move a code's border more than the rest of the arithmetic does
+    const float x2 = s * inv_dim + eps, r = rsqrtf(x2);
+    return r * fmaf(-0.5f * x2 * r, r, 1.5f);
 }
 
 enum class Kind { kQ, kK, kV };
