@@ -9,6 +9,7 @@ namespace wino {
 namespace {
 
 constexpr int kThreads = kRopeThreads;
+constexpr int kAhead = 4;  // rows of which a thread has loads in flight
 
 struct ReadArgs {
     wino_heads k, v;
@@ -29,25 +30,50 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
     ptx::grid_dep_wait();
     find_rows(b, wino_rope{}, nullptr, true, a.status, sh, row0, n_rows);
     const int chunks = b.head_dim / 8, units = 2 * b.n_kv_heads * chunks;
-    for (int x = (int)threadIdx.x; x < n_rows * units; x += kThreads) {
-        const int r = x / units, y = x - r * units, h = y / chunks, c = y - h * chunks;
+    for (int y = (int)threadIdx.x; y < units; y += kThreads) {
+        const int h = y / chunks, c = y - h * chunks;
         const bool is_v = h >= b.n_kv_heads;
         const int hk = is_v ? h - b.n_kv_heads : h;
         const wino_heads &to = is_v ? a.v : a.k;
-        if (sh.seq[r] < 0 || sh.page[r] < 0 || !to.data)
+        if (!to.data)
             continue;
-        const int64_t at = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride + hk * b.head_stride + 8 * c;
         const uint16_t *const cache = is_v ? b.v_cache : b.k_cache;
-        uint4 out;
-        if (kScaled) {
-            const uint2 codes = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(cache) + at);
-            const uint32_t f = read_factor<kBf16>((is_v ? a.scales.v_scale : a.scales.k_scale)[scale_at(b, sh.page[r], sh.in_page[r], hk)]);
-            decode4<kBf16>(codes.x, f, out.x, out.y);
-            decode4<kBf16>(codes.y, f, out.z, out.w);
-        } else {
-            out = *reinterpret_cast<const uint4 *>(cache + at);
+        const uint8_t *const scales = is_v ? a.scales.v_scale : a.scales.k_scale;
+        const int64_t at = hk * b.head_stride + 8 * c;
+        uint16_t *const dst = to.data + row0 * to.row_stride + hk * to.head_stride + 8 * c;
+#pragma unroll 1
+        for (int r0 = 0; r0 < n_rows; r0 += kAhead) {
+            uint4 out[kAhead];
+            uint32_t scale[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int r = min(r0 + k, n_rows - 1);
+                if (sh.seq[r] < 0 || sh.page[r] < 0)
+                    continue;
+                const int64_t slot = at + (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride;
+                if (kScaled) {
+                    const uint2 codes = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(cache) + slot);
+                    out[k].x = codes.x;
+                    out[k].y = codes.y;
+                    scale[k] = scales[scale_at(b, sh.page[r], sh.in_page[r], hk)];
+                } else {
+                    out[k] = *reinterpret_cast<const uint4 *>(cache + slot);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int r = r0 + k;
+                if (r >= n_rows || sh.seq[r] < 0 || sh.page[r] < 0)
+                    continue;
+                if (kScaled) {
+                    const uint2 codes = make_uint2(out[k].x, out[k].y);
+                    const uint32_t f = read_factor<kBf16>(scale[k]);
+                    decode4<kBf16>(codes.x, f, out[k].x, out[k].y);
+                    decode4<kBf16>(codes.y, f, out[k].z, out[k].w);
+                }
+                *reinterpret_cast<uint4 *>(dst + r * to.row_stride) = out[k];
+            }
         }
-        *reinterpret_cast<uint4 *>(to.data + (int64_t)(row0 + r) * to.row_stride + hk * to.head_stride + 8 * c) = out;
     }
 }
 
