@@ -483,9 +483,9 @@ WINO_API int wino_attend_workspace_size(const wino_kv_batch *b, size_t *bytes);
  *           cache
  *   scale   >= 2^-126, < 2^127 (commonly head_dim^-1/2); scores and scale times scores
  *           have to be finite in fp32
- *   ws      256-byte aligned, zero-filled before its first use, used by
- *           wino_attend and wino_rope_append only; calls that may overlap on
- *           the GPU need workspaces of their own
+ *   ws      256-byte aligned, zero-filled before its first use, used by the
+ *           paged-cache calls only; calls that may overlap on the GPU need
+ *           workspaces of their own
  * The result does not depend on the order in which CTAs run.  WINO_ERR_SHAPE
  * also for sizes at which the work could not be counted in 62 bits (n_seq
  * times n_rows times slots beyond any real batch).
@@ -568,8 +568,12 @@ WINO_API int wino_cache_read(const wino_heads *k, const wino_heads *v, const win
 /*
  * wino_attend over an 8-bit cache: the same rows, masks, arguments, workspace
  * and errors, K and V the values that codes and scales stand for.  The result is
- * that of wino_attend over a cache of the element type that holds these values.
- * Codes and scales in slots that no row of the sequence sees have no effect.
+ * that of wino_attend over a cache of the element type that holds these values:
+ * bit for bit, unless n_rows is at most n_seq * floor(8 / G) with G <= 8 query
+ * heads to a kv head (single tokens).  Those have a kernel of their own, with
+ * weights in fp16 whatever the element type (those below 2^-23 of a row's largest
+ * to steps of 2^-33 of it, V's scales included in both).  Codes and scales in slots
+ * that no row of the sequence sees have no effect.
  */
 WINO_API int wino_attend_scaled(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b,
                                 const wino_kv_scales *scales, void *ws, size_t ws_bytes, void *stream);
@@ -579,10 +583,11 @@ WINO_API int wino_attend_scaled(const wino_heads *q, const wino_heads *out, floa
  * (published by its last kernel): WINO_OK, WINO_ERR_DEVICE_TIMEOUT (a bounded
  * wait expired), WINO_ERR_ARG (an active-sequence list entry out of range, or
  * what a batch's device arrays must not hold, see wino_kv_batch) or
- * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).  Of wino_rope_append
- * and wino_attend calls, of which a step makes some per layer on one workspace,
- * it returns the first failure since the status of `ws` was last read, and
- * clears it: one read per step tells of all its layers.
+ * WINO_ERR_UNSUPPORTED (the TMEM allocation check failed).  Of paged-cache
+ * calls (the appends, wino_cache_read, both attentions), of which a step makes
+ * some per layer on one workspace, it returns the first failure since the status
+ * of `ws` was last read, and clears it: one read per step tells of all its
+ * layers.
  */
 WINO_API int wino_read_device_status(void *ws, void *stream, int *device_status);
 

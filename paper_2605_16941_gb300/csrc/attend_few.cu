@@ -514,6 +514,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                         const float behind = (y.x - big) * sl2;
                         top = fmaxf(top, y.y + behind);
                         sum += y.z * ptx::ex2(behind);
+                    } else {
+                        sum += y.z;  // 0, or NaN where every score is that
                     }
                 }
 #pragma unroll
@@ -666,10 +668,17 @@ int launch_few(const CUtensorMap &tk, const CUtensorMap &tv, const AttendArgs &a
 
 namespace attend {
 
+// The units that a batch may have at most in tasks of one tile, as attend_units counts them.
+static double few_units(const wino_kv_batch &b)
+{
+    const int32_t positions = kFewRows / (b.n_q_heads / b.n_kv_heads);
+    return (double)b.n_seq * (b.n_rows / positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kTaskCost);
+}
+
 bool few_rows(const wino_kv_batch &b)
 {
     const int32_t group = b.n_q_heads / b.n_kv_heads;
-    return group <= kFewRows && b.n_rows <= (int64_t)b.n_seq * (kFewRows / group);
+    return group <= kFewRows && b.n_rows <= (int64_t)b.n_seq * (kFewRows / group) && few_units(b) < 4611686018427387904.0;
 }
 
 int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
@@ -689,8 +698,7 @@ int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
         a.magic[i] = (uint32_t)(((uint64_t(1) << 32) + w - 1) / w);
     }
     a.min_units = 6;
-    a.wide = (double)b.n_seq * (b.n_rows / a.positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kTaskCost) >=
-             2147483648.0;
+    a.wide = few_units(b) >= 2147483648.0;
     const bool bf16 = (b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16;
     if (width == 64)
         return bf16 ? wino::launch_few<64, __nv_bfloat16>(tk, tv, a, ctas, stream) : wino::launch_few<64, __half>(tk, tv, a, ctas, stream);

@@ -35,6 +35,17 @@
 //     pays its own chain of latencies.  Single tokens over 61 slots, 8 heads of 64 over 2: 10 for 32 sequences, 29 for 256, 92
 //     for 1024, 371 for 4096, 1620 for 16384 (floor 81).
 //
+// An 8-bit cache (kScaled).  Two warps copy the codes of a slot tile and their scales into stages, one of K and one of V (two each
+// with 64 dims), and four warps more write them as the tiles of the element type that TMA would have brought, swizzled, into one ring
+// for both in the order of their use; from there on all is as above, and so are the results.  Few rows have a kernel of their own
+// (attend_few.cu).  What bounds it: those four warps, some 1600 clocks a tile in bf16 and 1170
+// in fp16 (804 and 581 of conversion by themselves, the rest reads of shared memory and waits, with one such warp to a
+// scheduler), K's and V's one after the other: 4 x 512 rows of 32 heads over 8-bit caches of 1605 to 3890 slots 69 us, 57 over 16-bit ones.
+// Shared memory alone would take 2560 clocks per pair of tiles at 128 bytes a clock (MMAs 1536, copies 256, conversion 768).
+// Tried, same case: codes straight from global memory to registers 122 (latency), eight warps for them 84 (the other roles' registers
+// then do not suffice), the next half tile's codes read while one is written 89, 44 bytes of spilled registers in any role 79,
+// stages of 64 slots 70.5.
+//
 // Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one device.
 //
 // Precision: S, m, l and O in fp32; P is rounded to the element type because the tensor cores take no wider weights beside

@@ -1,6 +1,9 @@
 // cache_read.cu -- wino_cache_read: K and V of the batch's rows out of the cache's pages, codes as the values they stand for.
 //
-// Bound by HBM: each element is read and written once; a thread moves 8 elements of a head (16 bytes, from 8 codes or 16 bytes).
+// Bound by HBM: each element is read and written once; a thread moves 8 elements of a head (16 bytes, from 8 codes or 16 bytes)
+// for one row after the other, with the loads of four in flight.  Measured (us, replayed; floors from 6.7 TB/s): 2048 rows of 2 x 32
+// heads of 128 from a 16-bit cache 12 (10), 13481 of 2 x 8 15.6 (16.4, in part from the L2 cache), 28931 of 2 x 8 from an 8-bit one 33 (26);
+// a row and chunk at a time 23, 21 and 47.
 #include "e4m3.cuh"
 #include "ptx.cuh"
 #include "rope_rows.cuh"

@@ -4,6 +4,14 @@
 // y = x (offset + w) / sqrt(mean(x^2) + eps) for a head x, then for each pair of its first rot_dim dims
 // a' = m (a cos t - b sin t), b' = m (b cos t + a sin t), all in fp32; then one rounding.  Sums of squares beyond 2^100 are
 // formed again of x 2^-100, so that no finite x overflows; eps >= 2^-60 covers what underflows.
+//
+// Bound by HBM where there are many rows, by latencies where there are few: every element is read and written once.  Measured
+// (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 5.0 (one chain of loads: lengths, pages, rows); 2048 rows
+// of 32 + 2 x 32 heads with three axes (101 MB) 27 (floor 15); 13481 rows of 32 + 2 x 8 heads with weights per head (331 MB) 69 (49);
+// 28931 rows into an 8-bit cache (651 MB) 142 (97).  The rest is instructions, some 230 per 16 elements of a lane, at half of the
+// issue slots, and the look-up of a CTA's rows.  What counted: the rotation's two layouts as branches, not as selects of
+// registers (2048 rows 56 and 31), heads of one kind per warp with the next ones' loads ahead, shared weights in shared memory
+// (198 and 220 at 28931 rows, read back).  3 CTAs an SM: 4 spill (35 instead of 28 at 2048 rows), 2 take 26, but 79 instead of 69 at 13481.
 #include <type_traits>
 
 #include "e4m3.cuh"
@@ -58,7 +66,7 @@ __device__ __forceinline__ float inverse_rms(float2 (&x)[kN], int lanes, float i
     }
     // a Newton step: the root's own error, 2^-22, would move a code's border more than the rest of the arithmetic does
     const float x2 = s * inv_dim + eps, r = rsqrtf(x2);
-    return r * fmaf(-0.5f * x2 * r, r, 1.5f);
+    return x2 < 0x1p127f ? r * fmaf(-0.5f * x2 * r, r, 1.5f) : r;  // infinite elements leave 0 of the finite ones
 }
 
 enum class Kind { kQ, kK, kV };

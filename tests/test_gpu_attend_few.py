@@ -122,6 +122,17 @@ def test_nan_rows():
         assert torch.isnan(c.out.float()).all(), name
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_query_that_is_nan_gives_nan(rows):
+    """In its row and head and no other, over few rows and over many."""
+    c = add_rows(make_kv8(CAUSAL, [(rows, 500, 500 - rows)], heads=4, kv_heads=2, dim=128))
+    c.q[rows - 1, 2, 7] = float("nan")
+    ws = attend8(c)
+    assert wino.wino_read_device_status(ws) == wino.WINO_OK
+    out = torch.isnan(c.out.float())
+    assert out[rows - 1, 2].all() and out.sum() == 128
+
+
 def test_bad_pages_and_lengths_are_errors():
     c = add_rows(make_kv8(CAUSAL, [(1, 500, 499), (1, 90, 89)], heads=8, kv_heads=2, dim=128))
     for bad in (-1, c.extra["k8"].size(0), 1 << 30):

@@ -246,6 +246,23 @@ def test_rows_of_any_size_are_normalised(dtype, sizes, dim):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [128, 72])
+def test_infinities_and_nan_under_the_norm(dim, dtype):
+    """By the formula: an infinity's root mean square leaves zeros of the finite elements and NaN of itself, a NaN leaves NaN."""
+    c = Call(CAUSAL, [(4, 4, 0)], dtype=dtype, dim=dim, rot=0, heads=2, kv_heads=2)
+    for x in (c.q, c.k):
+        x[0, 0, 3], x[1, 1, dim - 1], x[2, 0, 0] = float("inf"), -float("inf"), float("nan")
+    x = f64(c.q), f64(c.k)
+    c.append()
+    got = f64(c.out), f64(c.c.k_cache)[c.c.table[0, 0], :4]
+    for i, w in enumerate((c.qw, c.kw)):
+        with np.errstate(invalid="ignore"):
+            z = normed(x[i], w, c.eps, c.offset)
+        assert np.array_equal(np.isnan(got[i]), np.isnan(z))
+        assert (got[i][0, 0, [0, 1, 2, 4]] == 0).all() and np.isfinite(got[i][3]).all()
+
+
 @pytest.mark.parametrize("dtype,sizes", [(BF, 30.0), (FP, 12.0)], ids=["bf16", "fp16"])
 @pytest.mark.parametrize("rot", [0, 64, 20])
 def test_codes_of_rows_of_any_size(dtype, sizes, rot):
