@@ -1,5 +1,5 @@
 """wino_attend_scaled for sequences of few rows, whose codes go straight to the tensor cores, against the definition in 64 bits
-(kv_helpers, with its tolerances): groups, dims, lengths around its 32 slots and 11 warps, parts over several CTAs, scales of any
+(kv_helpers, with its tolerances): groups, dims, lengths around its 32 slots and 15 warps, parts over several CTAs, scales of any
 size, and rows beyond what it expects."""
 import pytest
 import torch
@@ -33,9 +33,24 @@ def test_dims(dim, layout):
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 def test_lengths(page):
-    """Around a warp's 32 slots, a round of 11 warps (352), slot tiles and pages."""
+    """Around a warp's 32 slots, rounds of 11, slot tiles and pages."""
     run(add_rows(make_kv8(CAUSAL, [(1, n, n - 1) for n in (1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 351, 352, 353, 384, 704, 705)],
                           heads=4, kv_heads=1, dim=128, page=page, gap=1)))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_lengths_around_a_round(dim):
+    """Of 15 warps: 480 slots."""
+    run(add_rows(make_kv8(CAUSAL, [(1, n, n - 1) for n in (447, 448, 449, 479, 480, 481, 512, 513, 959, 960, 961, 1440)], heads=4, kv_heads=2,
+                          dim=dim, page=32)))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("group,rows", [(4, 4), (4, 3), (8, 2), (5, 2), (1, 16), (3, 4), (2, 7)])
+def test_two_tiles_of_rows(group, rows, dtype):
+    """Rows of a sequence and kv head in two tiles of 8, the second in part; another sequence with more, one with fewer, and some without."""
+    run(add_rows(make_kv8(CAUSAL, [(rows, 700, 700 - rows), (rows + 1, 65, 64 - rows), (rows - 1, 1300, 1301 - rows)] +
+                          [(0, 9, 0)] * 4, heads=2 * group, kv_heads=2, dim=128, dtype=dtype)))
 
 
 @pytest.mark.parametrize("mask,seqs", [
