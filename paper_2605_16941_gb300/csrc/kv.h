@@ -27,7 +27,7 @@ cudaError_t launch_rope_append(const wino_heads *q, const wino_heads *q_out, con
 cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
                                     const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes,
                                     const wino_head_norm *norm, const wino_kv_scales *scales, StatusWords *status,
-                                    cudaStream_t stream);
+                                    int sm_count, cudaStream_t stream);
 
 // wino_cache_read (cache_read.cu).
 cudaError_t launch_cache_read(const wino_heads *k, const wino_heads *v, const wino_kv_batch &b, const wino_kv_scales *scales,

@@ -186,7 +186,7 @@ int wino_norm_rope_append(const wino_heads *q, const wino_heads *q_out, const wi
     if ((rc = device_info(&info)) != WINO_OK)
         return rc;
     return launch_norm_rope_append(q, q_out, k, v, *b, *rope, axes, norm, scales, static_cast<StatusWords *>(ws),
-                                   static_cast<cudaStream_t>(stream)) == cudaSuccess
+                                   info.sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? WINO_OK
                : WINO_ERR_CUDA;
 }

@@ -6,12 +6,14 @@
 // formed again of x 2^-100, so that no finite x overflows; eps >= 2^-60 covers what underflows.
 //
 // Bound by HBM where there are many rows, by latencies where there are few: every element is read and written once.  Measured
-// (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 5.0 (one chain of loads: lengths, pages, rows); 2048 rows
-// of 32 + 2 x 32 heads with three axes (101 MB) 27 (floor 15); 13481 rows of 32 + 2 x 8 heads with weights per head (331 MB) 69 (49);
-// 28931 rows into an 8-bit cache (651 MB) 142 (97).  The rest is instructions, some 230 per 16 elements of a lane, at half of the
+// (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 4.7 (one chain of loads: lengths, pages, rows); 2048 rows
+// of 32 + 2 x 32 heads with three axes (101 MB) 21 (floor 15); 13481 rows of 32 + 2 x 8 heads with weights per head (331 MB) 67 (49);
+// 28931 rows into an 8-bit cache (651 MB) 136 (97).  The rest is instructions, some 230 per 16 elements of a lane, at half of the
 // issue slots, and the look-up of a CTA's rows.  What counted: the rotation's two layouts as branches, not as selects of
-// registers (2048 rows 56 and 31), heads of one kind per warp with the next ones' loads ahead, shared weights in shared memory
-// (198 and 220 at 28931 rows, read back).  3 CTAs an SM: 4 spill (35 instead of 28 at 2048 rows), 2 take 26, but 79 instead of 69 at 13481.
+// registers (2048 rows 56 and 31), shared weights in shared memory (28931 rows, read back, 198 and 220), cosines read where they are
+// used instead of held in registers, some of which spilled (2048 rows 21 and 24, 28931 136 and 156).  3 CTAs an SM: with 4
+// registers spill (27 instead of 21, 144 instead of 136).  Rows of a CTA: the least that makes as few full waves of CTAs as there can
+// be (2048 rows: 5 in one wave 24, 4 in one and an eighth 27).
 #include <type_traits>
 
 #include "e4m3.cuh"
@@ -21,7 +23,7 @@
 namespace wino {
 namespace {
 
-constexpr int kThreads = kRopeThreads, kWarps = kThreads / 32;
+constexpr int kThreads = kRopeThreads, kWarps = kThreads / 32, kCtas = 3;  // CTAs of an SM
 
 struct NormRopeArgs {
     wino_heads q, q_out, k, v;
@@ -83,10 +85,11 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
 }
 
 // Head dims and rotations that are multiples of 16: a thread has two chunks of 8 dims of a head that hold whole pairs, and
-// the smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A warp
-// has one row and a unit of neighbouring heads of one kind at a time, so that it never branches apart.
+// the smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A unit is
+// some neighbouring heads of one kind of one row, so that a warp never branches apart; the CTA's units, row by row, are cut into
+// a run per warp, with the next unit's loads ahead, the first one's ahead of the look-up of pages and of the cosines.
 template <typename T, bool kScaled, int kAxes>
-__global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_constant__ NormRopeArgs a)
+__global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __grid_constant__ NormRopeArgs a)
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     __shared__ Rows<kAxes> sh;
@@ -101,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_c
         const uint16_t *const w = k ? a.norm.k_weight : a.norm.q_weight;
         shared_weight[k][c] = w && c < b.head_dim ? a.norm.offset + to_f<T>(w[c]) : 0.f;
     }
-    find_rows(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows);
+    const bool ok = find_sequences(b, a.rope, &a.axes, sh, row0, n_rows);
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const int turned = a.rope.rot_dim / 16, lanes = a.lanes, j = lane & (lanes - 1), of_unit = 32 / lanes, sub = lane / lanes;
     const bool live = j < b.head_dim / 16, turns = j < turned;
@@ -114,16 +117,38 @@ __global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_c
         for (int k = 0; k < 4; ++k)
             to[k] = make_float2(to_f<T>((uint16_t)w[k]), to_f<T>((uint16_t)(w[k] >> 16)));
     };
-    // a warp has a row, or a share of its heads, or two rows
-    const int share = warp / a.rows_per_cta, shares = max(1, kWarps / a.rows_per_cta);
-    for (int r = warp % a.rows_per_cta; r < n_rows; r += kWarps) {
+    const int nq = a.q.data ? b.n_q_heads : 0, nk = a.k.data ? b.n_kv_heads : 0;
+    const int q_units = (nq + of_unit - 1) / of_unit, k_units = (nk + of_unit - 1) / of_unit, units = q_units + 2 * k_units;
+    auto fetch = [&](int r, int u, uint4 &x, uint4 &y) {
+        auto load = [&](const wino_heads &from, int first, int heads) {
+            const int head = first * of_unit + sub;
+            if (live && head < heads) {
+                const uint4 *const p = reinterpret_cast<const uint4 *>(from.data + (row0 + r) * from.row_stride + head * from.head_stride);
+                x = p[c0];
+                y = p[c1];
+            }
+        };
+        x = y = make_uint4(0, 0, 0, 0);
         if (sh.seq[r] < 0)
-            continue;
-        float2 cs[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            cs[k] = turns ? sh.cs[r][8 * j + k] : make_float2(1.f, 0.f);
+            return;
+        if (u < q_units)
+            load(a.q, u, nq);
+        else if (u < q_units + k_units)
+            load(a.k, u - q_units, nk);
+        else
+            load(a.v, u - q_units - k_units, nk);
+    };
+    int i = warp * (n_rows * units) / kWarps;
+    const int end = (warp + 1) * (n_rows * units) / kWarps;
+    int r = i / units, u = i - r * units;
+    uint4 nx, ny;
+    if (i < end)
+        fetch(r, u, nx, ny);
+    find_pages(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows, ok,
+               [](int p) { return (p & 6) << 3 | (p >> 3) << 1 | (p & 1); });  // two of a lane's 8 pairs, of all lanes, then the next two
+    while (i < end) {
         const int64_t row = row0 + r, slot = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride;
+        const bool used = sh.seq[r] >= 0, stored = used && sh.page[r] >= 0;
         auto unit = [&](auto kind, int head, int heads, uint4 x, uint4 y) {
             constexpr bool kQ = decltype(kind)::value == Kind::kQ, kV = decltype(kind)::value == Kind::kV;
             const bool mine = live && head < heads;
@@ -158,6 +183,13 @@ __global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_c
                     z[k] = ptx::mul2(ptx::mul2(z[k], make_float2(by, by)), w[k]);
             }
             if (!kV && turns) {
+                float2 cs[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float4 p = reinterpret_cast<const float4 *>(sh.cs[r])[8 * k + j];
+                    cs[2 * k] = make_float2(p.x, p.y);
+                    cs[2 * k + 1] = make_float2(p.z, p.w);
+                }
                 if (a.rope.interleaved) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
@@ -207,38 +239,23 @@ __global__ void __launch_bounds__(kThreads, 3) norm_append_kernel(const __grid_c
                 }
             }
         };
-        const int nq = a.q.data ? b.n_q_heads : 0, nk = a.k.data && sh.page[r] >= 0 ? b.n_kv_heads : 0;
-        const int q_units = (nq + of_unit - 1) / of_unit, k_units = (nk + of_unit - 1) / of_unit;
-        const int units = q_units + 2 * k_units, step = shares;
-        auto fetch = [&](int u, uint4 &x, uint4 &y) {
-            auto load = [&](const wino_heads &from, int first, int heads) {
-                const int head = first * of_unit + sub;
-                if (live && head < heads) {
-                    const uint4 *const p = reinterpret_cast<const uint4 *>(from.data + row * from.row_stride + head * from.head_stride);
-                    x = p[c0];
-                    y = p[c1];
-                }
-            };
-            x = y = make_uint4(0, 0, 0, 0);
-            if (u < q_units)
-                load(a.q, u, nq);
-            else if (u < q_units + k_units)
-                load(a.k, u - q_units, nk);
-            else if (u < units)
-                load(a.v, u - q_units - k_units, nk);
-        };
-        uint4 nx, ny;
-        fetch(share, nx, ny);
-        for (int u = share; u < units; u += step) {
+        const int last = min(units, u + end - i);  // of this row
+        for (; u < last; ++u, ++i) {
             const uint4 x = nx, y = ny;
-            fetch(u + step, nx, ny);
-            if (u < q_units)
-                unit(std::integral_constant<Kind, Kind::kQ>(), u * of_unit + sub, nq, x, y);
-            else if (u < q_units + k_units)
-                unit(std::integral_constant<Kind, Kind::kK>(), (u - q_units) * of_unit + sub, nk, x, y);
-            else
-                unit(std::integral_constant<Kind, Kind::kV>(), (u - q_units - k_units) * of_unit + sub, nk, x, y);
+            if (i + 1 < end)
+                fetch(u + 1 < units ? r : r + 1, u + 1 < units ? u + 1 : 0, nx, ny);
+            if (u < q_units) {
+                if (used)
+                    unit(std::integral_constant<Kind, Kind::kQ>(), u * of_unit + sub, nq, x, y);
+            } else if (stored) {
+                if (u < q_units + k_units)
+                    unit(std::integral_constant<Kind, Kind::kK>(), (u - q_units) * of_unit + sub, nk, x, y);
+                else
+                    unit(std::integral_constant<Kind, Kind::kV>(), (u - q_units - k_units) * of_unit + sub, nk, x, y);
+            }
         }
+        u = 0;
+        ++r;
     }
 }
 
@@ -330,7 +347,7 @@ __global__ void __launch_bounds__(kThreads) norm_append_any_kernel(const __grid_
 cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out, const wino_heads *k, const wino_heads *v,
                                     const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes,
                                     const wino_head_norm *norm, const wino_kv_scales *scales, StatusWords *status,
-                                    cudaStream_t stream)
+                                    int sm_count, cudaStream_t stream)
 {
     NormRopeArgs a{};
     if (q) {
@@ -350,9 +367,13 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
     if (scales)
         a.scales = *scales;
     a.status = status;
-    // Twice the rows of the plain append where there are many: 13481 rows 71 us instead of 75, 28931 into an 8-bit cache 144 instead of
-    // 150 (of 8 at 2048 rows 30 instead of 28).
-    a.rows_per_cta = b.n_rows >= 8192 ? kMaxRowsPerCta : rope_rows_per_cta(b.n_rows);
+    // as few waves as kMaxRowsPerCta allows, and all of them full
+    const int64_t at_once = (int64_t)sm_count * kCtas;
+    a.rows_per_cta = (int32_t)((b.n_rows + at_once - 1) / at_once);
+    if (a.rows_per_cta > kMaxRowsPerCta) {
+        const int64_t waves = (b.n_rows + at_once * kMaxRowsPerCta - 1) / (at_once * kMaxRowsPerCta);
+        a.rows_per_cta = (int32_t)((b.n_rows + at_once * waves - 1) / (at_once * waves));
+    }
     a.lanes = 1;
     while (a.lanes < b.head_dim / 16)
         a.lanes *= 2;

@@ -70,7 +70,7 @@ __device__ __forceinline__ float2 turn(float a, float b, float2 c)
 // What a CTA knows of its rows.
 template <int kAxes>
 struct Rows {
-    float2 cs[kMaxRowsPerCta][kMaxPairs];
+    alignas(16) float2 cs[kMaxRowsPerCta][kMaxPairs];
     uint64_t turns[kMaxPairs];
     SeqRows q[kMaxRowsPerCta];
     int32_t seq[kMaxRowsPerCta];   // -1: a row of no sequence
@@ -79,10 +79,11 @@ struct Rows {
     uint8_t axis[kAxes > 1 ? kMaxPairs : 1];
 };
 
-// By all kRopeThreads threads.  axes: with kAxes > 1 only.  paged: the rows' pages are wanted.
+// By all kRopeThreads threads, as are the next two: the rows' sequences, and the pairs' turns.  axes: with kAxes > 1 only.
+// Returns whether this thread has seen nothing wrong.
 template <int kAxes>
-__device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
-                                          StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
+__device__ __forceinline__ bool find_sequences(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes,
+                                               Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
 {
     const int tid = (int)threadIdx.x, n_pairs = rope.rot_dim >> 1;
     if (tid < kMaxRowsPerCta)
@@ -109,6 +110,16 @@ __device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rop
         }
     }
     __syncthreads();
+    return ok;
+}
+
+// Then the rows' pages (paged: these are wanted), positions, cosines and sines.  ok: what find_sequences returned; place:
+// where in a row of cs a pair goes.
+template <int kAxes, typename Place>
+__device__ __forceinline__ void find_pages(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
+                                           StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows, bool ok, Place place)
+{
+    const int tid = (int)threadIdx.x, n_pairs = rope.rot_dim >> 1;
     if (tid < n_rows && sh.seq[tid] >= 0) {
         const SeqRows q = sh.q[tid];
         const int32_t i = row0 + tid - q.start, slot = row_slot(b, q, i), cap = b.table_width * b.page_size;
@@ -140,9 +151,17 @@ __device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rop
         const uint64_t t = sh.turns[j] * (uint64_t)(int64_t)sh.pos[r][kAxes > 1 ? sh.axis[j] : 0];
         float sn, cn;
         sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &sn, &cn);  // half-turns in [-1, 1)
-        sh.cs[r][j] = make_float2(cn * rope.factor, sn * rope.factor);
+        sh.cs[r][place(j)] = make_float2(cn * rope.factor, sn * rope.factor);
     }
     __syncthreads();
+}
+
+template <int kAxes>
+__device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
+                                          StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
+{
+    const bool ok = find_sequences(b, rope, axes, sh, row0, n_rows);
+    find_pages(b, rope, axes, paged, status, sh, row0, n_rows, ok, [](int j) { return j; });
 }
 
 // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads
