@@ -15,7 +15,7 @@
 namespace wino {
 
 constexpr int kRopeThreads = 256;
-constexpr int kMaxRowsPerCta = 16;
+constexpr int kMaxRowsPerCta = 32;
 constexpr int kMaxPairs = 64;  // head_dim / 2
 constexpr int kMaxAxes = 4;
 
