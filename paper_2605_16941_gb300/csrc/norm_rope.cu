@@ -146,7 +146,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
     if (i < end)
         fetch(r, u, nx, ny);
     find_pages(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows, ok,
-               [](int p) { return (p & 6) << 3 | (p >> 3) << 1 | (p & 1); });  // two of a lane's 8 pairs, of all lanes, then the next two
+               [](float2 *row, int p, float c, float s) {  // two of a lane's 8 pairs, cosines and then sines, of all lanes; then the next two
+                   float *const two = reinterpret_cast<float *>(row + ((p & 6) << 3 | (p >> 3) << 1)) + (p & 1);
+                   two[0] = c;
+                   two[2] = s;
+               });
     while (i < end) {
         const int64_t row = row0 + r, slot = (int64_t)sh.page[r] * b.page_stride + (int64_t)sh.in_page[r] * b.slot_stride;
         const bool used = sh.seq[r] >= 0, stored = used && sh.page[r] >= 0;
@@ -184,23 +188,25 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                     z[k] = ptx::mul2(ptx::mul2(z[k], make_float2(by, by)), w[k]);
             }
             if (!kV && turns) {
-                float2 cs[8];
+                float2 c[4], s[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float4 p = reinterpret_cast<const float4 *>(sh.cs[r])[8 * k + j];
-                    cs[2 * k] = make_float2(p.x, p.y);
-                    cs[2 * k + 1] = make_float2(p.z, p.w);
+                    c[k] = make_float2(p.x, p.y);
+                    s[k] = make_float2(p.z, p.w);
                 }
                 if (a.rope.interleaved) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        z[k] = turn(z[k].x, z[k].y, cs[k]);
+                    for (int k = 0; k < 4; ++k) {
+                        z[2 * k] = turn(z[2 * k].x, z[2 * k].y, make_float2(c[k].x, s[k].x));
+                        z[2 * k + 1] = turn(z[2 * k + 1].x, z[2 * k + 1].y, make_float2(c[k].y, s[k].y));
+                    }
                 } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 p = turn(z[k].x, z[4 + k].x, cs[2 * k]), q = turn(z[k].y, z[4 + k].y, cs[2 * k + 1]);
-                        z[k] = make_float2(p.x, q.x);
-                        z[4 + k] = make_float2(p.y, q.y);
+                    for (int k = 0; k < 4; ++k) {  // as turn, two pairs at a time
+                        const float2 p = z[k], q = z[4 + k];
+                        z[k] = ptx::fma2(p, c[k], ptx::mul2(make_float2(-q.x, -q.y), s[k]));
+                        z[4 + k] = ptx::fma2(q, c[k], ptx::mul2(p, s[k]));
                     }
                 }
             }

@@ -113,11 +113,11 @@ __device__ __forceinline__ bool find_sequences(const wino_kv_batch &b, const win
     return ok;
 }
 
-// Then the rows' pages (paged: these are wanted), positions, cosines and sines.  ok: what find_sequences returned; place:
-// where in a row of cs a pair goes.
-template <int kAxes, typename Place>
+// Then the rows' pages (paged: these are wanted), positions, cosines and sines.  ok: what find_sequences returned; put(row of cs, j,
+// c, s): stores pair j's.
+template <int kAxes, typename Put>
 __device__ __forceinline__ void find_pages(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
-                                           StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows, bool ok, Place place)
+                                           StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows, bool ok, Put put)
 {
     const int tid = (int)threadIdx.x, n_pairs = rope.rot_dim >> 1;
     if (tid < n_rows && sh.seq[tid] >= 0) {
@@ -151,7 +151,7 @@ __device__ __forceinline__ void find_pages(const wino_kv_batch &b, const wino_ro
         const uint64_t t = sh.turns[j] * (uint64_t)(int64_t)sh.pos[r][kAxes > 1 ? sh.axis[j] : 0];
         float sn, cn;
         sincospif((float)(int32_t)(t >> 32) * (1.f / 2147483648.f), &sn, &cn);  // half-turns in [-1, 1)
-        sh.cs[r][place(j)] = make_float2(cn * rope.factor, sn * rope.factor);
+        put(sh.cs[r], j, cn * rope.factor, sn * rope.factor);
     }
     __syncthreads();
 }
@@ -161,7 +161,8 @@ __device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rop
                                           StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
 {
     const bool ok = find_sequences(b, rope, axes, sh, row0, n_rows);
-    find_pages(b, rope, axes, paged, status, sh, row0, n_rows, ok, [](int j) { return j; });
+    find_pages(b, rope, axes, paged, status, sh, row0, n_rows, ok,
+               [](float2 *row, int j, float c, float s) { row[j] = make_float2(c, s); });
 }
 
 // Several rows per CTA once there are CTAs enough: the look-up of a CTA's rows is shared, and each thread has more heads
