@@ -8,8 +8,8 @@
 // Bound by HBM where there are many rows, by latencies where there are few: every element is read and written once.  Measured
 // (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 4.7 (one chain of loads: lengths, pages, rows); 2048 rows
 // of 32 + 2 x 32 heads with three axes (101 MB) 21 (floor 15); 13481 rows of 32 + 2 x 8 heads with weights per head (331 MB) 65 (49);
-// 28931 rows into an 8-bit cache (651 MB) 133 (97).  The rest is instructions, some 230 per 16 elements of a lane, at half of the
-// issue slots, and the look-up of a CTA's rows.  What counted: the rotation's two layouts as branches, not as selects of
+// 28931 rows into an 8-bit cache (651 MB) 133 (97).  The rest is instructions, some 290 per 16 elements of a lane with the look-up, at 62 % of the
+// issue slots.  What counted: the rotation's two layouts as branches, not as selects of
 // registers (2048 rows 56 and 31), shared weights in shared memory (28931 rows, read back, 198 and 220), cosines read where they are
 // used instead of held in registers, some of which spilled (2048 rows 21 and 24, 28931 136 and 156).  3 CTAs an SM: with 4
 // registers spill (27 instead of 21, 144 instead of 136; both with 16 rows of a CTA at most).  Rows of a CTA: the
