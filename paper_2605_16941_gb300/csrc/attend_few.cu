@@ -20,9 +20,11 @@
 // lie anywhere.
 //
 // Measured (us, replayed; floors from 6.7 TB/s): 64 tokens over 500 to 32767 slots, 32 heads over 8 kv heads of 128 (821 MB)
-// 166 (floor 122); one over 262144 slots (541 MB) 96 (80); one over 300 slots 9.1.  In the second a warp needs 4200 clocks for 32 slots
-// (29 bytes a clock and SM, 23 at the floor), 240 of them waiting for codes; in the first a part's start and end
-// take 6 us each of its 40.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads
+// 154 (floor 122; 143 with pages of 64 slots instead of 16); 64 over 16383 slots each 334 (321); one over 262144 slots (541 MB) 97 (80);
+// one over 300 slots 9.1.  In the middle of a part a warp needs 4200 clocks for 32 slots, 29 bytes a clock and SM, with 23 at the
+// floor; a part's start and end cost as much as 8 slot tiles, by which the work is cut: with 3 as for
+// attend_kernel.cuh 166, with 11 158.  The next part's copies ahead of the join, or the planning warp joining in the
+// background, gain nothing that the cut does not, and cost short calls 0.3 us; two CTAs of 7 warps an SM 109 for the one long token.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads
 // ran at 13 bytes a clock and SM, whatever was in flight.  11 warps of 168 registers instead of 15 of 128: 210 and 140 against 223 and
 // 143 with cp.async.
 #include <cuda_bf16.h>
@@ -672,11 +674,11 @@ namespace attend {
 static double few_units(const wino_kv_batch &b)
 {
     const int32_t positions = kFewRows / (b.n_q_heads / b.n_kv_heads);
-    return (double)b.n_seq * (b.n_rows / positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kTaskCost);
+    return (double)b.n_seq * (b.n_rows / positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kFewTaskCost);
 }
 
 // A tile of rows per sequence and kv head, on average. This kernel and wino_attend's over tiles of the element type (us): 64 tokens
-// of 4 heads to a kv head over up to 32767 slots 166 and 330, one over 262144 96 and about 180, one over 300 9.1 and 13. Two tiles each read
+// of 4 heads to a kv head over up to 32767 slots 154 and 330, one over 262144 96 and about 180, one over 300 9.1 and 13. Two tiles each read
 // K and V: 4 tokens a sequence, with other lengths, 502 and 579, 184 and 180, 9.7 and 13.3, and 349 and 343 with 64 dims. These are
 // left to the other one, whose results are the bits of wino_attend over the values.
 bool few_rows(const wino_kv_batch &b)

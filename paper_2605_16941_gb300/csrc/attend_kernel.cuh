@@ -85,6 +85,7 @@ constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kLevels = 8;              // of the tree over the parts of a task: 2^8 >= kMaxCtas
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
 constexpr int kTaskCost = 3;            // what a task costs beside its slot tiles, in slot tiles
+constexpr int kFewTaskCost = 8;         // and one of few rows, whose tiles take less (attend_few.cu)
 constexpr int kSnap = 2;                // a cut this near to a task's border (in slot tiles) is moved there
 constexpr float kRescaleBits[2] = {6.f, 8.f};  // fp16, bf16
 constexpr float kTopBits[2] = {9.9f, 0.f};     // the P of a score of m is 2^this
@@ -188,9 +189,9 @@ struct Cut {
     }
     // A start inside the task [t0, t1), moved to the task's border where that is near: joining parts costs more than it
     // evens out.
-    static __device__ __forceinline__ U snap(U unit, U t0, U t1)
+    static __device__ __forceinline__ U snap(U unit, U t0, U t1, int32_t cost)
     {
-        return unit < t0 + kTaskCost + kSnap ? t0 : (t1 < unit + kSnap ? t1 : unit);
+        return unit < t0 + cost + kSnap ? t0 : (t1 < unit + kSnap ? t1 : unit);
     }
 };
 
@@ -327,6 +328,7 @@ __device__ __forceinline__ U warp_scan(U x, int lane)  // inclusive
 template <typename U, typename S, int kMostTiles = 2>
 __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
 {
+    constexpr int kCost = kMostTiles == 1 ? kFewTaskCost : kTaskCost;
     const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads;
     bool ok = true;
     int width = 32;  // lanes per sequence
@@ -350,7 +352,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
         n_tasks = q.n > 0 ? tasks_of(a, q, row_tiles) : 0;
 #pragma unroll 1
         for (int32_t x = sub; x < n_tasks; x += width)
-            share += (U)(tiles_of(task_slots(a, q, row_tiles, x)) + kTaskCost);
+            share += (U)(tiles_of(task_slots(a, q, row_tiles, x)) + kCost);
         mine = warp_sum(share, width);
     };
     U total, tasks;
@@ -428,7 +430,7 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
 #pragma unroll 1
         for (int32_t p0 = 0; p0 < n_tasks && n_tasks > 1; p0 += 32) {
             const int32_t p = p0 + lane;
-            const U cost = p < n_tasks ? (U)(tiles_of(task_slots(a, q, row_tiles, p)) + kTaskCost) * heads : (U)0;
+            const U cost = p < n_tasks ? (U)(tiles_of(task_slots(a, q, row_tiles, p)) + kCost) * heads : (U)0;
             const U pre = warp_scan(cost, lane);
             const unsigned hit = __ballot_sync(0xffffffffu, task + pre > at);
             if (hit) {
@@ -439,11 +441,11 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
             }
             task += __shfl_sync(0xffffffffu, pre, 31);
         }
-        const U cost = (U)(tiles_of(task_slots(a, q, row_tiles, index)) + kTaskCost);
+        const U cost = (U)(tiles_of(task_slots(a, q, row_tiles, index)) + kCost);
         if (by_index)
             to_head(cost);
         // a start that moves to the task's end belongs to the next one, which the walk below finds
-        at = Cut<U>::snap(at, task, task + cost);
+        at = Cut<U>::snap(at, task, task + cost, kCost);
     }
 #pragma unroll 1
     while (true) {
@@ -452,8 +454,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
         part.kv_end = part.j0 = part.n = part.i0 = part.first = part.last = 0;
         if (go) {
             const int32_t slots = task_slots(a, q, row_tiles, index), tiles = tiles_of(slots);
-            const U tile0 = task + kTaskCost, next = tile0 + (U)tiles;  // a task's own cost comes before its tiles
-            const U stop = end >= next ? next : Cut<U>::snap(end, task, next);
+            const U tile0 = task + kCost, next = tile0 + (U)tiles;  // a task's own cost comes before its tiles
+            const U stop = end >= next ? next : Cut<U>::snap(end, task, next, kCost);
             part.j0 = at > tile0 ? (int32_t)(at - tile0) : 0;
             part.n = (stop > tile0 ? (int32_t)(stop - tile0) : 0) - part.j0;
             part.kv_end = slots;
