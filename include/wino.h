@@ -505,9 +505,9 @@ WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale
  * so that a value keeps 4 significant bits unless it is below 2^-13.8 of its row's
  * largest or below 2^(e_min - 6), values beyond +-57344 are held as that, and every
  * value read is exact in the element type.  A row with an infinity or NaN is
- * held as s = 255 and reads as NaN throughout.  The codes 0x7f and 0xff and the
- * scales from 135 to 254 are not written, and must not be in slots that some
- * row sees.
+ * held as s = 255 and reads as NaN throughout.  The codes 0x7f and 0xff, scales
+ * from 135 to 254 and, but over codes of 0, scales below e_min + 127 are not
+ * written, and must not be in slots that some row sees.
  * wino_norm_rope_append writes such a cache, wino_cache_read takes rows out of
  * it, wino_attend_scaled attends over it; wino_rope_append and wino_attend
  * refuse it with WINO_ERR_ARG.

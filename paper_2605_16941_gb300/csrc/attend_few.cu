@@ -24,9 +24,10 @@
 // one over 300 slots 9.1.  In the middle of a part a warp needs 4200 clocks for 32 slots, 29 bytes a clock and SM, with 23 at the
 // floor; a part's start and end cost as much as 8 slot tiles, by which the work is cut: with 3 as for
 // attend_kernel.cuh 166, with 11 158.  The next part's copies ahead of the join, or the planning warp joining in the
-// background, gain nothing that the cut does not, and cost short calls 0.3 us; two CTAs of 7 warps an SM 109 for the one long token.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads
-// ran at 13 bytes a clock and SM, whatever was in flight.  11 warps of 168 registers instead of 15 of 128: 210 and 140 against 223 and
-// 143 with cp.async.
+// background, gain nothing that the cut does not, and cost short calls 0.3 us; two CTAs of 7 warps an SM 109 for the one long
+// token.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads ran at 13 bytes
+// a clock and SM, whatever was in flight.  11 warps of 168 registers instead of 15 of 128: 210 and 140 against 223 and 143 with
+// cp.async.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -217,3 +217,20 @@ def test_far_offsets():
     c.table_dev.copy_(torch.from_numpy(c.table))
     run(add_rows(rebatch(c)))
     assert whole.numel() > 1 << 32
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Calls that overlap on the GPU over one cache: each as alone."""
+    calls = [add_rows(make_kv8(CAUSAL, [(1, 30001 + i, 30000 + i), (1, 500, 499)], heads=8, kv_heads=2, dim=128, page=64, seed=i)) for i in range(2)]
+    alone = []
+    for c in calls:
+        attend8(c)
+        alone.append(c.out.clone())
+    spaces, streams = [wino.attend_workspace(c.batch) for c in calls], [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, ws, stream in zip(calls, spaces, streams):
+            wino.wino_attend_scaled(c.q, c.out, c.batch, ws, stream=stream)
+    torch.cuda.synchronize()
+    for c, ws, want in zip(calls, spaces, alone):
+        assert wino.wino_read_device_status(ws) == wino.WINO_OK and torch.equal(c.out, want)

@@ -221,6 +221,13 @@ def test_dims_of_8(dim):
 
 
 @pytest.mark.parametrize("scaled", [False, True], ids=["plain", "e4m3"])
+@pytest.mark.parametrize("rows", [456, 457, 913, 7000, 14592, 14593])
+def test_rows_around_full_waves(rows, scaled):
+    """From one row of a CTA to as many as there can be, and to two waves of half as many; in two sequences that meet inside a CTA."""
+    run(CAUSAL, [(rows - 300, rows - 300, 0), (300, 300, 0)], heads=2, kv_heads=1, dim=16, page=64, scaled=scaled)
+
+
+@pytest.mark.parametrize("scaled", [False, True], ids=["plain", "e4m3"])
 @pytest.mark.parametrize("dim", [128, 96])
 def test_in_place(dim, scaled):
     run(CAUSAL, [(40, 40, 0)], in_place=True, gap=1, heads=3, kv_heads=3, dim=dim, scaled=scaled)
