@@ -569,11 +569,12 @@ WINO_API int wino_cache_read(const wino_heads *k, const wino_heads *v, const win
  * wino_attend over an 8-bit cache: the same rows, masks, arguments, workspace
  * and errors, K and V the values that codes and scales stand for.  The result is
  * that of wino_attend over a cache of the element type that holds these values:
- * bit for bit, unless n_rows is at most n_seq * floor(8 / G) with G <= 8 query
- * heads to a kv head (single tokens).  Those have a kernel of their own, with
- * weights in fp16 whatever the element type (those below 2^-23 of a row's largest
- * to steps of 2^-33 of it, V's scales included in both).  Codes and scales in slots
- * that no row of the sequence sees have no effect.
+ * bit for bit, unless the rows are few (single tokens): with g the largest divisor
+ * of the G query heads to a kv head up to 8, G / g <= 2 and n_rows <= n_seq *
+ * floor(8 / g).  Those have a kernel of their own, with weights in fp16 whatever
+ * the element type (those below 2^-23 of a row's largest to steps of 2^-33 of it,
+ * V's scales included in both).  Codes and scales in slots that no row of the
+ * sequence sees have no effect.
  */
 WINO_API int wino_attend_scaled(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b,
                                 const wino_kv_scales *scales, void *ws, size_t ws_bytes, void *stream);

@@ -80,6 +80,7 @@ int attend_args(const wino_heads &q, const wino_heads &out, float scale, const w
     a.piece = L.piece;
     a.group = b.n_q_heads / b.n_kv_heads;
     a.positions = positions_per_tile(b);
+    a.split = 1;
     a.box_rows = std::min(b.page_size, kTileN);
     a.boxes = kTileN / a.box_rows;
     for (int i = 0; i < 2; ++i) {

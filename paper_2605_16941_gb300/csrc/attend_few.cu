@@ -1,7 +1,7 @@
 // attend_few.cu -- wino_attend_scaled for sequences of few rows (single tokens).
 //
 // out = softmax(scale Q K^T) V as in attend_kernel.cuh, whose planning warp cuts the work here too.  Up to 8 rows times heads of
-// a kv head are a tile, the 8 columns of mma.m16n8k16: S^T = K Q^T and O^T = V^T P^T, with K and V as the A operand.  The stream of
+// a kv head, or half of its heads, are a tile, the 8 columns of mma.m16n8k16: S^T = K Q^T and O^T = V^T P^T, with K and V as the A operand.  The stream of
 // codes bounds this: a token's products would fill a few of the 128 rows that tcgen05 takes, and its operands would have to go
 // through shared memory as values of the element type (attend_kernel.cuh, 64 tokens: 330 us).
 //
@@ -230,6 +230,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
             // ---- the part's slots, 32 at a time; pages and scales a turn ahead of the codes, codes a turn ahead of their use
             const int32_t end = min(part.kv_end, (part.j0 + part.n) * kTileN);
             const int32_t *const table = b.page_table + (int64_t)part.seq * b.table_width;
+            const int32_t kv_head = part.kv_head >> (a.split - 1);
             int32_t at = part.j0 * kTileN + warp * kChunk;
             constexpr int32_t kStep = kWorkers * kChunk;
             // of a slot behind the last one: the last one's, which nothing reads
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                 box_bytes = (lane == 0 || (lane == 16 && boxes > 1)) ? a.box_rows * DP : 0;
                 scales[0] = scales[1] = 0;
                 if (there && lane < left) {
-                    const int64_t scale = scale_at(b, page, in_page + (lane & 15), part.kv_head);
+                    const int64_t scale = scale_at(b, page, in_page + (lane & 15), kv_head);
                     scales[0] = a.scales.k_scale[scale];
                     scales[1] = a.scales.v_scale[scale];
                 }
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                     ptx::mbar_arrive_expect_tx(bar, (uint32_t)(box_bytes + second));
                 __syncwarp();
                 if (box_bytes)
-                    ptx::tma_load_4d(to + (uint32_t)(lane ? 16 * DP : 0), map, bar, 0, box_slot, part.kv_head, box_page);
+                    ptx::tma_load_4d(to + (uint32_t)(lane ? 16 * DP : 0), map, bar, 0, box_slot, kv_head, box_page);
                 __syncwarp();
             };
             auto next_unit = [&]() -> const uint8_t * {  // waits for it
@@ -671,21 +672,38 @@ int launch_few(const CUtensorMap &tk, const CUtensorMap &tv, const AttendArgs &a
 
 namespace attend {
 
-// The units that a batch may have at most in tasks of one tile, as attend_units counts them.
-static double few_units(const wino_kv_batch &b)
+namespace {
+
+// How the query heads of a kv head go into tiles: the most that divide them, up to kFewRows.
+int32_t few_group(const wino_kv_batch &b)
 {
-    const int32_t positions = kFewRows / (b.n_q_heads / b.n_kv_heads);
-    return (double)b.n_seq * (b.n_rows / positions + 1) * b.n_kv_heads * ((double)b.table_width * b.page_size / kTileN + 1 + kFewTaskCost);
+    const int32_t heads = b.n_q_heads / b.n_kv_heads;
+    int32_t group = std::min(heads, kFewRows);
+    while (heads % group != 0)
+        --group;
+    return group;
 }
 
-// A tile of rows per sequence and kv head, on average. This kernel and wino_attend's over tiles of the element type (us): 64 tokens
-// of 4 heads to a kv head over up to 32767 slots 154 and 330, one over 262144 96 and about 180, one over 300 9.1 and 13. Two tiles each read
-// K and V: 4 tokens a sequence, with other lengths, 502 and 579, 184 and 180, 9.7 and 13.3, and 349 and 343 with 64 dims. These are
-// left to the other one, whose results are the bits of wino_attend over the values.
+// The units that a batch may have at most in tasks of one tile, as attend_units counts them.
+double few_units(const wino_kv_batch &b)
+{
+    const int32_t group = few_group(b), positions = kFewRows / group;
+    return (double)b.n_seq * (b.n_rows / positions + 1) * (b.n_q_heads / group) *
+           ((double)b.table_width * b.page_size / kTileN + 1 + kFewTaskCost);
+}
+
+}  // namespace
+
+// A tile of rows per sequence and kv head on average, or two where the heads of one row need them: each tile reads K and V, the
+// second mostly from the L2 cache. This kernel and wino_attend's over tiles of the element type (us), heads of 128: 64 tokens of 4
+// heads to a kv head over up to 32767 slots 154 and 330, one over 262144 97 and about 180, one over 300 9.1 and 13; 64 of 16 heads
+// to a kv head over up to 16000 142 and 174, of 32 (four tiles) 134 and 107. Two tiles of rows gain less and would lose
+// the bits of wino_attend over the values: 64 sequences of 4 rows over up to 16000 252 and 279, one over 262144 171 and 181.
 bool few_rows(const wino_kv_batch &b)
 {
-    const int32_t group = b.n_q_heads / b.n_kv_heads;
-    return group <= kFewRows && b.n_rows <= (int64_t)b.n_seq * (kFewRows / group) && few_units(b) < 4611686018427387904.0;
+    const int32_t group = few_group(b);
+    return b.n_q_heads / b.n_kv_heads <= 2 * group && b.n_rows <= (int64_t)b.n_seq * (kFewRows / group) &&
+           few_units(b) < 4611686018427387904.0;
 }
 
 int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
@@ -699,6 +717,8 @@ int launch_few(AttendArgs a, int ctas, cudaStream_t stream)
     if ((rc = encode_codes(&tk, b.k_cache, b, width, a.box_rows, true)) != WINO_OK ||
         (rc = encode_codes(&tv, b.v_cache, b, width, a.box_rows, true)) != WINO_OK)
         return rc;
+    a.group = few_group(b);
+    a.split = b.n_q_heads / b.n_kv_heads / a.group;
     a.positions = kFewRows / a.group;
     for (int i = 0; i < 2; ++i) {
         const uint64_t w = (uint64_t)(i + 1) * a.positions;

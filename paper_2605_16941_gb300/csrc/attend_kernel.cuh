@@ -111,6 +111,7 @@ struct AttendArgs {
     float4 *part_o;   // [kMaxCtas][2][2 quarters][piece / 4][32 lanes]
     int32_t quarters, piece;   // warps of a warpgroup with rows at most, columns that a warp keeps at most
     int32_t group, positions;  // query heads per kv head, row positions per tile
+    int32_t split;             // 2: a task has half of a kv head's query heads (`group`), and each half counts as a kv head in Part
     uint32_t magic[2];         // ceil(2^32 / w) for tasks of w = positions and of 2 positions
     int32_t box_rows, boxes;   // slots per copy (a page, or 128 of one), copies per slot tile and 64 dims
     int32_t min_units;         // a CTA's run is at least this long
@@ -329,7 +330,7 @@ template <typename U, typename S, int kMostTiles = 2>
 __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
 {
     constexpr int kCost = kMostTiles == 1 ? kFewTaskCost : kTaskCost;
-    const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads;
+    const int32_t n_seq = a.b.n_seq, n_kv = a.b.n_kv_heads * a.split;
     bool ok = true;
     int width = 32;  // lanes per sequence
     while (width > 1 && n_seq * width > 32)

@@ -25,6 +25,14 @@ def test_groups(dim, group, dtype):
     run(add_rows(make_kv8(CAUSAL, [(1, n, n - 1) for n in (1, 33, 700)], heads=2 * group, kv_heads=2, dim=dim, dtype=dtype)))
 
 
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("group", [9, 10, 11, 12, 14, 16, 32])
+def test_groups_of_more_than_a_tile(group, dtype):
+    """Heads of a kv head in two tiles where 5, 6, 7 or 8 divide them; the others beside them."""
+    for mask, seqs in ((CAUSAL, [(1, n, n - 1) for n in (1, 33, 700)]), (SHADOW, [(2, 90, 89), (0, 9, 0), (0, 9, 0), (2, 33, 0)])):
+        run(add_rows(make_kv8(mask, seqs, heads=3 * group, kv_heads=3, dim=128, dtype=dtype, layout="heads")))
+
+
 @pytest.mark.parametrize("dim", [16, 32, 48, 80, 96, 112])
 @pytest.mark.parametrize("layout", ["slots", "heads"])
 def test_dims(dim, layout):
