@@ -427,6 +427,7 @@ def make_kv_batch(k_cache, v_cache, page_table, q_start, q_len, kv_len, new_slot
     b.scales = scales
     # plain attributes: what the calls compare with, cheaper than the struct's fields
     b.q_shape, b.kv_shape = (n_rows, n_q_heads, head_dim), (n_rows, n_kv_heads, head_dim)
+    b.q_weights, b.k_weights = ((None, (head_dim,), (h, head_dim)) for h in (n_q_heads, n_kv_heads))  # of norms
     b.elements, b.device = elements, k_cache.get_device()
     b.devices = {b.device}
     return b
@@ -476,7 +477,7 @@ def make_head_norm(q_weight, k_weight, *, eps: float = 1e-6, offset: float = 0.0
     n.tensors = (q_weight, k_weight)
     n.devices = {w.get_device() for w in given}
     n.elements = given[0].dtype if given else None
-    n.shapes = tuple(None if w is None else tuple(w.shape) for w in (q_weight, k_weight))
+    n.shapes = n.q_shape, n.k_shape = tuple(None if w is None else tuple(w.shape) for w in (q_weight, k_weight))
     return n
 
 
@@ -544,9 +545,8 @@ def wino_norm_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, no
         if axes.device != batch.device:
             raise WinoError(WINO_ERR_ARG, where)
     if norm is not None:
-        for shape, want in zip(norm.shapes, (batch.q_shape, batch.kv_shape)):
-            if shape is not None and shape != want[2:] and shape != want[1:]:
-                raise WinoError(WINO_ERR_SHAPE, where)
+        if norm.q_shape not in batch.q_weights or norm.k_shape not in batch.k_weights:
+            raise WinoError(WINO_ERR_SHAPE, where)
         if not norm.devices <= batch.devices or norm.elements not in (None, batch.elements):
             raise WinoError(WINO_ERR_ARG, where)
     _check(lib().wino_norm_rope_append(*heads, batch, rope, axes, norm, batch.scales, _ptr(ws), _stream(stream)), where)
