@@ -35,7 +35,7 @@ struct NormRopeArgs {
     wino_kv_scales scales;
     StatusWords *status;
     int32_t rows_per_cta;
-    int32_t lanes;  // per head: the smallest power of two that is no less than head_dim / 16
+    int32_t lanes;  // per head: the smallest power of two that covers it with 16 (kWhole) or 8 dims each
 };
 
 // 1 / sqrt(mean(x^2) + eps) of a head whose values `lanes` neighbouring lanes hold (others zero), by all lanes of the warp; x is
@@ -85,15 +85,19 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
     return r;
 }
 
-// Head dims and rotations that are multiples of 16: a thread has two chunks of 8 dims of a head that hold whole pairs, and
-// the smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A unit is
+// kWhole (head dims and rotations that are multiples of 16): a thread has two chunks of 8 dims of a head that hold whole pairs.
+// Else it has one, whose partners it finds in shared memory where halves turn. 12000 rows of 32 + 2 x 8 heads of 128 dims, 58 of them
+// turned, 114 us into an 8-bit cache; of 80 dims, 40 turned, 116, and 93 as neighbours; 13481 rows that turn whole 65.
+// The smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A unit is
 // some neighbouring heads of one kind of one row, so that a warp never branches apart; the CTA's units, row by row, are cut into
 // a run per warp, with the next unit's loads ahead, the first one's ahead of the look-up of pages and of the cosines.
-template <typename T, bool kScaled, int kAxes>
+template <typename T, bool kScaled, int kAxes, bool kWhole>
 __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __grid_constant__ NormRopeArgs a)
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+    constexpr int kPairs = kWhole ? 8 : 4;  // of neighbours, that a thread has
     __shared__ Rows<kAxes> sh;
+    __shared__ float beside[kWhole ? 1 : kWarps][8][32];  // not kWhole: dims 8 j + e of a warp's heads, by e and lane
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
@@ -107,10 +111,10 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
     }
     const bool ok = find_sequences(b, a.rope, &a.axes, sh, row0, n_rows);
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int turned = a.rope.rot_dim / 16, lanes = a.lanes, j = lane & (lanes - 1), of_unit = 32 / lanes, sub = lane / lanes;
-    const bool live = j < b.head_dim / 16, turns = j < turned;
+    const int n_pairs = a.rope.rot_dim >> 1, turned = a.rope.rot_dim / 16, lanes = a.lanes, j = lane & (lanes - 1), of_unit = 32 / lanes, sub = lane / lanes;
+    const bool live = j < b.head_dim / (2 * kPairs), turns = kWhole ? j < turned : n_pairs > 0;
     // the item's chunks: halves j and j + turned, or neighbours
-    const int c0 = turns && !a.rope.interleaved ? j : 2 * j, c1 = turns && !a.rope.interleaved ? j + turned : 2 * j + 1;
+    const int c0 = !kWhole || (turns && !a.rope.interleaved) ? j : 2 * j, c1 = turns && !a.rope.interleaved ? j + turned : 2 * j + 1;
     const float inv_dim = 1.f / (float)b.head_dim;
     auto unpack = [&](const uint4 &v, float2 *to) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -126,7 +130,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
             if (live && head < heads) {
                 const uint4 *const p = reinterpret_cast<const uint4 *>(from.data + (row0 + r) * from.row_stride + head * from.head_stride);
                 x = p[c0];
-                y = p[c1];
+                if (kWhole)
+                    y = p[c1];
             }
         };
         x = y = make_uint4(0, 0, 0, 0);
@@ -146,7 +151,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
     if (i < end)
         fetch(r, u, nx, ny);
     find_pages(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows, ok,
-               [](float2 *row, int p, float c, float s) {  // two of a lane's 8 pairs, cosines and then sines, of all lanes; then the next two
+               [](float2 *row, int p, float c, float s) {
+                   if (!kWhole) {
+                       row[(p & 7) << 3 | p >> 3] = make_float2(c, s);  // neighbouring lanes' side by side
+                       return;
+                   }
+                   // two of a lane's 8 pairs, cosines and then sines, of all lanes; then the next two
                    float *const two = reinterpret_cast<float *>(row + ((p & 6) << 3 | (p >> 3) << 1)) + (p & 1);
                    two[0] = c;
                    two[2] = s;
@@ -157,57 +167,96 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
         auto unit = [&](auto kind, int head, int heads, uint4 x, uint4 y) {
             constexpr bool kQ = decltype(kind)::value == Kind::kQ, kV = decltype(kind)::value == Kind::kV;
             const bool mine = live && head < heads;
-            float2 z[8];  // the first chunk's pairs of neighbours, then the second's
+            float2 z[kPairs];  // the first chunk's pairs of neighbours, then the second's
             unpack(x, z);
-            unpack(y, z + 4);
+            if constexpr (kWhole)
+                unpack(y, z + 4);
             const uint16_t *const weight = kQ ? a.norm.q_weight : a.norm.k_weight;
             if (!kV && weight) {
                 const float by = inverse_rms(z, lanes, inv_dim, a.norm.eps);
                 const int64_t stride = kQ ? a.norm.q_head_stride : a.norm.k_head_stride;
-                float2 w[8];
+                float2 w[kPairs];
                 if (stride == 0) {
                     const float4 *const f = reinterpret_cast<const float4 *>(shared_weight[kQ ? 0 : 1]);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float4 p = f[2 * c0 + k], q = f[2 * c1 + k];
+                        const float4 p = f[2 * c0 + k];
                         w[2 * k] = make_float2(p.x, p.y);
                         w[2 * k + 1] = make_float2(p.z, p.w);
-                        w[4 + 2 * k] = make_float2(q.x, q.y);
-                        w[4 + 2 * k + 1] = make_float2(q.z, q.w);
+                        if constexpr (kWhole) {
+                            const float4 q = f[2 * c1 + k];
+                            w[4 + 2 * k] = make_float2(q.x, q.y);
+                            w[4 + 2 * k + 1] = make_float2(q.z, q.w);
+                        }
                     }
                 } else {
                     const uint4 *const p = reinterpret_cast<const uint4 *>(weight + min(head, heads - 1) * stride);
                     unpack(p[live ? c0 : 0], w);
-                    unpack(p[live ? c1 : 0], w + 4);
+                    if constexpr (kWhole)
+                        unpack(p[live ? c1 : 0], w + 4);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
+                    for (int k = 0; k < kPairs; ++k)
                         w[k] = ptx::add2(w[k], make_float2(a.norm.offset, a.norm.offset));
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < kPairs; ++k)
                     z[k] = ptx::mul2(ptx::mul2(z[k], make_float2(by, by)), w[k]);
             }
-            if (!kV && turns) {
-                float2 c[4], s[4];
+            if constexpr (kWhole) {
+                if (!kV && turns) {
+                    float2 c[4], s[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float4 p = reinterpret_cast<const float4 *>(sh.cs[r])[8 * k + j];
-                    c[k] = make_float2(p.x, p.y);
-                    s[k] = make_float2(p.z, p.w);
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 p = reinterpret_cast<const float4 *>(sh.cs[r])[8 * k + j];
+                        c[k] = make_float2(p.x, p.y);
+                        s[k] = make_float2(p.z, p.w);
+                    }
+                    if (a.rope.interleaved) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            z[2 * k] = turn(z[2 * k].x, z[2 * k].y, make_float2(c[k].x, s[k].x));
+                            z[2 * k + 1] = turn(z[2 * k + 1].x, z[2 * k + 1].y, make_float2(c[k].y, s[k].y));
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {  // as turn, two pairs at a time
+                            const float2 p = z[k], q = z[4 + k];
+                            z[k] = ptx::fma2(p, c[k], ptx::mul2(make_float2(-q.x, -q.y), s[k]));
+                            z[4 + k] = ptx::fma2(q, c[k], ptx::mul2(p, s[k]));
+                        }
+                    }
                 }
+            } else if (!kV && turns) {
+                const float2 *const cs = sh.cs[r];
                 if (a.rope.interleaved) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        z[2 * k] = turn(z[2 * k].x, z[2 * k].y, make_float2(c[k].x, s[k].x));
-                        z[2 * k + 1] = turn(z[2 * k + 1].x, z[2 * k + 1].y, make_float2(c[k].y, s[k].y));
+                        const int p = 4 * j + k;
+                        if (p < n_pairs)
+                            z[k] = turn(z[k].x, z[k].y, cs[(p & 7) << 3 | p >> 3]);
                     }
                 } else {
+                    float(&mine_beside)[8][32] = beside[warp];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {  // as turn, two pairs at a time
-                        const float2 p = z[k], q = z[4 + k];
-                        z[k] = ptx::fma2(p, c[k], ptx::mul2(make_float2(-q.x, -q.y), s[k]));
-                        z[4 + k] = ptx::fma2(q, c[k], ptx::mul2(p, s[k]));
+                    for (int k = 0; k < 4; ++k) {
+                        mine_beside[2 * k][lane] = z[k].x;
+                        mine_beside[2 * k + 1][lane] = z[k].y;
                     }
+                    __syncwarp();
+                    auto turned_dim = [&](int e, float x) {  // as turn
+                        const int i = 8 * j + e;
+                        const bool second = i >= n_pairs;
+                        const int p = second ? i - n_pairs : i, other = second ? p : i + n_pairs;
+                        if (p >= n_pairs)
+                            return x;
+                        const float2 c = cs[(p & 7) << 3 | p >> 3];
+                        const float y = mine_beside[other & 7][lane - j + (other >> 3)];
+                        return fmaf(x, c.x, y * (second ? c.y : -c.y));
+                    };
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        z[k] = make_float2(turned_dim(2 * k, z[k].x), turned_dim(2 * k + 1, z[k].y));
+                    __syncwarp();
                 }
             }
             if (kQ || !kScaled) {
@@ -219,12 +268,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                 };
                 if (mine) {
                     reinterpret_cast<uint4 *>(dst)[c0] = pack(z);
-                    reinterpret_cast<uint4 *>(dst)[c1] = pack(z + 4);
+                    if constexpr (kWhole)
+                        reinterpret_cast<uint4 *>(dst)[c1] = pack(z + 4);
                 }
             } else {
                 uint32_t most = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < kPairs; ++k)
                     most = max(most, max(__float_as_uint(z[k].x) & 0x7fffffffu, __float_as_uint(z[k].y) & 0x7fffffffu));
                 for (int i = lanes >> 1; i; i >>= 1)
                     most = max(most, __shfl_xor_sync(0xffffffffu, most, i));
@@ -240,7 +290,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                     uint2 *const dst = reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(kV ? b.v_cache : b.k_cache) + slot +
                                                                  head * b.head_stride);
                     dst[c0] = codes(z);
-                    dst[c1] = codes(z + 4);
+                    if constexpr (kWhole)
+                        dst[c1] = codes(z + 4);
                     if (j == 0)
                         (kV ? a.scales.v_scale : a.scales.k_scale)[scale_at(b, sh.page[r], sh.in_page[r], head)] = (uint8_t)s;
                 }
@@ -263,90 +314,6 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
         }
         u = 0;
         ++r;
-    }
-}
-
-// Any dims: a warp per head, whose lane l has the dims l, l + 32, l + 64 and l + 96.  Where both can do it 64 rows take 9.4 us
-// instead of 4.7, 13481 338 instead of 66.
-template <typename T, bool kScaled, int kAxes>
-__global__ void __launch_bounds__(kThreads) norm_append_any_kernel(const __grid_constant__ NormRopeArgs a)
-{
-    constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
-    __shared__ Rows<kAxes> sh;
-    __shared__ float head[kWarps][128];
-    const wino_kv_batch &b = a.b;
-    const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
-    const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, D = b.head_dim;
-    ptx::grid_dep_launch_dependents();
-    ptx::grid_dep_wait();
-    find_rows(b, a.rope, &a.axes, a.k.data != nullptr, a.status, sh, row0, n_rows);
-    const int n_pairs = a.rope.rot_dim >> 1, nq = a.q.data ? b.n_q_heads : 0;
-    const int heads = nq + (a.k.data ? 2 * b.n_kv_heads : 0);
-    for (int u = warp; u < n_rows * heads; u += kWarps) {
-        const int r = u / heads, h = u - r * heads;
-        if (sh.seq[r] < 0 || (h >= nq && sh.page[r] < 0))
-            continue;
-        const bool is_q = h < nq, is_v = h >= nq + b.n_kv_heads;
-        const int hk = is_q ? h : (is_v ? h - nq - b.n_kv_heads : h - nq);
-        const wino_heads &from = is_q ? a.q : (is_v ? a.v : a.k);
-        const uint16_t *const src = from.data + (int64_t)(row0 + r) * from.row_stride + hk * from.head_stride;
-        auto dim = [&](int k) { return lane + 32 * k < D ? to_f<T>(src[lane + 32 * k]) : 0.f; };
-        float2 pairs[2] = {make_float2(dim(0), dim(1)), make_float2(dim(2), dim(3))};
-        const uint16_t *const weight = is_q ? a.norm.q_weight : a.norm.k_weight;
-        const float by = !is_v && weight ? inverse_rms(pairs, 32, 1.f / (float)D, a.norm.eps) : 1.f;
-        float x[4] = {pairs[0].x, pairs[0].y, pairs[1].x, pairs[1].y};
-        if (!is_v && weight) {
-            const uint16_t *const w = weight + hk * (is_q ? a.norm.q_head_stride : a.norm.k_head_stride);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (lane + 32 * k < D)
-                    x[k] = x[k] * by * (a.norm.offset + to_f<T>(w[lane + 32 * k]));
-        }
-        if (!is_v && n_pairs) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                head[warp][lane + 32 * k] = x[k];
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int c = lane + 32 * k;
-                if (c < 2 * n_pairs) {
-                    const bool second = a.rope.interleaved ? (c & 1) != 0 : c >= n_pairs;
-                    const int j = a.rope.interleaved ? c >> 1 : (second ? c - n_pairs : c);
-                    const int other = a.rope.interleaved ? c ^ 1 : (second ? j : c + n_pairs);
-                    const float y = head[warp][other];
-                    const float2 p = second ? turn(y, x[k], sh.cs[r][j]) : turn(x[k], y, sh.cs[r][j]);
-                    x[k] = second ? p.y : p.x;
-                }
-            }
-            __syncwarp();
-        }
-        if (is_q || !kScaled) {
-            uint16_t *const dst = is_q ? a.q_out.data + (int64_t)(row0 + r) * a.q_out.row_stride + hk * a.q_out.head_stride
-                                       : (is_v ? b.v_cache : b.k_cache) + (int64_t)sh.page[r] * b.page_stride +
-                                             (int64_t)sh.in_page[r] * b.slot_stride + hk * b.head_stride;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (lane + 32 * k < D)
-                    dst[lane + 32 * k] = from_f<T>(x[k]);
-        } else {
-            uint32_t most = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                most = max(most, __float_as_uint(x[k]) & 0x7fffffffu);
-            most = __reduce_max_sync(0xffffffffu, most);
-            const uint32_t s = scale_byte<kBf16>(most);
-            const float f = code_factor(s);
-            uint8_t *const dst = reinterpret_cast<uint8_t *>(is_v ? b.v_cache : b.k_cache) + (int64_t)sh.page[r] * b.page_stride +
-                                 (int64_t)sh.in_page[r] * b.slot_stride + hk * b.head_stride;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (lane + 32 * k < D)
-                    dst[lane + 32 * k] = s == kScaleNan ? (uint8_t)0 : (uint8_t)codes2(x[k] * f, 0.f);
-            if (lane == 0)
-                (is_v ? a.scales.v_scale : a.scales.k_scale)[scale_at(b, sh.page[r], sh.in_page[r], hk)] = (uint8_t)s;
-        }
     }
 }
 
@@ -382,8 +349,9 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
         const int64_t waves = (b.n_rows + at_once * kMaxRowsPerCta - 1) / (at_once * kMaxRowsPerCta);
         a.rows_per_cta = (int32_t)((b.n_rows + at_once * waves - 1) / (at_once * waves));
     }
+    const bool whole = b.head_dim % 16 == 0 && rope.rot_dim % 16 == 0;
     a.lanes = 1;
-    while (a.lanes < b.head_dim / 16)
+    while (a.lanes < b.head_dim / (whole ? 16 : 8))
         a.lanes *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((b.n_rows + a.rows_per_cta - 1) / a.rows_per_cta));
@@ -398,9 +366,9 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
     auto of_type = [&](auto type, auto scaled) {
         using T = decltype(type);
         constexpr bool kScaled = decltype(scaled)::value;
-        if (b.head_dim % 16 == 0 && rope.rot_dim % 16 == 0)
-            return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes>) : launch(norm_append_kernel<T, kScaled, 1>);
-        return axes ? launch(norm_append_any_kernel<T, kScaled, kMaxAxes>) : launch(norm_append_any_kernel<T, kScaled, 1>);
+        if (whole)
+            return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes, true>) : launch(norm_append_kernel<T, kScaled, 1, true>);
+        return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes, false>) : launch(norm_append_kernel<T, kScaled, 1, false>);
     };
     if ((b.dtype & ~WINO_CACHE_E4M3) == WINO_BF16)
         return scales ? of_type(__nv_bfloat16(), std::true_type()) : of_type(__nv_bfloat16(), std::false_type());
