@@ -364,7 +364,8 @@ WINO_API int wino_decode(const uint16_t *W, int64_t d, int64_t V, int32_t *token
  * Values: whatever the cache holds in slots that no row of the sequence sees
  * (behind kv_len, in pages that are not the sequence's) has no effect, not
  * even as NaN or infinity.  A slot that some rows see and others do not has
- * to hold finite values, or those others may become NaN too.
+ * to hold finite values, or those others may become NaN too (in an 8-bit cache
+ * they do not, see wino_kv_scales).
  *
  * The lengths, slots and pages are read on the device when the call runs, so a
  * captured call may be replayed with new ones.  What cannot be checked before
@@ -505,7 +506,8 @@ WINO_API int wino_attend(const wino_heads *q, const wino_heads *out, float scale
  * so that a value keeps 4 significant bits unless it is below 2^-13.8 of its row's
  * largest or below 2^(e_min - 6), values beyond +-57344 are held as that, and every
  * value read is exact in the element type.  A row with an infinity or NaN is
- * held as s = 255 and reads as NaN throughout.  The codes 0x7f and 0xff, scales
+ * held as s = 255 and codes of 0 and reads as NaN throughout: rows of a call that
+ * see it get NaN from that kv head, and those that do not nothing.  The codes 0x7f and 0xff, scales
  * from 135 to 254 and, but over codes of 0, scales below e_min + 127 are not
  * written, and must not be in slots that some row sees.
  * wino_norm_rope_append writes such a cache, wino_cache_read takes rows out of
@@ -568,7 +570,8 @@ WINO_API int wino_cache_read(const wino_heads *k, const wino_heads *v, const win
 /*
  * wino_attend over an 8-bit cache: the same rows, masks, arguments, workspace
  * and errors, K and V the values that codes and scales stand for.  The result is
- * that of wino_attend over a cache of the element type that holds these values:
+ * that of wino_attend over a cache of the element type that holds these values
+ * (without the NaNs that rows may get there from slots that they do not see):
  * bit for bit, unless the rows are few (single tokens): with g the largest divisor
  * of the G query heads to a kv head up to 8, G / g <= 2 and n_rows <= n_seq *
  * floor(8 / g).  Those have a kernel of their own, with weights in fp16 whatever

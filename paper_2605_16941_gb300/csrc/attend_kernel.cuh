@@ -37,7 +37,8 @@
 //
 // An 8-bit cache (kScaled).  Two warps copy the codes of a slot tile and their scales into stages, one of K and one of V (two each
 // with 64 dims), and four warps more write them as the tiles of the element type that TMA would have brought, swizzled, into one ring
-// for both in the order of their use; from there on all is as above, and so are the results.  Few rows have a kernel of their own
+// for both in the order of their use; from there on all is as above, and so are the results.  Rows that are held as NaN become
+// something finite (0 times NaN is not 0), and the sums of the rows that see them NaN.  Few rows have a kernel of their own
 // (attend_few.cu).  What bounds it: those four warps, some 1600 clocks a tile in bf16 and 1170
 // in fp16 (804 and 581 of conversion by themselves, the rest reads of shared memory and waits, with one such warp to a
 // scheduler), K's and V's one after the other: 4 x 512 rows of 32 heads over 8-bit caches of 1605 to 3890 slots 69 us, 57 over 16-bit ones.
@@ -81,6 +82,7 @@ constexpr int kSoftmaxThreads = 256;
 constexpr int kWarpK = 8, kWarpMma = 9, kWarpV = 10, kWarpPlan = 11, kWarpDecode = 12;  // the last: the first of four
 template <bool kScaled>
 constexpr int kAttendThreads = kSoftmaxThreads + (kScaled ? 256 : 128);
+constexpr int32_t kNoSlot = 1 << 30;    // behind every slot
 constexpr int kMaxCtas = 160;           // an SM each
 constexpr int kLevels = 8;              // of the tree over the parts of a task: 2^8 >= kMaxCtas
 constexpr int kParts = 4;               // parts of tasks that the planning warp may be ahead
@@ -247,6 +249,9 @@ struct alignas(16) Shared {
     int32_t abort;
     float2 ml[2][kTileM];
     alignas(16) uint8_t scale[kAll][kScaled ? kStageN : 16];
+    // Of a part, by converting warp: the first two of its slots whose K or V is held as NaN, kNoSlot behind them.  Two, since a
+    // row sees all slots before its limit but one.
+    int2 nan[kScaled ? kParts : 1][4];
 };
 
 template <bool kBf16>
@@ -902,6 +907,17 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 if (!warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort))
                     break;
                 ptx::tc_fence_after();
+                if constexpr (kScaled) {
+                    // what was noted of this warpgroup's slot tiles is there, of the other's maybe
+                    const int2 *const nan = sh.nan[reader.slot()];
+                    if (__builtin_expect(min(min(nan[0].x, nan[1].x), min(nan[2].x, nan[3].x)) != kNoSlot, 0) && valid) {
+                        const RowSees sees = row_sees(a.b, part.q, i);
+#pragma unroll 1
+                        for (int k = 0; k < 4; ++k)
+                            if ((nan[k].x < sees.lim && nan[k].x != sees.hole) || (nan[k].y < sees.lim && nan[k].y != sees.hole))
+                                l = NAN;
+                    }
+                }
             }
             // Columns [c0, c1) of O, as f0 O_0 + f1 O_1 where two warpgroups join.
             float f0 = 1.f, f1 = 0.f;
@@ -1333,9 +1349,12 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
             // Tiles in the order in which the MMAs take them: the first scores' K, then K and V in turn, then the last V.
             const int32_t n = part.n, lead = min(n, (part.flags & kTwo) != 0 ? 1 : 2);
             const int32_t slots = part.kv_end - part.j0 * kTileN;  // from the part's first on
+            int2 &noted = sh.nan[reader.slot()][warp & 3];
+            if (lane == 0)
+                noted = make_int2(kNoSlot, kNoSlot);
             __syncwarp();
             if (lane == 0)
-                done_with();
+                done_with();  // the softmax warps hold the part until its last tile has been used
             ++reader.count;
             bool good = true;
             int32_t next_k = 0, next_v = 0;
@@ -1352,6 +1371,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 // their number xor r % 8.
                 uint8_t *const to = smem_raw + (slot_addr(tile) - raw) + (chunk >> 2) * kHalfBytes;
                 const uint8_t *const codes = smem_raw + kStage0 + (uint32_t)stage * C::kStageBytes;
+                uint32_t most = 0;  // of the scales
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half, left -= kHalfN) {
                     uint4 c[kTurns];
@@ -1372,7 +1392,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
 #pragma unroll
                     for (int k = 0; k < kTurns; ++k) {
                         const int r = half * kHalfN + of_warp + k * kAtOnce;
-                        const uint32_t factor = read_factor<kBf16>(f[k]);
+                        const uint32_t factor = finite_factor<kBf16>(f[k]);
                         uint4 lo, hi;
                         decode4<kBf16>(c[k].x, factor, lo.x, lo.y);
                         decode4<kBf16>(c[k].y, factor, lo.z, lo.w);
@@ -1381,6 +1401,18 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                         const int at = ((chunk & 3) * 2) ^ (r & 7);
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at ^ 1 : at) * 16) = swap ? hi : lo;
                         *reinterpret_cast<uint4 *>(to + r * 128 + (swap ? at : at ^ 1) * 16) = swap ? lo : hi;
+                    }
+#pragma unroll
+                    for (int k = 0; k < kTurns; ++k)
+                        most = max(most, f[k]);
+                }
+                if (__builtin_expect(__any_sync(0xffffffffu, most == kScaleNan), 0)) {
+#pragma unroll 1
+                    for (int k = 0; k < 32; ++k) {  // the warp's 16 slots of each half
+                        const int r = (k >> 4) * kHalfN + (warp & 3) * 16 + (k & 15);
+                        const int32_t rest = left + kTileN, slot = part.kv_end - rest + r;
+                        if (lane == 0 && r < rest && sh.scale[stage][r] == kScaleNan && slot != noted.x)
+                            noted = slot < noted.x ? make_int2(slot, noted.x) : make_int2(noted.x, min(noted.y, slot));
                     }
                 }
                 ptx::fence_proxy_async();

@@ -55,6 +55,15 @@ __device__ __forceinline__ uint32_t read_factor(uint32_t scale)
     return f | f << 16;
 }
 
+// The same, but of rows that are held as NaN something finite.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t finite_factor(uint32_t scale)
+{
+    const uint32_t e = min(scale, (uint32_t)(kScaleBias + kMaxScaleExp));
+    const uint32_t f = kBf16 ? (e + 120u) << 7 : (uint32_t)(max((int)e, kScaleBias + kMinScaleExp<kBf16>) - kScaleBias + 15) << 10;
+    return f | f << 16;
+}
+
 // The values of four codes (lowest byte first) as pairs of the element type.
 template <bool kBf16>
 __device__ __forceinline__ void decode4(uint32_t codes, uint32_t factor, uint32_t &lo, uint32_t &hi)
