@@ -367,7 +367,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
                         t[x][k] = ptx::mul2(ptx::add2(t[x][k], make_float2(-base.x, -base.y)), make_float2(sl2, sl2));
                 const uint8_t *const v_unit = next_unit();
                 const uint32_t nan = __ballot_sync(0xffffffffu, k_scale == kScaleNan || v_scale == kScaleNan);
-                const int exponent = v_scale == kScaleNan ? 0 : (int)v_scale - kScaleBias;
+                // Slots that were not written, zeros at any scale, count as of the least exponent: c is then no less, and 2^c normal.
+                constexpr int kLeast = kScaleBias + kMinScaleExp<__is_same(T, __nv_bfloat16)>;
+                const int exponent = v_scale == kScaleNan ? 0 : max((int)v_scale, kLeast) - kScaleBias;
                 // Weights 2^(t + e - c + kWeightTop) of slots with V's exponent e, c no less than any t + e: the largest e so far where
                 // the slots' are alike, else the largest t + e itself, so that weights far below 1 do not leave fp16.
                 const int most = __reduce_max_sync(0xffffffffu, here + lane < end ? exponent : -1000);
@@ -614,13 +616,13 @@ __global__ void __launch_bounds__(kFewThreads, 1)
             if (whole && mine && dim < b.head_dim) {
                 const int pos = row / a.group, i = part.i0 + pos;
                 if (pos < a.positions && i < part.q.n) {
-                    // no slot seen: zeros; NaN stays NaN
-                    const float by = sum == 0.f ? 0.f : ptx::ex2(top - kWeightTop) / sum;
+                    // No slot seen: zeros; NaN stays NaN.  2^c last: with 1 / l it would leave fp32's range for V near 2^-110.
+                    const float by = sum == 0.f ? 0.f : 1.f / sum, up = ptx::ex2(top - kWeightTop);
                     uint16_t *const dst = a.out.data + (int64_t)(part.q.start + i) * a.out.row_stride +
                                           (int64_t)(part.kv_head * a.group + row - pos * a.group) * a.out.head_stride;
                     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
                     *reinterpret_cast<uint2 *>(dst + dim) =
-                        make_uint2(pack2<kBf16>(y.x * by, y.y * by), pack2<kBf16>(y.z * by, y.w * by));
+                        make_uint2(pack2<kBf16>(y.x * by * up, y.y * by * up), pack2<kBf16>(y.z * by * up, y.w * by * up));
                 }
             }
         }
