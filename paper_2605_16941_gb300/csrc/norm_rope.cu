@@ -86,15 +86,18 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
 }
 
 // kWhole (head dims and rotations that are multiples of 16): a thread has two chunks of 8 dims of a head that hold whole pairs.
-// Else it has one, whose partners it finds in shared memory where halves turn. 12000 rows of 32 + 2 x 8 heads of 128 dims, 58 of them
-// turned, 114 us into an 8-bit cache; of 80 dims, 40 turned, 116, and 93 as neighbours; 13481 rows that turn whole 65.
+// Else it has one, whose partners it finds in shared memory where halves turn: 12000 rows of 32 + 2 x 8 heads of 80 dims, 40 of them
+// turned (184 MB), 107 us, and 86 as neighbours; of 128 dims, 58 turned, into an 8-bit cache (270 MB), 113.  Whole, 13481 rows of 128
+// dims (331 MB) take 64.
 // The smallest power of two of lanes that covers a head works on it, so that sums and maxima take shuffles alone.  A unit is
 // some neighbouring heads of one kind of one row, so that a warp never branches apart; the CTA's units, row by row, are cut into
 // a run per warp, with the next unit's loads ahead, the first one's ahead of the look-up of pages and of the cosines.
-template <typename T, bool kScaled, int kAxes, bool kWhole>
+// kPlain: no norms, no axes, no codes; the results are wino_rope_append's, bit for bit.
+template <typename T, bool kScaled, int kAxes, bool kWhole, bool kPlain = false>
 __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __grid_constant__ NormRopeArgs a)
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+    static_assert(!kPlain || (!kScaled && kAxes == 1 && !kWhole), "the others are wino_rope_append's own");
     constexpr int kPairs = kWhole ? 8 : 4;  // of neighbours, that a thread has
     __shared__ Rows<kAxes> sh;
     __shared__ float beside[kWhole ? 1 : kWarps][8][32];  // not kWhole: dims 8 j + e of a warp's heads, by e and lane
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
             if constexpr (kWhole)
                 unpack(y, z + 4);
             const uint16_t *const weight = kQ ? a.norm.q_weight : a.norm.k_weight;
-            if (!kV && weight) {
+            if (!kPlain && !kV && weight) {
                 const float by = inverse_rms(z, lanes, inv_dim, a.norm.eps);
                 const int64_t stride = kQ ? a.norm.q_head_stride : a.norm.k_head_stride;
                 float2 w[kPairs];
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                     for (int k = 0; k < 4; ++k) {
                         const int p = 4 * j + k;
                         if (p < n_pairs)
-                            z[k] = turn(z[k].x, z[k].y, cs[(p & 7) << 3 | p >> 3]);
+                            z[k] = turn<kPlain && kBf16>(z[k].x, z[k].y, cs[(p & 7) << 3 | p >> 3]);
                     }
                 } else {
                     float(&mine_beside)[8][32] = beside[warp];
@@ -251,6 +254,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                             return x;
                         const float2 c = cs[(p & 7) << 3 | p >> 3];
                         const float y = mine_beside[other & 7][lane - j + (other >> 3)];
+                        if (kPlain && kBf16 && second)
+                            return fmaf(y, c.y, x * c.x);
                         return fmaf(x, c.x, y * (second ? c.y : -c.y));
                     };
 #pragma unroll
@@ -266,10 +271,21 @@ __global__ void __launch_bounds__(kThreads, kCtas) norm_append_kernel(const __gr
                     return make_uint4(pack_pair<T>(v[0].x, v[0].y), pack_pair<T>(v[1].x, v[1].y), pack_pair<T>(v[2].x, v[2].y),
                                       pack_pair<T>(v[3].x, v[3].y));
                 };
-                if (mine) {
-                    reinterpret_cast<uint4 *>(dst)[c0] = pack(z);
+                if constexpr (!kV) {  // V is stored as it came, NaNs and all
+                    const uint4 as_was = x;
+                    x = pack(z);
                     if constexpr (kWhole)
-                        reinterpret_cast<uint4 *>(dst)[c1] = pack(z + 4);
+                        y = pack(z + 4);
+                    if (kPlain) {  // and so are the dims that do not turn
+                        const int turned_dims = a.rope.rot_dim - 8 * j;  // of the chunk
+                        x = make_uint4(turned_dims > 0 ? x.x : as_was.x, turned_dims > 2 ? x.y : as_was.y,
+                                       turned_dims > 4 ? x.z : as_was.z, turned_dims > 6 ? x.w : as_was.w);
+                    }
+                }
+                if (mine) {
+                    reinterpret_cast<uint4 *>(dst)[c0] = x;
+                    if constexpr (kWhole)
+                        reinterpret_cast<uint4 *>(dst)[c1] = y;
                 }
             } else {
                 uint32_t most = 0;
@@ -324,6 +340,9 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
                                     const wino_head_norm *norm, const wino_kv_scales *scales, StatusWords *status,
                                     int sm_count, cudaStream_t stream)
 {
+    const bool plain = !axes && !scales && (!norm || (!norm->q_weight && !norm->k_weight));
+    if (plain && rope.rot_dim % 8 == 0)  // 2048 rows of 32 + 2 x 32 heads 16.0 us, by the kernel here 19.0; of 80 dims, 40 turned, 44 and 108
+        return launch_rope_append(q, q_out, k, v, b, rope, status, stream);
     NormRopeArgs a{};
     if (q) {
         a.q = *q;
@@ -366,6 +385,9 @@ cudaError_t launch_norm_rope_append(const wino_heads *q, const wino_heads *q_out
     auto of_type = [&](auto type, auto scaled) {
         using T = decltype(type);
         constexpr bool kScaled = decltype(scaled)::value;
+        if constexpr (!kScaled)
+            if (plain)  // pair by pair there: 12000 rows of 80 dims, 20 turned, 211
+                return launch(norm_append_kernel<T, false, 1, false, true>);
         if (whole)
             return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes, true>) : launch(norm_append_kernel<T, kScaled, 1, true>);
         return axes ? launch(norm_append_kernel<T, kScaled, kMaxAxes, false>) : launch(norm_append_kernel<T, kScaled, 1, false>);

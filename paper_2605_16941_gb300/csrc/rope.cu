@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_any_kernel(const RopeArg
         if (u < n_pairs) {
             const int i0 = a.rope.interleaved ? 2 * u : u, i1 = a.rope.interleaved ? 2 * u + 1 : u + n_pairs;
             if (rotate) {
-                const float2 p = turn(to_f<T>(src[i0]), to_f<T>(src[i1]), sh.cs[r][u]);
+                const float2 p = turn<__is_same(T, __nv_bfloat16)>(to_f<T>(src[i0]), to_f<T>(src[i1]), sh.cs[r][u]);
                 dst[i0] = from_f<T>(p.x);
                 dst[i1] = from_f<T>(p.y);
             } else {

@@ -61,10 +61,12 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
     return (uint32_t)from_f<T>(lo) | (uint32_t)from_f<T>(hi) << 16;
 }
 
-// a' and b' of one pair.
+// a' and b' of one pair.  The products' rounding is written out, so that all kernels agree to the bit; kOther: b' with the other of
+// its products rounded, as the pair by pair rotation of bf16 has it.
+template <bool kOther = false>
 __device__ __forceinline__ float2 turn(float a, float b, float2 c)
 {
-    return make_float2(a * c.x - b * c.y, b * c.x + a * c.y);
+    return make_float2(fmaf(a, c.x, -(b * c.y)), kOther ? fmaf(a, c.y, b * c.x) : fmaf(b, c.x, a * c.y));
 }
 
 // What a CTA knows of its rows.
