@@ -518,8 +518,8 @@ typedef struct {
     uint8_t *k_scale, *v_scale; /* device [n_pages, n_kv_heads, page_size], 16-byte aligned */
 } wino_kv_scales;
 
-/* Norms of queries and keys: each head x of a row becomes x (offset + weight) / sqrt(mean(x^2) + eps), in fp32 and not
-   rounded before the rotation. */
+/* Norms of queries and keys: each head x of a row becomes x (offset + weight) / sqrt(mean(x^2) + eps), in fp32 (whose
+   subnormal numbers count as zeros) and not rounded before the rotation. */
 typedef struct {
     const uint16_t *q_weight, *k_weight; /* device, element type, 16-byte aligned, [head_dim] per head; NULL: q (or k) is not normalised */
     int64_t q_head_stride, k_head_stride; /* elements from one head's weights to the next: 0 (all heads share them) or a

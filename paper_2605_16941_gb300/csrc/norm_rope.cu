@@ -3,7 +3,8 @@
 //
 // y = x (offset + w) / sqrt(mean(x^2) + eps) for a head x, then for each pair of its first rot_dim dims
 // a' = m (a cos t - b sin t), b' = m (b cos t + a sin t), all in fp32; then one rounding.  Sums of squares beyond 2^100 are
-// formed again of x 2^-100, so that no finite x overflows; eps >= 2^-60 covers what underflows.
+// formed again of x 2^-100, so that no finite x overflows; eps >= 2^-60 covers what underflows.  Subnormal numbers count as
+// zeros.
 //
 // Bound by HBM where there are many rows, by latencies where there are few: every element is read and written once.  Measured
 // (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 4.7 (one chain of loads: lengths, pages, rows); 2048 rows
@@ -38,38 +39,40 @@ struct NormRopeArgs {
     int32_t lanes;  // per head: the smallest power of two that covers it with 16 (kWhole) or 8 dims each
 };
 
-// 1 / sqrt(mean(x^2) + eps) of a head whose values `lanes` neighbouring lanes hold (others zero), by all lanes of the warp; x is
-// scaled by 2^-100 first, here and in the result, where its squares come too close to fp32's limits.
+// 1 / sqrt(mean(x^2) + eps) of a head whose values `lanes` neighbouring lanes hold (others zero), by all lanes of the warp.  Where
+// the squares come too close to fp32's limits they are formed of x 2^-100, and x becomes x 2^-30 and the result 2^30 times as
+// large: both and their products with elements of any size are then normal numbers, if the quotient is.
 template <int kN>
 __device__ __forceinline__ float inverse_rms(float2 (&x)[kN], int lanes, float inv_dim, float eps)
 {
-    auto squares = [&]() {
+    auto squares = [&](float by) {
         float2 p = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < kN; ++k)
-            p = ptx::fma2(x[k], x[k], p);
+        for (int k = 0; k < kN; ++k) {
+            const float2 y = by == 1.f ? x[k] : ptx::mul2(x[k], make_float2(by, by));
+            p = ptx::fma2(y, y, p);
+        }
         float s = p.x + p.y;
         for (int i = lanes >> 1; i; i >>= 1)
             s += __shfl_xor_sync(0xffffffffu, s, i);
         return s;
     };
-    float s = squares();
+    float s = squares(1.f), back = 1.f;
     const bool large = !(s < 0x1p100f);
     if (__any_sync(0xffffffffu, large)) {
+        const float again = squares(0x1p-100f);
         if (large) {
 #pragma unroll
             for (int k = 0; k < kN; ++k)
-                x[k] = make_float2(x[k].x * 0x1p-100f, x[k].y * 0x1p-100f);
-        }
-        const float again = squares();
-        if (large) {
+                x[k] = ptx::mul2(x[k], make_float2(0x1p-30f, 0x1p-30f));
             s = again;
             eps = 0.f;  // times 2^-200
+            back = 0x1p-70f;
         }
     }
     // a Newton step: the root's own error, 2^-22, would move a code's border more than the rest of the arithmetic does
     const float x2 = s * inv_dim + eps, r = rsqrtf(x2);
-    return x2 < 0x1p127f ? r * fmaf(-0.5f * x2 * r, r, 1.5f) : r;  // infinite elements leave 0 of the finite ones
+    return (x2 < 0x1p127f ? r * fmaf(-0.5f * x2 * r, r, 1.5f) : r) * back;  // infinite elements leave 0 of the finite ones
 }
 
 enum class Kind { kQ, kK, kV };
