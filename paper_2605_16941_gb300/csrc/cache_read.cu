@@ -25,7 +25,7 @@ struct ReadArgs {
 template <bool kScaled, bool kBf16>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ ReadArgs a)
 {
-    __shared__ Rows<1> sh;
+    __shared__ Rows<1, kFewRowsPerCta, 0> sh;
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);

@@ -44,7 +44,7 @@ struct Chunk<2> {
 template <typename T, int kWords>
 __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs a)
 {
-    __shared__ Rows<1> sh;
+    __shared__ Rows<1, kFewRowsPerCta> sh;
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_append_kernel(const RopeArgs
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_append_any_kernel(const RopeArgs a)
 {
-    __shared__ Rows<1> sh;
+    __shared__ Rows<1, kFewRowsPerCta> sh;
     const wino_kv_batch &b = a.b;
     const int32_t row0 = (int32_t)blockIdx.x * a.rows_per_cta;
     const int32_t n_rows = min(a.rows_per_cta, b.n_rows - row0);

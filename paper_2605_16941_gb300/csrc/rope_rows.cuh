@@ -15,7 +15,8 @@
 namespace wino {
 
 constexpr int kRopeThreads = 256;
-constexpr int kMaxRowsPerCta = 32;
+constexpr int kMaxRowsPerCta = 32;  // of any kernel
+constexpr int kFewRowsPerCta = 8;   // of those that go by rope_rows_per_cta
 constexpr int kMaxPairs = 64;  // head_dim / 2
 constexpr int kMaxAxes = 4;
 
@@ -69,26 +70,28 @@ __device__ __forceinline__ float2 turn(float a, float b, float2 c)
     return make_float2(fmaf(a, c.x, -(b * c.y)), kOther ? fmaf(a, c.y, b * c.x) : fmaf(b, c.x, a * c.y));
 }
 
-// What a CTA knows of its rows.
-template <int kAxes>
+// What a CTA knows of its rows, kRows at most, of which kPairs pairs may turn (0: none does).
+template <int kAxes, int kRows = kMaxRowsPerCta, int kPairs = kMaxPairs>
 struct Rows {
-    alignas(16) float2 cs[kMaxRowsPerCta][kMaxPairs];
-    uint64_t turns[kMaxPairs];
-    SeqRows q[kMaxRowsPerCta];
-    int32_t seq[kMaxRowsPerCta];   // -1: a row of no sequence
-    int32_t page[kMaxRowsPerCta];  // -1: not stored
-    int32_t in_page[kMaxRowsPerCta], pos[kMaxRowsPerCta][kAxes];
-    uint8_t axis[kAxes > 1 ? kMaxPairs : 1];
+    static constexpr int kMost = kRows, kOfAxes = kAxes;
+    alignas(16) float2 cs[kRows][kPairs ? kPairs : 1];
+    uint64_t turns[kPairs ? kPairs : 1];
+    SeqRows q[kRows];
+    int32_t seq[kRows];   // -1: a row of no sequence
+    int32_t page[kRows];  // -1: not stored
+    int32_t in_page[kRows], pos[kRows][kAxes];
+    uint8_t axis[kAxes > 1 ? kPairs : 1];
 };
 
 // By all kRopeThreads threads, as are the next two: the rows' sequences, and the pairs' turns.  axes: with kAxes > 1 only.
 // Returns whether this thread has seen nothing wrong.
-template <int kAxes>
+template <typename R>
 __device__ __forceinline__ bool find_sequences(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes,
-                                               Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
+                                               R &sh, int32_t row0, int32_t n_rows)
 {
+    constexpr int kAxes = R::kOfAxes;
     const int tid = (int)threadIdx.x, n_pairs = rope.rot_dim >> 1;
-    if (tid < kMaxRowsPerCta)
+    if (tid < R::kMost)
         sh.seq[tid] = -1;
     __syncthreads();
     bool ok = true;
@@ -117,10 +120,11 @@ __device__ __forceinline__ bool find_sequences(const wino_kv_batch &b, const win
 
 // Then the rows' pages (paged: these are wanted), positions, cosines and sines.  ok: what find_sequences returned; put(row of cs, j,
 // c, s): stores pair j's.
-template <int kAxes, typename Put>
+template <typename R, typename Put>
 __device__ __forceinline__ void find_pages(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
-                                           StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows, bool ok, Put put)
+                                           StatusWords *status, R &sh, int32_t row0, int32_t n_rows, bool ok, Put put)
 {
+    constexpr int kAxes = R::kOfAxes;
     const int tid = (int)threadIdx.x, n_pairs = rope.rot_dim >> 1;
     if (tid < n_rows && sh.seq[tid] >= 0) {
         const SeqRows q = sh.q[tid];
@@ -158,9 +162,9 @@ __device__ __forceinline__ void find_pages(const wino_kv_batch &b, const wino_ro
     __syncthreads();
 }
 
-template <int kAxes>
+template <typename R>
 __device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rope &rope, const wino_rope_axes *axes, bool paged,
-                                          StatusWords *status, Rows<kAxes> &sh, int32_t row0, int32_t n_rows)
+                                          StatusWords *status, R &sh, int32_t row0, int32_t n_rows)
 {
     const bool ok = find_sequences(b, rope, axes, sh, row0, n_rows);
     find_pages(b, rope, axes, paged, status, sh, row0, n_rows, ok,
@@ -173,7 +177,7 @@ __device__ __forceinline__ void find_rows(const wino_kv_batch &b, const wino_rop
 // 32 + 2 x 8 heads 90.5 and 83.6).
 inline int32_t rope_rows_per_cta(int32_t n_rows)
 {
-    return n_rows >= 8192 ? 8 : (n_rows >= 1024 ? 4 : (n_rows >= 512 ? 2 : 1));
+    return n_rows >= 8192 ? kFewRowsPerCta : (n_rows >= 1024 ? 4 : (n_rows >= 512 ? 2 : 1));
 }
 
 }  // namespace wino
