@@ -517,10 +517,10 @@ def _append_args(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, q_out, where: 
         vh = _heads(v, batch, batch.kv_shape, where)
     if rope.n_positions not in (None, batch.q_shape[0]):
         raise WinoError(WINO_ERR_SHAPE, where)
-    if _nbytes(ws) < STATUS_BYTES:
+    if ws.numel() * ws.element_size() < STATUS_BYTES:
         raise WinoError(WINO_ERR_WORKSPACE, where)
     # the kernels run on the current device; wino_rope_frequencies' values are on the host
-    if not rope.devices <= batch.devices or batch.device != _current_device() or ws.get_device() != batch.device:
+    if not rope.devices <= batch.devices or not batch.device == _current_device() == ws.get_device():
         raise WinoError(WINO_ERR_ARG, where)
     return qh, qo, kh, vh
 
@@ -529,8 +529,10 @@ def wino_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, q_out=N
     """Rotate the rows' queries (into ``q_out``, or in place) and write their rotated keys and their values into the
     batch's cache.  ``q`` None: the cache alone; ``k`` and ``v`` None: the queries alone."""
     where = "wino_rope_append"
-    heads = _append_args(q, k, v, batch, rope, ws, q_out, where)
-    _check(lib().wino_rope_append(*heads, batch, rope, _ptr(ws), _stream(stream)), where)
+    qh, qo, kh, vh = _append_args(q, k, v, batch, rope, ws, q_out, where)
+    status = lib().wino_rope_append(qh, qo, kh, vh, batch, rope, ws.data_ptr(), _stream(stream))
+    if status != WINO_OK:
+        raise WinoError(status, where)
 
 
 def wino_norm_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, norm: WinoHeadNorm | None = None,
@@ -538,7 +540,7 @@ def wino_norm_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, no
     """``wino_rope_append`` with per-head norms of queries and keys (``norm``), positions of several axes (``axes``, with a
     ``rope`` without positions), and into an 8-bit cache where ``batch`` has one."""
     where = "wino_norm_rope_append"
-    heads = _append_args(q, k, v, batch, rope, ws, q_out, where)
+    qh, qo, kh, vh = _append_args(q, k, v, batch, rope, ws, q_out, where)
     if axes is not None:
         if axes.n_positions != batch.q_shape[0] or axes.n_pairs != rope.rot_dim // 2:
             raise WinoError(WINO_ERR_SHAPE, where)
@@ -549,7 +551,9 @@ def wino_norm_rope_append(q, k, v, batch: WinoKvBatch, rope: WinoRope, ws, *, no
             raise WinoError(WINO_ERR_SHAPE, where)
         if not norm.devices <= batch.devices or norm.elements not in (None, batch.elements):
             raise WinoError(WINO_ERR_ARG, where)
-    _check(lib().wino_norm_rope_append(*heads, batch, rope, axes, norm, batch.scales, _ptr(ws), _stream(stream)), where)
+    status = lib().wino_norm_rope_append(qh, qo, kh, vh, batch, rope, axes, norm, batch.scales, ws.data_ptr(), _stream(stream))
+    if status != WINO_OK:
+        raise WinoError(status, where)
 
 
 def wino_cache_read(k, v, batch: WinoKvBatch, ws, *, stream=None) -> None:
@@ -558,11 +562,13 @@ def wino_cache_read(k, v, batch: WinoKvBatch, ws, *, stream=None) -> None:
     where = "wino_cache_read"
     kh = None if k is None else _heads(k, batch, batch.kv_shape, where)
     vh = None if v is None else _heads(v, batch, batch.kv_shape, where)
-    if _nbytes(ws) < STATUS_BYTES:
+    if ws.numel() * ws.element_size() < STATUS_BYTES:
         raise WinoError(WINO_ERR_WORKSPACE, where)
-    if batch.device != _current_device() or ws.get_device() != batch.device:
+    if not batch.device == _current_device() == ws.get_device():
         raise WinoError(WINO_ERR_ARG, where)
-    _check(lib().wino_cache_read(kh, vh, batch, batch.scales, _ptr(ws), _stream(stream)), where)
+    status = lib().wino_cache_read(kh, vh, batch, batch.scales, ws.data_ptr(), _stream(stream))
+    if status != WINO_OK:
+        raise WinoError(status, where)
 
 
 def wino_attend_workspace_size(batch: WinoKvBatch) -> int:
@@ -585,7 +591,7 @@ def append_workspace(device=None):
 
 def _attend_args(q, out, batch: WinoKvBatch, ws, scale, where: str):
     qh, oh = _heads(q, batch, batch.q_shape, where), _heads(out, batch, batch.q_shape, where)
-    if batch.device != _current_device() or ws.get_device() != batch.device:  # the kernels run on the current device
+    if not batch.device == _current_device() == ws.get_device():  # the kernels run on the current device
         raise WinoError(WINO_ERR_ARG, where)
     return qh, oh, batch.q_shape[2] ** -0.5 if scale is None else scale
 
@@ -594,14 +600,18 @@ def wino_attend(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, s
     """Attention of the batch's rows over its cache, into ``out``; ``scale`` defaults to head_dim^-1/2."""
     where = "wino_attend"
     qh, oh, scale = _attend_args(q, out, batch, ws, scale, where)
-    _check(lib().wino_attend(qh, oh, scale, batch, _ptr(ws), _nbytes(ws), _stream(stream)), where)
+    status = lib().wino_attend(qh, oh, scale, batch, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream))
+    if status != WINO_OK:
+        raise WinoError(status, where)
 
 
 def wino_attend_scaled(q, out, batch: WinoKvBatch, ws, *, scale: float | None = None, stream=None) -> None:
     """``wino_attend`` over an 8-bit cache."""
     where = "wino_attend_scaled"
     qh, oh, scale = _attend_args(q, out, batch, ws, scale, where)
-    _check(lib().wino_attend_scaled(qh, oh, scale, batch, batch.scales, _ptr(ws), _nbytes(ws), _stream(stream)), where)
+    status = lib().wino_attend_scaled(qh, oh, scale, batch, batch.scales, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream))
+    if status != WINO_OK:
+        raise WinoError(status, where)
 
 
 def wino_read_device_status(ws, stream=None) -> int:
