@@ -249,9 +249,9 @@ struct alignas(16) Shared {
     int32_t abort;
     float2 ml[2][kTileM];
     alignas(16) uint8_t scale[kAll][kScaled ? kStageN : 16];
-    // Of a part, by converting warp: the first two of its slots whose K or V is held as NaN, kNoSlot behind them.  Two, since a
-    // row sees all slots before its limit but one.
-    int2 nan[kScaled ? kParts : 1][4];
+    // Of a part: the first two of its slots whose K or V is held as NaN, kNoSlot where there are none.  Two suffice, since a row
+    // sees all slots before its limit but one.
+    alignas(8) int32_t nan[kScaled ? kParts : 1][2];
 };
 
 template <bool kBf16>
@@ -331,7 +331,7 @@ __device__ __forceinline__ U warp_scan(U x, int lane)  // inclusive
 }
 
 // The planning warp: cuts the work and hands this CTA's run out part by part.  U is unsigned.  kMostTiles: row tiles of a task.
-template <typename U, typename S, int kMostTiles = 2>
+template <typename U, typename S, int kMostTiles = 2, bool kOverCodes = false>
 __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
 {
     constexpr int kCost = kMostTiles == 1 ? kFewTaskCost : kTaskCost;
@@ -494,6 +494,8 @@ __device__ __forceinline__ void plan(const AttendArgs &a, S &sh, int lane)
                 break;
             if (lane == 0) {
                 sh.parts[slot] = part;
+                if constexpr (kOverCodes)
+                    sh.nan[slot][0] = sh.nan[slot][1] = kNoSlot;
                 ptx::mbar_arrive(ptx::smem_u32(&sh.part_full[slot]));
             }
             __syncwarp();
@@ -907,17 +909,6 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 if (!warp_wait(o_done(g), (done - 1u) & 1u, &sh.abort))
                     break;
                 ptx::tc_fence_after();
-                if constexpr (kScaled) {
-                    // what was noted of this warpgroup's slot tiles is there, of the other's maybe
-                    const int2 *const nan = sh.nan[reader.slot()];
-                    if (__builtin_expect(min(min(nan[0].x, nan[1].x), min(nan[2].x, nan[3].x)) != kNoSlot, 0) && valid) {
-                        const RowSees sees = row_sees(a.b, part.q, i);
-#pragma unroll 1
-                        for (int k = 0; k < 4; ++k)
-                            if ((nan[k].x < sees.lim && nan[k].x != sees.hole) || (nan[k].y < sees.lim && nan[k].y != sees.hole))
-                                l = NAN;
-                    }
-                }
             }
             // Columns [c0, c1) of O, as f0 O_0 + f1 O_1 where two warpgroups join.
             float f0 = 1.f, f1 = 0.f;
@@ -939,6 +930,14 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                 sum = m0.y * f0 + m1.y * f1;
                 c0 = g * (DP / 2);
                 c1 = c0 + DP / 2;
+            }
+            if constexpr (kScaled) {  // what the converting warps found of the part is there: its last tile has been used
+                const int2 nan = *reinterpret_cast<const int2 *>(sh.nan[reader.slot()]);
+                if (__builtin_expect(nan.x != kNoSlot, 0) && valid) {
+                    const RowSees sees = row_sees(a.b, part.q, i);
+                    if ((nan.x < sees.lim && nan.x != sees.hole) || (nan.y < sees.lim && nan.y != sees.hole))
+                        sum = NAN;
+                }
             }
             if (any) {
                 const uint32_t t_o = lanes + C::kTmemO + (uint32_t)(two ? g * DP : 0);
@@ -1038,9 +1037,9 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
         ptx::regs_dec<kScaled ? 72 : 88>();
         if (warp == kWarpPlan) {
             if (a.wide)
-                plan<uint64_t>(a, sh, lane);
+                plan<uint64_t, SharedBlock, 2, kScaled>(a, sh, lane);
             else
-                plan<uint32_t>(a, sh, lane);
+                plan<uint32_t, SharedBlock, 2, kScaled>(a, sh, lane);
         } else if (warp == kWarpK || warp == kWarpV) {
             // -------------------------------------------------------- copies of Q and K, and of V
             // The issue of small boxes bounds a warp (68 clocks per box of 16 slots x 64 dims from 16 lanes, 174 from one
@@ -1349,12 +1348,10 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
             // Tiles in the order in which the MMAs take them: the first scores' K, then K and V in turn, then the last V.
             const int32_t n = part.n, lead = min(n, (part.flags & kTwo) != 0 ? 1 : 2);
             const int32_t slots = part.kv_end - part.j0 * kTileN;  // from the part's first on
-            int2 &noted = sh.nan[reader.slot()][warp & 3];
-            if (lane == 0)
-                noted = make_int2(kNoSlot, kNoSlot);
+            int32_t *const nan = sh.nan[reader.slot()];
             __syncwarp();
             if (lane == 0)
-                done_with();  // the softmax warps hold the part until its last tile has been used
+                done_with();  // the softmax warps hold the part, and its `nan`, until its last tile has been used
             ++reader.count;
             bool good = true;
             int32_t next_k = 0, next_v = 0;
@@ -1407,13 +1404,14 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                         most = max(most, f[k]);
                 }
                 if (__builtin_expect(__any_sync(0xffffffffu, most == kScaleNan), 0)) {
-#pragma unroll 1
-                    for (int k = 0; k < 32; ++k) {  // the warp's 16 slots of each half
-                        const int r = (k >> 4) * kHalfN + (warp & 3) * 16 + (k & 15);
-                        const int32_t rest = left + kTileN, slot = part.kv_end - rest + r;
-                        if (lane == 0 && r < rest && sh.scale[stage][r] == kScaleNan && slot != noted.x)
-                            noted = slot < noted.x ? make_int2(slot, noted.x) : make_int2(noted.x, min(noted.y, slot));
+                    // a slot of the warp's 16 of each half per lane
+                    const int r = (lane >> 4) * kHalfN + (warp & 3) * 16 + (lane & 15);
+                    if (r < left + kTileN && sh.scale[stage][r] == kScaleNan) {
+                        const int32_t slot = part.kv_end - left - kTileN + r, least = atomicMin(&nan[0], slot);
+                        if (slot != least)
+                            atomicMin(&nan[1], max(slot, least));
                     }
+                    __syncwarp();
                 }
                 ptx::fence_proxy_async();
                 __syncwarp();
