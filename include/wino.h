@@ -576,7 +576,8 @@ WINO_API int wino_cache_read(const wino_heads *k, const wino_heads *v, const win
  * of the G query heads to a kv head up to 8, G / g <= 2 and n_rows <= n_seq *
  * floor(8 / g).  Those have a kernel of their own, with weights in fp16 whatever
  * the element type (those below 2^-23 of a row's largest to steps of 2^-33 of it,
- * V's scales included in both).  Codes and scales in slots that no row of the
+ * V's scales included in both), and queries too (elements below 2^-28 of a row and
+ * head's largest to steps of 2^-38 of it).  Codes and scales in slots that no row of the
  * sequence sees have no effect.
  */
 WINO_API int wino_attend_scaled(const wino_heads *q, const wino_heads *out, float scale, const wino_kv_batch *b,

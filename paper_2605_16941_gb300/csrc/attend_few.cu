@@ -27,7 +27,7 @@
 // background, gain nothing that the cut does not, and cost short calls 0.3 us; two CTAs of 7 warps an SM 109 for the one long
 // token.  Codes read by the lanes themselves, to registers or by cp.async, 205 to 223 and 137 to 143: such reads ran at 13 bytes
 // a clock and SM, whatever was in flight.  11 warps of 168 registers instead of 15 of 128: 210 and 140 against 223 and 143 with
-// cp.async.
+// cp.async.  With 128 dims 32 bytes of registers spill.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -701,6 +701,9 @@ double few_units(const wino_kv_batch &b)
 // heads to a kv head over up to 32767 slots 154 and 330, one over 262144 97 and about 180, one over 300 9.1 and 13; 64 of 16 heads
 // to a kv head over up to 16000 142 and 174, of 32 (four tiles) 134 and 107. Two tiles of rows gain less and would lose
 // the bits of wino_attend over the values: 64 sequences of 4 rows over up to 16000 252 and 279, one over 262144 171 and 181.
+// The host does not know the lengths, so averages decide: 127 single tokens over up to 8000 with a chunk of 100 rows behind 7900
+// take 307 here and 474 there (the tokens alone 200 and 410), but 2 sequences of 64 rows over 4000 in a batch of 64 whose others are
+// absent 94 and 35.
 bool few_rows(const wino_kv_batch &b)
 {
     const int32_t group = few_group(b);

@@ -44,8 +44,10 @@
 // scheduler), K's and V's one after the other: 4 x 512 rows of 32 heads over 8-bit caches of 1605 to 3890 slots 69 us, 57 over 16-bit ones.
 // Shared memory alone would take 2560 clocks per pair of tiles at 128 bytes a clock (MMAs 1536, copies 256, conversion 768).
 // Tried, same case: codes straight from global memory to registers 122 (latency), eight warps for them 84 (the other roles' registers
-// then do not suffice), the next half tile's codes read while one is written 89, 44 bytes of spilled registers in any role 79,
-// stages of 64 slots 70.5.
+// then do not suffice), the next half tile's codes read while one is written 89, stages of 64 slots 70.5, a form that spilled
+// registers in its loops 79 (spills of 44 bytes in the planning warp and ahead of the roles cost nothing; now there are none).
+// Code counts: a tenth of the warps' stalls is for instructions, and one wait and ten instructions more per part in the softmax's role
+// cost prompts 5 %.
 //
 // Times in these comments are of calls replayed from a CUDA graph on one input, both sides of a rule on one device.
 //
@@ -94,7 +96,6 @@ constexpr float kTopBits[2] = {9.9f, 0.f};     // the P of a score of m is 2^thi
 constexpr float kFarBits = 65536.f;            // up to here m sl2 is rounded by 2^-8 at most: P stays below 65504
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kSharedBytes = 3 * 1024;  // for struct Shared, behind the tiles
-constexpr int kStageN = kTileN;  // slots of a stage of codes
 constexpr uint32_t kHalfBytes = kTileN * 128;  // 128 rows of 64 elements: one 128-byte swizzled block
 // Where slot row r, dims 64 h .. 64 h + 63 of a K or V tile lie: (r / 8) group + h half + (r % 8) 128 bytes.  With 128 dims
 // one copy brings both halves of a page's rows, interleaved by groups of 8 rows, if the cache's strides let one
@@ -219,7 +220,7 @@ struct Config {
     static constexpr int kSlotsK = kScaled ? 0 : (DP == 128 ? 2 : 5), kSlotsV = kScaled ? (DP == 128 ? 4 : 6) : (DP == 128 ? 3 : 7);
     static constexpr int kSlots = kSlotsK + kSlotsV;
     static constexpr int kStages = kScaled ? (DP == 128 ? 1 : 2) : 0;
-    static constexpr uint32_t kStageBytes = kStageN * DP;
+    static constexpr uint32_t kStageBytes = kTileN * DP;
     static constexpr uint32_t kRing = kSlots * kTileBytes + 2 * kStages * kStageBytes;
     static constexpr uint32_t kShared = kSharedBytes + (kScaled && DP == 64 ? 1024 : 0);
     // Tensor memory columns of warpgroup g: S at kTmemS + g 128, P at kTmemP + g kStrideP, O at kTmemO + g DP.  With 64 dims
@@ -248,7 +249,7 @@ struct alignas(16) Shared {
     uint32_t tmem;
     int32_t abort;
     float2 ml[2][kTileM];
-    alignas(16) uint8_t scale[kAll][kScaled ? kStageN : 16];
+    alignas(16) uint8_t scale[kAll][kScaled ? kTileN : 16];
     // Of a part: the first two of its slots whose K or V is held as NaN, kNoSlot where there are none.  Two suffice, since a row
     // sees all slots before its limit but one.
     alignas(8) int32_t nan[kScaled ? kParts : 1][2];
@@ -1093,7 +1094,7 @@ __global__ void __launch_bounds__(kAttendThreads<kScaled>, 1)
                     // codes and scales, a box and an untiled copy per page
                     const int32_t box_rows = a.box_rows;
                     for (int32_t x = 0; x < n; ++x) {
-                        const int32_t first = part.j0 * kTileN + x * kStageN;
+                        const int32_t first = part.j0 * kTileN + x * kTileN;
                         const int32_t boxes = min(a.boxes, (part.kv_end - first + box_rows - 1) / box_rows);
                         const int32_t at = first + lane * box_rows;
                         const int32_t entry = page_entry(a, at);

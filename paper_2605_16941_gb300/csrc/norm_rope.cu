@@ -10,12 +10,12 @@
 // (us, replayed; floors from 6.7 TB/s): 64 rows of 32 + 2 x 8 heads of 128 4.7 (one chain of loads: lengths, pages, rows); 2048 rows
 // of 32 + 2 x 32 heads with three axes (101 MB) 21 (floor 15); 13481 rows of 32 + 2 x 8 heads with weights per head (331 MB) 65 (49);
 // 28931 rows into an 8-bit cache (651 MB) 133 (97).  The rest is instructions, some 290 per 16 elements of a lane with the look-up, at 62 % of the
-// issue slots.  What counted: the rotation's two layouts as branches, not as selects of
+// issue slots.  What counted, as it was measured then: the rotation's two layouts as branches, not as selects of
 // registers (2048 rows 56 and 31), shared weights in shared memory (28931 rows, read back, 198 and 220), cosines read where they are
 // used instead of held in registers, some of which spilled (2048 rows 21 and 24, 28931 136 and 156).  3 CTAs an SM: with 4
-// registers spill (27 instead of 21, 144 instead of 136; both with 16 rows of a CTA at most).  Rows of a CTA: the
-// least that makes as few full waves of CTAs as there can be, up to 32 (2048 rows: 5 in one wave 24, 4 in one and an eighth 27;
-// 13481 rows: 30 in one wave 65.4, 15 in two 67.4; up to 64 the same).
+// registers spill (27 instead of 21, 144 instead of 136, as it was with 16 rows of a CTA at most).  Rows of a CTA: the
+// least that makes as few full waves of CTAs as there can be, up to 32 (2048 rows: 5 in one wave 20.7, 4 in one and an eighth
+// 27.3; 13481 rows: 30 in one wave 64.8, 15 in two 67.2; up to 64 the same).
 #include <type_traits>
 
 #include "e4m3.cuh"
