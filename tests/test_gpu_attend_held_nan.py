@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 import paper_2605_16941_gb300 as wino  # noqa: E402
 from cache8_helpers import BF, FP, NAN, attend8, make_kv8  # noqa: E402
-from kv_helpers import CAUSAL, FULL, SHADOW, add_rows, check, sees  # noqa: E402
+from kv_helpers import CAUSAL, FULL, SHADOW, add_rows, check_on_device, sees  # noqa: E402
 
 CASES = {
     # name: (mask, sequences, slots of the first sequence that are held as NaN, other arguments of make_kv)
@@ -42,7 +42,7 @@ def test_rows_that_see_it_and_no_others(name, of, dim, dtype):
     mask, seqs, slots, kw = CASES[name]
     c = add_rows(make_kv8(mask, seqs, heads=4, kv_heads=2, dim=dim, dtype=dtype, gap=1, **kw))
     ws = attend8(c)
-    check(c)
+    check_on_device(c)
     without = c.out.clone()
     for slot in slots:
         for x in of:
